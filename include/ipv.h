@@ -19,6 +19,16 @@
  *   ipv_ckv_step     append, then compress when the memory cap is reached
  *   ipv_ckv_stream   many frames through that loop in one call
  *
+ * Around the compressed cache, what a model needs to answer from it ("Paged
+ * cache" below):
+ *
+ *   ipv_page_write   rows of keys and values into pages: keys rotated to their
+ *                    position, rows quantised to 8 or 4 bits as they are written
+ *   ipv_page_read    rows out of pages, dequantised, keys rotated back
+ *   ipv_attend       attention of new tokens (one or many) over the pages or
+ *                    over the cache itself, causal, with a sliding window and
+ *                    first rows that stay visible
+ *
  * A `mode` argument (IPV_MODE_* bits, 0 = the method as published) selects the
  * variants of the paper's ablation (Tab. 5: TaR Reverse, VaN Reverse, TaR
  * between consecutive frames) and the head-shared reading of the scores.
@@ -108,10 +118,13 @@ enum {
                                   compaction then moves nothing) */
   IPV_DEV_BAD_KEEP = 8u,       /* keep_idx[j] outside [j, n) or not above keep_idx[j-1]: the compaction
                                   chunk (512 rows) holding row j was not moved */
-  IPV_DEV_NAN = 16u,           /* a candidate score is NaN: its rank is unspecified */
-  IPV_DEV_WAIT_TIMEOUT = 32u   /* compaction: a chunk's bounded wait expired or its walk's counters were
+  IPV_DEV_NAN = 16u,           /* a candidate score is NaN: its rank is unspecified; ipv_page_write: an infinite
+                                  or NaN element in a block of a quantised row */
+  IPV_DEV_WAIT_TIMEOUT = 32u,  /* compaction: a chunk's bounded wait expired or its walk's counters were
                                   not zero (a workspace shared by overlapping calls); its rows were not
                                   moved */
+  IPV_DEV_BAD_PAGE = 64u       /* paged cache: a page_table entry outside [0, pages): ipv_page_write left the
+                                  row out, ipv_page_read and ipv_attend read page 0 in its place */
 };
 
 /*
@@ -337,6 +350,105 @@ ipv_status ipv_ckv_stream(const ipv_shape* shape, void* K, void* V, int32_t* fra
                           int32_t rows, int32_t first_frame_id, int32_t mem_cap, int32_t budget, double alpha,
                           int32_t recent_frames, uint32_t mode, const double* cv_tau, float* tar, float* van,
                           int32_t* keep_idx, void* ws, size_t ws_bytes, int32_t* passes, void* stream);
+
+/* ------------------------------------------------------------ paged cache
+ * A pool holds `pages` pages; a page holds page_rows rows of every layer and
+ * KV head. K_pages and V_pages are [pages, layers, kv_heads, page_rows, X]:
+ *   IPV_PAGES_BF16, IPV_PAGES_F32   X = D elements of that type
+ *   IPV_PAGES_FP8   X = D bytes: e4m3 elements (1 sign, 4 exponent, 3 mantissa
+ *                   bits, bias 7, largest 448, 0x7f / 0xff NaN, no infinities)
+ *   IPV_PAGES_FP4   X = D / 2 bytes: e2m1 elements (0, 0.5, 1, 1.5, 2, 3, 4, 6
+ *                   and their negatives), element 2i in the low half of byte i
+ * The quantised formats keep one scale for each 32 consecutive elements of a
+ * row, K_scales and V_scales [pages, layers, kv_heads, page_rows, D / 32] bytes:
+ * an element stands for its value times 2^(byte - 127); byte 255: the block is NaN.
+ * Row j of stream b (its position) is slot j % page_rows of page
+ * page_table[b * table_cols + j / page_rows] (int32, device). Pages may be
+ * shared between streams that only read them. page_table NULL: stream b's rows
+ * are page b (then table_cols = 1, and a cache K, V [B, L, H, S, D] of this
+ * library is itself such a pool, of B pages of S rows).
+ * Pools and K/V rows are 16-byte aligned; scales, tables and lse 4-byte.
+ * Every count is a HOST array with one entry per stream. The workspace of
+ * ipv_page_write and ipv_page_read is the 256 bytes of the error word; that of
+ * ipv_attend is sized by ipv_attend_workspace_bytes and must have been zeroed
+ * when it was allocated. Calls that share a workspace must not overlap in time.
+ * Strides are HOST arrays, in elements, each a multiple of 8; the elements of a
+ * row are contiguous.
+ */
+typedef enum { IPV_PAGES_BF16 = 0, IPV_PAGES_F32 = 1, IPV_PAGES_FP8 = 2, IPV_PAGES_FP4 = 3 } ipv_page_format;
+
+typedef struct {
+  int32_t pages;      /* P >= 1 */
+  int32_t layers;     /* L >= 1 */
+  int32_t kv_heads;   /* H >= 1 */
+  int32_t page_rows;  /* T >= 1 */
+  int32_t head_dim;   /* D: 32, 64, 128 or 256 */
+  int32_t format;     /* ipv_page_format */
+} ipv_page_shape;
+
+/*
+ * Write rows[b] rows of every layer of [first_layer, first_layer + layers) and
+ * every KV head into the pool, at positions first_row[b], first_row[b] + 1, ...
+ * of stream b (0 rows: the stream is left alone). Row i of (b, l, h) is at
+ * K + b * strides[0] + l * strides[1] + h * strides[2] + i * strides[3] (l counted
+ * from the call's first layer), V alike, in `dtype` (ipv_dtype).
+ * rotary (device, [rotary_rows, D / 2, 2] fp32, the cosine and sine of each
+ * position and pair; NULL: no rotation) turns the pairs (d, d + D/2) of a key:
+ *   k'[d] = k[d] cos - k[d + D/2] sin,   k'[d + D/2] = k[d + D/2] cos + k[d] sin
+ * in fp32, each product and sum rounded once; positions must be below
+ * rotary_rows. Quantised formats: a block's scale is the smallest power of two 2^e,
+ * -126 <= e, that keeps its largest magnitude within the type's largest value (so
+ * nothing is cut off), and the elements round to nearest, ties to even, after the
+ * division, which is exact. A block that holds an infinity or NaN becomes NaN
+ * and raises IPV_DEV_NAN.
+ * Positions of one call that lie in the same page and slot (pages shared by two
+ * streams that both write) are written in no fixed order.
+ */
+ipv_status ipv_page_write(const ipv_page_shape* pool, void* K_pages, void* V_pages, uint8_t* K_scales,
+                          uint8_t* V_scales, const int32_t* page_table, int32_t table_cols, int32_t streams,
+                          const int32_t* first_row, const int32_t* rows, int32_t first_layer, int32_t layers,
+                          const void* K, const void* V, int32_t dtype, const int64_t* strides, const float* rotary,
+                          int32_t rotary_rows, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The way back: rows[b] rows from position first_row[b] on into K and V
+ * (described as above), each element's value rounded once to `dtype`; with
+ * rotary the keys are turned back (by the negative angle, in fp32).
+ */
+ipv_status ipv_page_read(const ipv_page_shape* pool, const void* K_pages, const void* V_pages, const uint8_t* K_scales,
+                         const uint8_t* V_scales, const int32_t* page_table, int32_t table_cols, int32_t streams,
+                         const int32_t* first_row, const int32_t* rows, int32_t first_layer, int32_t layers, void* K,
+                         void* V, int32_t dtype, const int64_t* strides, const float* rotary, int32_t rotary_rows,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of device workspace (zeroed when allocated) that every ipv_attend call with this pool, at most `streams`
+   streams, q_heads query heads and at most max_rows queries a stream needs. */
+ipv_status ipv_attend_workspace_bytes(const ipv_page_shape* pool, int32_t streams, int32_t q_heads, int32_t max_rows,
+                                      size_t* bytes);
+
+/*
+ * Attention of q_rows[b] queries of every stream over one layer of the pool.
+ * Query i of stream b stands at position p = q_first[b] + i and sees row j when
+ *   j < n_tokens[b],  j <= p,  and, with window > 0,  j > p - window or j < sinks.
+ * Query head a reads KV head a / (q_heads / kv_heads). With x_j = scale * (q . K_j):
+ *   out = sum_j exp(x_j) V_j / sum_j exp(x_j),   lse = log(sum_j exp(x_j))
+ * over the rows seen; a query that sees none gets zeros and lse = -infinity.
+ * Rows that a query does not see do not reach its result, whatever they hold
+ * (infinities and NaN included). New tokens attend among themselves once their own rows
+ * are written: q_first[b] = n_tokens[b] - q_rows[b].
+ * q and out are bf16 (fp32 for IPV_PAGES_F32); query i of head a of stream b is
+ * at q + b * q_strides[0] + a * q_strides[1] + i * q_strides[2], out alike; lse (fp32,
+ * may be NULL) is [streams, q_heads, max_rows], written for i < q_rows[b].
+ * Queries are expected rotated to their positions where the keys are. Products
+ * accumulate in fp32 and the softmax is fp32; its weights are rounded to bf16 before
+ * they multiply V (not with IPV_PAGES_F32). One call gives the same bits every time.
+ */
+ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const void* V_pages, const uint8_t* K_scales,
+                      const uint8_t* V_scales, const int32_t* page_table, int32_t table_cols, int32_t streams,
+                      const int32_t* n_tokens, const int32_t* q_first, const int32_t* q_rows, int32_t layer,
+                      const void* q, const int64_t* q_strides, int32_t q_heads, int32_t max_rows, double scale,
+                      int32_t window, int32_t sinks, void* out, const int64_t* out_strides, float* lse, void* ws,
+                      size_t ws_bytes, void* stream);
 
 /* Reset the workspace's device error word (a small kernel on `stream`). */
 ipv_status ipv_clear_device_errors(void* ws, size_t ws_bytes, void* stream);

@@ -1,0 +1,905 @@
+// Attention of new tokens over a paged cache.
+//
+// For a query q at position p, x_j = scale * (q . K_j) over the rows j it sees,
+// out = sum_j 2^(c x_j - m) V_j / sum_j 2^(c x_j - m), c = log2 e: one pass over
+// the rows with a running maximum m, the running sum and the running weighted
+// sum of V rescaled when m grows. The rows of a split or of a wave are done
+// apart and joined by the same rule.
+//
+// Scores are computed transposed, S^T = K Q^T, and so is O^T = V^T P^T: the
+// matrix instruction leaves in each lane scores of one query, so a softmax
+// reduces within a lane and across two or four of them, and the same registers,
+// rounded to bf16, are the second product's operand as they stand: its keys are
+// taken in the order in which the first product left them, and the transposing
+// LDS read brings V's elements in that order.
+//
+// All query heads of a KV head are rows of one operand (row r: token r / G, head
+// r % G), so the cache is read once for them.
+#pragma once
+
+#include "ipv_pages.hpp"
+
+namespace ipv {
+
+constexpr int kAttendStreams = 96;  // streams of one launch (their counts travel in its arguments)
+constexpr int kMaxSplits = 64;      // parts of a key range that are joined: a lane each
+
+struct AttendStream {
+  int32_t n, first, rows;  // rows of the cache; position of the first query; queries
+  int32_t start;           // its first workgroup
+  int32_t tiles, splits;   // row tiles of a KV head; parts of a tile's keys
+};
+
+struct AttendArgs {
+  Pool pool;
+  int64_t layer_row;  // rows of a page before the layer's first head
+  const char* q;
+  char* out;
+  float* lse;
+  int64_t q_b, q_h, q_m, o_b, o_h, o_m;  // strides, elements
+  int32_t b0, H, G, max_rows;
+  FastDiv G_div;
+  float c;  // scale * log2(e)
+  int32_t window, sinks;
+  float* part;     // unnormalised sums of a split's rows, [workgroup][row][D]
+  float* part_ml;  // their maxima and sums of weights, [workgroup][row][2]
+  uint32_t* err;
+  int32_t streams, blocks;
+  AttendStream s[kAttendStreams];
+};
+
+// The key tiles of a range of queries: those that hold one of the first rows
+// that stay visible, then those from the oldest row seen to the newest.
+struct KeyTiles {
+  int32_t sink_tiles, main_first, count;
+  int32_t lo, hi, sink_end;  // rows [0, sink_end) and [lo, hi) are seen by some query
+  __host__ __device__ KeyTiles(int32_t n, int32_t p_lo, int32_t p_hi, int32_t window, int32_t sinks, int32_t BN) {
+    hi = p_hi < n ? p_hi + 1 : n;
+    lo = window > 0 && p_lo >= window ? p_lo - window + 1 : 0;
+    sink_end = window > 0 ? (sinks < lo ? sinks : lo) : 0;
+    if (sink_end > hi) sink_end = hi;
+    main_first = lo / BN;
+    const int32_t sink = (sink_end + BN - 1) / BN, main_last = (hi + BN - 1) / BN;
+    sink_tiles = sink < main_first ? sink : main_first;
+    count = sink_tiles + (main_last > main_first ? main_last - main_first : 0);
+  }
+  __device__ int32_t tile(int32_t t) const { return t < sink_tiles ? t : main_first + t - sink_tiles; }
+  __device__ bool some(int32_t j) const { return j < hi && (j >= lo || j < sink_end); }
+};
+
+// Whether a query at p sees row j of n.
+__device__ __forceinline__ bool sees(int32_t j, int32_t p, int32_t n, int32_t window, int32_t sinks) {
+  return j <= p && j < n && (window <= 0 || j > p - window || j < sinks);
+}
+// Whether every query of [p_lo, p_hi] sees all rows of [j0, j1).
+__device__ __forceinline__ bool all_see(int32_t j0, int32_t j1, int32_t p_lo, int32_t p_hi, int32_t n, int32_t window,
+                                        int32_t sinks) {
+  return j1 - 1 <= p_lo && j1 <= n && (window <= 0 || j0 > p_hi - window || j1 <= sinks);
+}
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
+constexpr float kLn2 = 0.693147180559945309f;
+
+// A maximum as the exponent's shift: a query that has seen nothing has -inf,
+// and nothing to shift.
+__device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// Maximum and sum over the lanes that hold the same query: 32 apart (two
+// halves of a 32-wide tile), or 16 and 32 apart.
+template <int N>
+__device__ __forceinline__ float lanes_max(float v) {
+  if (N == 4) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <int N>
+__device__ __forceinline__ float lanes_sum(float v) {
+  if (N == 4) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
+  const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)v, lane, kWave);
+  const uint32_t hi = (uint32_t)__shfl((int)(uint32_t)((uint64_t)v >> 32), lane, kWave);
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// Four bf16 of one column from four rows of LDS: the 16 lanes of a group give
+// the addresses of a 4 x 16 block, row by row, 8 bytes each; lane i receives
+// column i.
+typedef short S16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ U32x2 lds_column4(const char* p) {
+  return __builtin_bit_cast(U32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((S16x4 __attribute__((address_space(3)))*)p));
+}
+
+// The block's place: its stream, KV head, row tile and part of the keys.
+// Workgroups go to the eight XCDs in turn; each XCD takes a run of consecutive
+// places, so the tiles and parts that read one head's rows share its L2.
+struct Place {
+  int32_t slot, b, h, tile, split;
+};
+__device__ __forceinline__ Place place_of(const AttendArgs& a) {
+  const uint32_t per = (uint32_t)(a.blocks + 7) / 8u;
+  Place p;
+  p.slot = (int32_t)((blockIdx.x % 8u) * per + blockIdx.x / 8u);
+  p.b = 0;
+  if (p.slot >= a.blocks) {
+    p.slot = -1;
+    return p;
+  }
+  int lo = 0, hi = a.streams - 1;  // the last stream that starts at or before the slot (empty ones hold no slot)
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (a.s[mid].start <= p.slot) lo = mid;
+    else hi = mid - 1;
+  }
+  p.b = lo;
+  const AttendStream& s = a.s[lo];
+  uint32_t x = (uint32_t)(p.slot - s.start);
+  p.split = (int32_t)(x % (uint32_t)s.splits);
+  x /= (uint32_t)s.splits;
+  // the last row tile first: under a causal mask it has the most keys
+  p.tile = s.tiles - 1 - (int32_t)(x % (uint32_t)s.tiles);
+  p.h = (int32_t)(x / (uint32_t)s.tiles);
+  return p;
+}
+
+__device__ __forceinline__ bool bf16_special(uint32_t w) {  // an infinity or NaN in either half
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+
+// Zero the infinities and NaN among eight bf16; whether there were any.
+__device__ __forceinline__ bool clear_special(Raw16& r) {
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (!bf16_special(r.w[i])) continue;
+    any = true;
+    if ((r.w[i] & 0x7f80u) == 0x7f80u) r.w[i] &= 0xffff0000u;
+    if ((r.w[i] & 0x7f800000u) == 0x7f800000u) r.w[i] &= 0xffffu;
+  }
+  return any;
+}
+
+// One element of V, for the rare rows that need care.
+template <int F, int D>
+__device__ __forceinline__ float v_element(const Pool& p, int64_t row, int d) {
+  float f[8];
+  decode_row8<F, D>(p.V, p.Vs, row, d & ~7, f);
+  float v = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i == (d & 7)) v = f[i];
+  return v;
+}
+
+// Scale bytes of a row as a 64-bit word.
+template <int D>
+__device__ __forceinline__ uint64_t load_scales(const uint8_t* scales, int64_t row) {
+  const uint8_t* p = scales + row * (D / kScaleBlock);
+  if (D == 32) return *p;
+  if (D == 64) return *reinterpret_cast<const uint16_t*>(p);
+  if (D == 128) return *reinterpret_cast<const uint32_t*>(p);
+  const uint32_t lo = reinterpret_cast<const uint32_t*>(p)[0], hi = reinterpret_cast<const uint32_t*>(p)[1];
+  return ((uint64_t)hi << 32) | lo;
+}
+__device__ __forceinline__ float scale_at(uint64_t w, int block) { return scale_of((uint32_t)(w >> (8 * block)) & 255u); }
+
+// Eight elements at 8 * s of a 16-byte (or shorter) piece of stored bytes, as bf16.
+template <int F>
+__device__ __forceinline__ Raw16 piece8(const uint32_t* w, int s, float scale) {
+  if (F == kFmtFp8) return fp8_to_bf16(w[2 * s], w[2 * s + 1], scale);
+  if (F == kFmtFp4) return fp4_to_bf16(w[s], scale);
+  return Raw16{w[0], w[1], w[2], w[3]};
+}
+
+template <int BYTES>
+__device__ __forceinline__ void load_piece(const char* p, uint32_t* w) {
+  if (BYTES == 16) {
+    const Raw16 r = load16(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = r.w[i];
+  } else if (BYTES == 8) {
+    const U32x2 r = *reinterpret_cast<const U32x2*>(p);
+    w[0] = r.x, w[1] = r.y;
+  } else {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  }
+}
+
+// ---------------------------------------------------------------- few rows
+// Up to 16 * NB rows a KV head (single tokens of grouped heads): bound by the
+// bytes of the cache. Each wave takes key tiles of its own (32 rows), K straight
+// into the matrix operand's layout, V through an LDS tile that only this wave
+// uses; the next tile's rows are in flight while one is computed. The four waves
+// join through LDS, the splits of a key range through k_attend_join.
+constexpr int kFewWaves = 4;
+constexpr int kFewKeys = 32;
+
+template <int F, int D>
+struct FewCfg {
+  static constexpr int RB = fmt_row_bytes(F, D);
+  static constexpr int KQ = RB / 4;                   // bytes of a K row that a lane holds
+  static constexpr int KB = KQ < 16 ? KQ : 16;        // bytes a load
+  static constexpr int KN = KQ / KB;
+  static constexpr int KE = KB * 8 / fmt_bits(F);     // elements a load
+  static constexpr int CPR = RB / 16;                 // 16-byte chunks of a V row
+  static constexpr int NV = CPR >= 2 ? CPR / 2 : 1;   // chunks a lane loads
+  static constexpr int VE = 128 / fmt_bits(F);        // elements a chunk
+  // V's 16-byte chunks of bf16 are stored at ch ^ swizzle(row): eight rows of a
+  // transposing read then lie in different banks
+  static __device__ int swz(int row) {
+    return D >= 128 ? 2 * (row & 7) : D == 64 ? 2 * ((row >> 1) & 3) : 2 * ((row >> 2) & 1);
+  }
+};
+
+template <int D, int NB>
+constexpr size_t few_wave_lds() {
+  const size_t tile = (size_t)kFewKeys * D * 2, join = (size_t)16 * NB * (D + 4) * 4;
+  return tile > join ? tile : join;
+}
+
+template <int F, int D, int NB>
+__global__ __launch_bounds__(64 * kFewWaves) void k_attend_few(AttendArgs a) {
+  using C = FewCfg<F, D>;
+  __shared__ __attribute__((aligned(16))) char lds[kFewWaves][few_wave_lds<D, NB>()];
+  __shared__ float lds_ml[kFewWaves][16 * NB][2];
+  const Place pl = place_of(a);
+  if (pl.slot < 0) return;  // the whole workgroup
+  const AttendStream st = a.s[pl.b];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, g = lane / 16, l16 = lane % 16;
+  const int32_t n = st.n, p_lo = st.first, p_hi = st.first + st.rows - 1, R = st.rows * a.G;
+  const int b = a.b0 + pl.b;
+  const int64_t head_row = a.layer_row + (int64_t)pl.h * a.pool.T.d;
+  const KeyTiles kt(n, p_lo, p_hi, a.window, a.sinks, kFewKeys);
+  const int32_t t_end = (int32_t)((int64_t)kt.count * (pl.split + 1) / st.splits);
+  int32_t t = (int32_t)((int64_t)kt.count * pl.split / st.splits) + wave;
+
+  // queries: lane's row and, in its pieces' order, its elements
+  Bf16x8 q[NB][D / 32];
+  int32_t pos[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int r = nb * 16 + l16, tok = (int)fast_div((uint32_t)min(r, R - 1), a.G_div);
+    pos[nb] = p_lo + tok;
+    const char* at = a.q + 2 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + min(r, R - 1) - tok * a.G) * a.q_h + (int64_t)tok * a.q_m);
+#pragma unroll
+    for (int c = 0; c < C::KN; ++c)
+#pragma unroll
+      for (int s = 0; s < C::KE / 8; ++s)
+        q[nb][c * (C::KE / 8) + s] = __builtin_bit_cast(Bf16x8, load16(at + 2 * ((c * 4 + g) * C::KE + 8 * s)));
+  }
+
+  F32x4 o[NB][D / 16];
+  float m[NB], l[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    m[nb] = -INFINITY, l[nb] = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) o[nb][i] = F32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  bool bad = false;
+  // row (in the pool) of the tile's key lane % 32; a key past the last is the last
+  auto row_of = [&](int32_t tt) {
+    const int32_t j = kt.tile(min(tt, kt.count - 1)) * kFewKeys + lane % 32;
+    bool x;
+    const int64_t r = pool_row(a.pool, b, (uint32_t)min(j, n - 1), &x) + head_row;
+    bad |= x;
+    return r;
+  };
+  uint32_t kr[2][C::KQ / 4], vr[C::NV][4];
+  uint64_t ks[2], vs[C::NV];
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const int64_t r = shfl64(row, kb * 16 + l16);
+      const char* p = a.pool.K + r * C::RB + g * C::KB;
+#pragma unroll
+      for (int c = 0; c < C::KN; ++c) load_piece<C::KB>(p + c * 4 * C::KB, kr[kb] + c * (C::KB / 4));
+      if (fmt_scaled(F)) ks[kb] = load_scales<D>(a.pool.Ks, r);
+    }
+#pragma unroll
+    for (int i = 0; i < C::NV; ++i) {
+      const int x = i * kWave + lane, key = (x / C::CPR) % kFewKeys;
+      const int64_t r = shfl64(row, key);
+      load_piece<16>(a.pool.V + r * C::RB + (x % C::CPR) * 16, vr[i]);
+      if (fmt_scaled(F)) vs[i] = load_scales<D>(a.pool.Vs, r);
+    }
+  };
+
+  char* tile = lds[wave];
+  int64_t row = 0, next = 0;
+  if (t < t_end) {
+    row = row_of(t);
+    next = row_of(t + kFewWaves);
+    fetch(row);
+  }
+  for (; t < t_end; t += kFewWaves) {
+    const int32_t j0 = kt.tile(t) * kFewKeys;
+    const bool full = all_see(j0, j0 + kFewKeys, p_lo, p_hi, n, a.window, a.sinks);
+    // scores of this tile's keys (the operand is built from the loaded bytes)
+    F32x4 sc[NB][2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) sc[nb][kb] = F32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < C::KN; ++c)
+#pragma unroll
+        for (int s = 0; s < C::KE / 8; ++s) {
+          const float scale = fmt_scaled(F) ? scale_at(ks[kb], ((c * 4 + g) * C::KE + 8 * s) / kScaleBlock) : 0.f;
+          const Bf16x8 k = __builtin_bit_cast(Bf16x8, piece8<F>(kr[kb] + c * (C::KB / 4), s, scale));
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            sc[nb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[nb][c * (C::KE / 8) + s], sc[nb][kb], 0, 0, 0);
+        }
+    }
+    // V into LDS as bf16; rows that no query sees become zeros, and what is
+    // infinite or NaN in rows that only some see is taken out and added below
+    bool special = false;
+#pragma unroll
+    for (int i = 0; i < C::NV; ++i) {
+      const int x = i * kWave + lane, key = x / C::CPR, col = x % C::CPR;
+      if (C::CPR == 1 && x >= kFewKeys) continue;
+      const float scale = fmt_scaled(F) ? scale_at(vs[i], col * C::VE / kScaleBlock) : 0.f;
+#pragma unroll
+      for (int s = 0; s < C::VE / 8; ++s) {
+        Raw16 v = piece8<F>(vr[i], s, scale);
+        if (!full) {
+          if (!kt.some(j0 + key)) v = Raw16{0, 0, 0, 0};
+          else special |= clear_special(v);
+        }
+        *reinterpret_cast<Raw16*>(tile + key * (D * 2) + 16 * ((col * (C::VE / 8) + s) ^ C::swz(key))) = v;
+      }
+    }
+    const int64_t here = row;
+    if (t + kFewWaves < t_end) {
+      row = next;
+      fetch(row);
+      next = row_of(t + 2 * kFewWaves);
+    }
+    // softmax: weights of 8 keys a lane, keys 4 g + i and 16 + 4 g + i
+    Bf16x8 w[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      if (!full)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!sees(j0 + kb * 16 + 4 * g + i, pos[nb], n, a.window, a.sinks)) sc[nb][kb][i] = -INFINITY;
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, sc[nb][0][i]), sc[nb][1][i]);
+      top = fmaxf(m[nb], lanes_max<4>(top) * a.c);
+      const float shift = shift_of(top), old = exp2_hw(m[nb] - shift);
+      m[nb] = top;
+      float sum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = exp2_hw(__builtin_fmaf(sc[nb][kb][i], a.c, -shift));
+          sum += e;
+          w[nb][kb * 4 + i] = (__bf16)e;
+        }
+      l[nb] = l[nb] * old + sum;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) o[nb][i] *= old;
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) {
+      const int k0 = 4 * g + l16 / 4, ch = 2 * db + (l16 % 4) / 2, in = 8 * (l16 & 1);
+      const U32x2 x = lds_column4(tile + k0 * (D * 2) + 16 * (ch ^ C::swz(k0)) + in);
+      const U32x2 y = lds_column4(tile + (k0 + 16) * (D * 2) + 16 * (ch ^ C::swz(k0 + 16)) + in);
+      const Raw16 r = {x.x, x.y, y.x, y.y};
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+        o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf16x8, r), w[nb], o[nb][db], 0, 0, 0);
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (!full && __ballot(special) != 0) {
+#pragma unroll 1
+      for (int key = 0; key < kFewKeys; ++key) {
+        if (!kt.some(j0 + key)) continue;
+        const int64_t r = shfl64(here, key);
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float v = v_element<F, D>(a.pool, r, 16 * db + 4 * g + i);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+              if (!(fabsf(v) < INFINITY) && sees(j0 + key, pos[nb], n, a.window, a.sinks)) o[nb][db][i] += v;
+          }
+      }
+    }
+  }
+  if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, kDevBadPage);
+
+  // join the waves: each scales its sums to the largest maximum
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    l[nb] = lanes_sum<4>(l[nb]);
+    if (lane < 16) lds_ml[wave][nb * 16 + lane][0] = m[nb], lds_ml[wave][nb * 16 + lane][1] = l[nb];
+  }
+  __syncthreads();
+  constexpr int STRIDE = D + 4;
+  float* mine = reinterpret_cast<float*>(lds[wave]);
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, lds_ml[w][nb * 16 + l16][0]);
+    const float f = exp2_hw(m[nb] - shift_of(top));
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db)
+      *reinterpret_cast<F32x4*>(mine + (nb * 16 + l16) * STRIDE + 16 * db + 4 * g) = o[nb][db] * f;
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < min(R, 16 * NB) * (D / 4); x += 64 * kFewWaves) {
+    const int r = x / (D / 4), d = x % (D / 4) * 4;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, lds_ml[w][r][0]);
+    F32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      sum += lds_ml[w][r][1] * exp2_hw(lds_ml[w][r][0] - shift_of(top));
+      v += *reinterpret_cast<const F32x4*>(reinterpret_cast<const float*>(lds[w]) + r * STRIDE + d);
+    }
+    if (st.splits > 1) {
+      *reinterpret_cast<F32x4*>(a.part + ((int64_t)pl.slot * (16 * NB) + r) * D + d) = v;
+      if (d == 0) {
+        float* ml = a.part_ml + ((int64_t)pl.slot * (16 * NB) + r) * 2;
+        ml[0] = top, ml[1] = sum;
+      }
+    } else {
+      const int tok = (int)fast_div((uint32_t)r, a.G_div), head = pl.h * a.G + r - tok * a.G;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      uint32_t* at = reinterpret_cast<uint32_t*>(a.out + 2 * ((int64_t)b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m + d));
+      at[0] = pack_bf16(v[0] * inv, v[1] * inv), at[1] = pack_bf16(v[2] * inv, v[3] * inv);
+      if (d == 0 && a.lse)
+        a.lse[((int64_t)b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (top + log2_hw(sum)) * kLn2;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- many rows
+// Row tiles of 32 * NQ * W rows, keys in tiles of 64 through LDS, where all waves
+// read them; the next tile's rows are in flight meanwhile.
+constexpr int kTileKeys = 64;
+
+template <int F, int D, int W>
+struct TileCfg {
+  static constexpr int RB = fmt_row_bytes(F, D);
+  static constexpr int CPR = RB / 16;
+  static constexpr int CHUNKS = kTileKeys * CPR;
+  static constexpr int NL = CHUNKS >= 64 * W ? CHUNKS / (64 * W) : 1;  // chunks a thread loads
+  static constexpr int E = 128 / fmt_bits(F);                          // elements a chunk
+  // LDS places of 16-byte chunks of bf16: K is read 16 bytes a lane from 32
+  // rows, V by transposing reads of 4 rows and 32 columns
+  static __device__ int kswz(int row) { return D >= 64 ? row & 7 : (row >> 2) & 3; }
+  static __device__ int vswz(int row) { return D >= 128 ? 4 * (row & 3) : D == 64 ? 4 * ((row >> 1) & 1) : 0; }
+};
+
+// How far a maximum may grow before the sums are rescaled to it: weights stay
+// below 2^8, which costs no bit of their bf16 or of the fp32 sums.
+constexpr float kLazy = 8.f;
+
+template <int F, int D, int W, int NQ>
+__global__ __launch_bounds__(64 * W) void k_attend_tile(AttendArgs a) {
+  using C = TileCfg<F, D, W>;
+  constexpr int BM = 32 * NQ * W, BN = kTileKeys;
+  __shared__ __attribute__((aligned(16))) char ldsK[2][BN * D * 2];
+  __shared__ __attribute__((aligned(16))) char ldsV[2][BN * D * 2];
+  __shared__ int32_t lds_special[2];
+  const Place pl = place_of(a);
+  if (pl.slot < 0) return;
+  const AttendStream st = a.s[pl.b];
+  const int lane = threadIdx.x % kWave, h = lane / 32, l32 = lane % 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int32_t n = st.n, R = st.rows * a.G, r0 = pl.tile * BM;
+  const int b = a.b0 + pl.b;
+  const int64_t head_row = a.layer_row + (int64_t)pl.h * a.pool.T.d;
+  const int32_t p_lo = st.first + (int32_t)fast_div((uint32_t)r0, a.G_div);
+  const int32_t p_hi = st.first + (int32_t)fast_div((uint32_t)(min(r0 + BM, R) - 1), a.G_div);
+  const KeyTiles kt(n, p_lo, p_hi, a.window, a.sinks, BN);
+  const int32_t t_end = (int32_t)((int64_t)kt.count * (pl.split + 1) / st.splits);
+  int32_t t = (int32_t)((int64_t)kt.count * pl.split / st.splits);
+
+  Bf16x8 q[NQ][D / 16];
+  int32_t pos[NQ];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    const int r = min(r0 + (wave * NQ + nq) * 32 + l32, R - 1), tok = (int)fast_div((uint32_t)r, a.G_div);
+    pos[nq] = st.first + tok;
+    const char* at = a.q + 2 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + r - tok * a.G) * a.q_h + (int64_t)tok * a.q_m);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) q[nq][kk] = __builtin_bit_cast(Bf16x8, load16(at + 2 * (16 * kk + 8 * h)));
+  }
+  // the wave's own positions
+  const int32_t pw_lo = st.first + (int32_t)fast_div((uint32_t)min(r0 + wave * NQ * 32, R - 1), a.G_div);
+  const int32_t pw_hi = st.first + (int32_t)fast_div((uint32_t)min(r0 + (wave + 1) * NQ * 32 - 1, R - 1), a.G_div);
+
+  F32x16 o[NQ][D / 32];
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    m[nq] = -INFINITY, l[nq] = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) o[nq][i][k] = 0.f;
+  }
+  if (threadIdx.x < 2) lds_special[threadIdx.x] = -1;
+
+  bool bad = false;
+  auto row_of = [&](int32_t tt) {  // the pool's row of the tile's key `lane`
+    const int32_t j = kt.tile(min(tt, kt.count - 1)) * BN + lane;
+    bool x;
+    const int64_t r = pool_row(a.pool, b, (uint32_t)min(j, n - 1), &x) + head_row;
+    bad |= x;
+    return r;
+  };
+  uint32_t kr[C::NL][4], vr[C::NL][4];
+  uint64_t ks[C::NL], vs[C::NL];
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int i = 0; i < C::NL; ++i) {
+      const int x = i * 64 * W + threadIdx.x, key = (x / C::CPR) % BN;
+      const int64_t r = shfl64(row, key);
+      load_piece<16>(a.pool.K + r * C::RB + (x % C::CPR) * 16, kr[i]);
+      load_piece<16>(a.pool.V + r * C::RB + (x % C::CPR) * 16, vr[i]);
+      if (fmt_scaled(F)) ks[i] = load_scales<D>(a.pool.Ks, r), vs[i] = load_scales<D>(a.pool.Vs, r);
+    }
+  };
+  auto stage = [&](int32_t tt, int buf) {
+    const int32_t j0 = kt.tile(tt) * BN;
+    const bool full = all_see(j0, j0 + BN, p_lo, p_hi, n, a.window, a.sinks);
+    bool special = false;
+#pragma unroll
+    for (int i = 0; i < C::NL; ++i) {
+      const int x = i * 64 * W + threadIdx.x, key = x / C::CPR, col = x % C::CPR;
+      if (C::CHUNKS < 64 * W && x >= C::CHUNKS) continue;
+      const int block = col * C::E / kScaleBlock;
+#pragma unroll
+      for (int s = 0; s < C::E / 8; ++s) {
+        const int ch = col * (C::E / 8) + s;
+        *reinterpret_cast<Raw16*>(ldsK[buf] + key * (D * 2) + 16 * (ch ^ C::kswz(key))) =
+            piece8<F>(kr[i], s, fmt_scaled(F) ? scale_at(ks[i], block) : 0.f);
+        Raw16 v = piece8<F>(vr[i], s, fmt_scaled(F) ? scale_at(vs[i], block) : 0.f);
+        if (!full) {
+          if (!kt.some(j0 + key)) v = Raw16{0, 0, 0, 0};
+          else special |= clear_special(v);
+        }
+        *reinterpret_cast<Raw16*>(ldsV[buf] + key * (D * 2) + 16 * (ch ^ C::vswz(key))) = v;
+      }
+    }
+    if (special) lds_special[buf] = tt;
+  };
+
+  int64_t row = 0, next = 0;
+  if (t < t_end) {
+    row = row_of(t);
+    next = row_of(t + 1);
+    fetch(row);
+  }
+  __syncthreads();
+  if (t < t_end) stage(t, 0);
+  int buf = 0;
+  for (; t < t_end; ++t, buf ^= 1) {
+    const int64_t here = row;
+    const bool more = t + 1 < t_end;
+    if (more) {
+      row = next;
+      fetch(row);
+      next = row_of(t + 2);
+    }
+    __syncthreads();  // tile t is in LDS, and no wave reads the other buffer any more
+    const int32_t j0 = kt.tile(t) * BN;
+    const bool full = all_see(j0, j0 + BN, pw_lo, pw_hi, n, a.window, a.sinks);
+    // nothing of the tile is seen by this wave's queries
+    const bool none = j0 > pw_hi || (a.window > 0 && j0 + BN - 1 <= pw_lo - a.window && j0 >= a.sinks);
+    if (!none) {
+      F32x16 s[NQ][2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+          for (int k = 0; k < 16; ++k) s[nq][kb][k] = 0.f;
+        const int key = kb * 32 + l32;
+        const char* at = ldsK[buf] + key * (D * 2);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const Bf16x8 k = __builtin_bit_cast(Bf16x8, load16(at + 16 * ((2 * kk + h) ^ C::kswz(key))));
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq) s[nq][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[nq][kk], s[nq][kb], 0, 0, 0);
+        }
+      }
+      Bf16x8 w[NQ][4];
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+        if (!full)
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (!sees(j0 + kb * 32 + 8 * (i / 4) + 4 * h + i % 4, pos[nq], n, a.window, a.sinks)) s[nq][kb][i] = -INFINITY;
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(fmaxf(top, s[nq][0][i]), s[nq][1][i]);
+        top = lanes_max<2>(top) * a.c;
+        if (__ballot(top > m[nq] + kLazy || (m[nq] == -INFINITY && top != -INFINITY)) != 0) {
+          top = fmaxf(top, m[nq]);
+          const float old = exp2_hw(m[nq] - shift_of(top));
+          m[nq] = top;
+          l[nq] *= old;
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) o[nq][i] *= old;
+        }
+        const float shift = shift_of(m[nq]);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float e = exp2_hw(__builtin_fmaf(s[nq][kb][i], a.c, -shift));
+            l[nq] += e;
+            w[nq][kb * 2 + i / 8][i % 8] = (__bf16)e;
+          }
+      }
+#pragma unroll
+      for (int ks4 = 0; ks4 < 4; ++ks4)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+          const int k0 = ks4 * 16 + 4 * h + (lane % 16) / 4;
+          const int ch = 4 * db + 2 * ((lane / 16) % 2) + (lane % 4) / 2, in = 8 * (lane & 1);
+          const U32x2 x = lds_column4(ldsV[buf] + k0 * (D * 2) + 16 * (ch ^ C::vswz(k0)) + in);
+          const U32x2 y = lds_column4(ldsV[buf] + (k0 + 8) * (D * 2) + 16 * (ch ^ C::vswz(k0 + 8)) + in);
+          const Raw16 r = {x.x, x.y, y.x, y.y};
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq)
+            o[nq][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Bf16x8, r), w[nq][ks4], o[nq][db], 0, 0, 0);
+        }
+      if (lds_special[buf] == t) {
+#pragma unroll 1
+        for (int key = 0; key < BN; ++key) {
+          if (!kt.some(j0 + key)) continue;
+          const int64_t r = shfl64(here, key);
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float v = v_element<F, D>(a.pool, r, 32 * db + 8 * (i / 4) + 4 * h + i % 4);
+#pragma unroll
+              for (int nq = 0; nq < NQ; ++nq)
+                if (!(fabsf(v) < INFINITY) && sees(j0 + key, pos[nq], n, a.window, a.sinks)) o[nq][db][i] += v;
+            }
+        }
+      }
+    }
+    if (more) stage(t + 1, buf ^ 1);
+  }
+  if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, kDevBadPage);
+
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq) {
+    const int rr = (wave * NQ + nq) * 32 + l32, r = r0 + rr;
+    const float sum = lanes_sum<2>(l[nq]);
+    if (r >= R) continue;
+    if (st.splits > 1) {
+      float* at = a.part + ((int64_t)pl.slot * BM + rr) * D;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<F32x4*>(at + 32 * db + 8 * i + 4 * h) =
+              F32x4{o[nq][db][4 * i], o[nq][db][4 * i + 1], o[nq][db][4 * i + 2], o[nq][db][4 * i + 3]};
+      if (h == 0) {
+        float* ml = a.part_ml + ((int64_t)pl.slot * BM + rr) * 2;
+        ml[0] = m[nq], ml[1] = sum;
+      }
+    } else {
+      const int tok = (int)fast_div((uint32_t)r, a.G_div), head = pl.h * a.G + r - tok * a.G;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      char* at = a.out + 2 * ((int64_t)b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<U32x2*>(at + 2 * (32 * db + 8 * i + 4 * h)) =
+              U32x2{pack_bf16(o[nq][db][4 * i] * inv, o[nq][db][4 * i + 1] * inv),
+                    pack_bf16(o[nq][db][4 * i + 2] * inv, o[nq][db][4 * i + 3] * inv)};
+      if (h == 0 && a.lse)
+        a.lse[((int64_t)b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (m[nq] + log2_hw(sum)) * kLn2;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- fp32 pools
+// One wave has 32 rows and a part of the keys, 32 at a time, with the fp32 matrix
+// instruction (an eighteenth of the bf16 one's rate, so rows are read straight
+// from the caches into its operands, without LDS).
+template <int D>
+__global__ __launch_bounds__(64) void k_attend_f32(AttendArgs a) {
+  constexpr int BN = 32;
+  const Place pl = place_of(a);
+  if (pl.slot < 0) return;
+  const AttendStream st = a.s[pl.b];
+  const int lane = threadIdx.x, h = lane / 32, l32 = lane % 32;
+  const int32_t n = st.n, R = st.rows * a.G, r0 = pl.tile * 32;
+  const int b = a.b0 + pl.b;
+  const int64_t head_row = a.layer_row + (int64_t)pl.h * a.pool.T.d;
+  const int32_t p_lo = st.first + (int32_t)fast_div((uint32_t)r0, a.G_div);
+  const int32_t p_hi = st.first + (int32_t)fast_div((uint32_t)(min(r0 + 32, R) - 1), a.G_div);
+  const KeyTiles kt(n, p_lo, p_hi, a.window, a.sinks, BN);
+  const int32_t t_end = (int32_t)((int64_t)kt.count * (pl.split + 1) / st.splits);
+  const int32_t r = min(r0 + l32, R - 1), tok = (int32_t)fast_div((uint32_t)r, a.G_div), pos = st.first + tok;
+  const int32_t head = pl.h * a.G + r - tok * a.G;
+  // half h of the wave holds the elements h * D / 2 + k
+  float q[D / 2];
+  const char* qa = a.q + 4 * ((int64_t)b * a.q_b + (int64_t)head * a.q_h + (int64_t)tok * a.q_m + h * (D / 2));
+#pragma unroll
+  for (int k = 0; k < D / 2; k += 4) {
+    const F32x4 v = *reinterpret_cast<const F32x4*>(qa + 4 * k);
+    q[k] = v.x, q[k + 1] = v.y, q[k + 2] = v.z, q[k + 3] = v.w;
+  }
+  F32x16 o[D / 32];
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int k = 0; k < 16; ++k) o[i][k] = 0.f;
+  bool bad = false;
+  for (int32_t t = (int32_t)((int64_t)kt.count * pl.split / st.splits); t < t_end; ++t) {
+    const int32_t j0 = kt.tile(t) * BN;
+    bool x;
+    const int64_t row = pool_row(a.pool, b, (uint32_t)min(j0 + l32, n - 1), &x) + head_row;
+    bad |= x;
+    const bool full = all_see(j0, j0 + BN, p_lo, p_hi, n, a.window, a.sinks);
+    const F32x4* ka = reinterpret_cast<const F32x4*>(a.pool.K + 4 * (row * D + h * (D / 2)));
+    F32x16 s;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s[k] = 0.f;
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k) {
+      const F32x4 v = ka[k];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(v[i], q[4 * k + i], s, 0, 0, 0);
+    }
+    if (!full)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!sees(j0 + 8 * (i / 4) + 4 * h + i % 4, pos, n, a.window, a.sinks)) s[i] = -INFINITY;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
+    top = fmaxf(m, lanes_max<2>(top) * a.c);
+    const float shift = shift_of(top), old = exp2_hw(m - shift);
+    m = top;
+    l *= old;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[i] *= old;
+    bool special = false;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int key = 8 * (i / 4) + 4 * h + i % 4;
+      const float e = exp2_hw(__builtin_fmaf(s[i], a.c, -shift));
+      l += e;
+      const float* va = reinterpret_cast<const float*>(a.pool.V) + shfl64(row, key) * D + l32;
+      const bool some = full || kt.some(j0 + key);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        float v = va[32 * db];
+        if (!full) {
+          if (!some) v = 0.f;
+          else if (!(fabsf(v) < INFINITY)) v = 0.f, special = true;
+        }
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, e, o[db], 0, 0, 0);
+      }
+    }
+    if (!full && __ballot(special) != 0) {
+#pragma unroll 1
+      for (int key = 0; key < BN; ++key) {
+        if (!kt.some(j0 + key)) continue;
+        const int64_t rv = shfl64(row, key);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float v = reinterpret_cast<const float*>(a.pool.V)[rv * D + 32 * db + 8 * (i / 4) + 4 * h + i % 4];
+            if (!(fabsf(v) < INFINITY) && sees(j0 + key, pos, n, a.window, a.sinks)) o[db][i] += v;
+          }
+      }
+    }
+  }
+  if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, kDevBadPage);
+  const float sum = lanes_sum<2>(l);
+  if (r0 + l32 >= R) return;
+  const bool parts = st.splits > 1;
+  const float f = parts ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+  float* at = parts ? a.part + ((int64_t)pl.slot * 32 + l32) * D
+                    : reinterpret_cast<float*>(a.out) + (int64_t)b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<F32x4*>(at + 32 * db + 8 * i + 4 * h) =
+          F32x4{o[db][4 * i] * f, o[db][4 * i + 1] * f, o[db][4 * i + 2] * f, o[db][4 * i + 3] * f};
+  if (h != 0) return;
+  if (parts) {
+    a.part_ml[((int64_t)pl.slot * 32 + l32) * 2] = m, a.part_ml[((int64_t)pl.slot * 32 + l32) * 2 + 1] = sum;
+  } else if (a.lse) {
+    a.lse[((int64_t)b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (m + log2_hw(sum)) * kLn2;
+  }
+}
+
+// ---------------------------------------------------------------- joining splits
+// One wave a row: lane s has split s's maximum and sum, then every lane a part
+// of the row's elements over the splits in order.
+template <int D, bool F32OUT>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int32_t BM) {
+  const AttendStream st = a.s[blockIdx.y];
+  if (st.splits <= 1) return;
+  const int lane = threadIdx.x % kWave;
+  const uint32_t R = (uint32_t)(st.rows * a.G), x = blockIdx.x * 4 + threadIdx.x / kWave;
+  if (x >= R * (uint32_t)a.H) return;
+  const int32_t h = (int32_t)(x / R), r = (int32_t)(x % R), tile = r / BM, rr = r % BM;
+  // places run over the splits, the tiles from the last, the heads
+  const int64_t slot = st.start + ((int64_t)h * st.tiles + (st.tiles - 1 - tile)) * st.splits;
+  const float* ml = a.part_ml + (slot * BM + rr) * 2;
+  float m = -INFINITY, l = 0.f;
+  if (lane < st.splits) m = ml[(int64_t)lane * BM * 2], l = ml[(int64_t)lane * BM * 2 + 1];
+  float top = m;
+#pragma unroll
+  for (int k = 1; k < kWave; k *= 2) top = fmaxf(top, __shfl_xor(top, k, kWave));
+  const float w = exp2_hw(m - shift_of(top));
+  float sum = l * w;
+#pragma unroll
+  for (int k = 1; k < kWave; k *= 2) sum += __shfl_xor(sum, k, kWave);
+  constexpr int E = D >= 64 ? D / 64 : 1;
+  float v[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = 0.f;
+  const float* p = a.part + (slot * BM + rr) * D + (lane * E) % D;
+  for (int s = 0; s < st.splits; ++s) {
+    const float f = __shfl(w, s, kWave);
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] += f * p[(int64_t)s * BM * D + e];
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int32_t tok = (int32_t)fast_div((uint32_t)r, a.G_div), head = h * a.G + r - tok * a.G;
+  const int64_t b = a.b0 + blockIdx.y, at = b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m + lane * E;
+  if (lane * E < D) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (F32OUT) reinterpret_cast<float*>(a.out)[at + e] = v[e] * inv;
+      else reinterpret_cast<__bf16*>(a.out)[at + e] = (__bf16)(v[e] * inv);
+    }
+  }
+  if (lane == 0 && a.lse)
+    a.lse[(b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (top + log2_hw(sum)) * kLn2;
+}
+
+// ---------------------------------------------------------------- launches
+// What a format's translation unit offers: the kernel for `shape` rows.
+enum AttendKind { kFew1, kFew2, kTile, kF32 };
+template <int F>
+hipError_t launch_attend(int D, AttendKind kind, uint32_t grid, const AttendArgs& a, hipStream_t st);
+hipError_t launch_join(int D, bool f32, uint32_t rows, int32_t BM, const AttendArgs& a, hipStream_t st);
+constexpr int kTileW = 4, kTileNQ = 1;
+inline int attend_rows(AttendKind k) { return k == kFew1 ? 16 : k == kFew2 ? 32 : k == kF32 ? 32 : 32 * kTileW * kTileNQ; }
+inline int attend_keys(AttendKind k) { return k == kTile ? kTileKeys : 32; }
+
+}  // namespace ipv

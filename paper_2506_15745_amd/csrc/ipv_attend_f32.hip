@@ -1,0 +1,4 @@
+// Attention over f32 pages.
+#include "ipv_attend_launch.hpp"
+
+template hipError_t ipv::launch_attend<ipv::kFmtF32>(int, ipv::AttendKind, uint32_t, const ipv::AttendArgs&, hipStream_t);

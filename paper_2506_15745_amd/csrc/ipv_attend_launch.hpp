@@ -1,0 +1,30 @@
+// The attention kernels of one page format (included by one source file a format).
+#pragma once
+
+#include "ipv_attend.hpp"
+
+namespace ipv {
+
+template <int F, int D>
+hipError_t launch_attend_d(AttendKind kind, uint32_t grid, const AttendArgs& a, hipStream_t st) {
+  if constexpr (F == kFmtF32) {
+    k_attend_f32<D><<<dim3(grid), dim3(64), 0, st>>>(a);
+  } else {
+    if (kind == kFew1) k_attend_few<F, D, 1><<<dim3(grid), dim3(64 * kFewWaves), 0, st>>>(a);
+    else if (kind == kFew2) k_attend_few<F, D, 2><<<dim3(grid), dim3(64 * kFewWaves), 0, st>>>(a);
+    else k_attend_tile<F, D, kTileW, kTileNQ><<<dim3(grid), dim3(64 * kTileW), 0, st>>>(a);
+  }
+  return hipGetLastError();
+}
+
+template <int F>
+hipError_t launch_attend(int D, AttendKind kind, uint32_t grid, const AttendArgs& a, hipStream_t st) {
+  switch (D) {
+    case 32: return launch_attend_d<F, 32>(kind, grid, a, st);
+    case 64: return launch_attend_d<F, 64>(kind, grid, a, st);
+    case 128: return launch_attend_d<F, 128>(kind, grid, a, st);
+    default: return launch_attend_d<F, 256>(kind, grid, a, st);
+  }
+}
+
+}  // namespace ipv

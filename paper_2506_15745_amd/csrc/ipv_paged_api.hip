@@ -1,0 +1,336 @@
+// C entry points of the paged cache: argument checks, the split of the work and
+// the launches. As in the pass, every check that the host can make comes before
+// the first launch, and nothing here allocates, throws or waits.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/ipv.h"
+#include "ipv_attend.hpp"
+
+using namespace ipv;
+
+#define IPV_TRY(x)               \
+  do {                           \
+    const ipv_status _s = (x);   \
+    if (_s != IPV_OK) return _s; \
+  } while (0)
+
+namespace {
+
+static_assert(kFmtBf16 == IPV_PAGES_BF16 && kFmtF32 == IPV_PAGES_F32 && kFmtFp8 == IPV_PAGES_FP8 && kFmtFp4 == IPV_PAGES_FP4,
+              "the formats of the header");
+static_assert((int)kFmtBf16 == IPV_BF16 && (int)kFmtF32 == IPV_F32, "rows in the cache's types");
+static_assert(kDevNan == IPV_DEV_NAN && kDevBadPage == IPV_DEV_BAD_PAGE, "the error bits of the header");
+
+constexpr int32_t kMaxPosition = 1 << 30;  // positions and their tiles' ends stay in 31 bits
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+ipv_status launched(hipError_t e) { return e == hipSuccess ? IPV_OK : IPV_ERR_HIP; }
+
+ipv_status check_pool_shape(const ipv_page_shape* s) {
+  if (!s) return IPV_ERR_NULL;
+  if (s->format < IPV_PAGES_BF16 || s->format > IPV_PAGES_FP4) return IPV_ERR_DTYPE;
+  if (s->pages < 1 || s->layers < 1 || s->kv_heads < 1 || s->page_rows < 1 || s->page_rows > kMaxPosition) return IPV_ERR_SHAPE;
+  if (s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128 && s->head_dim != 256) return IPV_ERR_SHAPE;
+  // rows of the pool, and their bytes, in 63 bits
+  const double rows = (double)s->pages * s->layers * s->kv_heads * s->page_rows;
+  if (rows > 0x1p50) return IPV_ERR_SHAPE;
+  return IPV_OK;
+}
+
+ipv_status check_pool(const ipv_page_shape* s, const void* K, const void* V, const uint8_t* Ks, const uint8_t* Vs,
+                      const int32_t* table, int32_t cols, int32_t streams, Pool* p) {
+  IPV_TRY(check_pool_shape(s));
+  const bool scaled = fmt_scaled(s->format);
+  if (!K || !V || (scaled && (!Ks || !Vs))) return IPV_ERR_NULL;
+  if (!aligned(K, 16) || !aligned(V, 16)) return IPV_ERR_ALIGN;
+  if (scaled && (!aligned(Ks, 4) || !aligned(Vs, 4))) return IPV_ERR_ALIGN;
+  if (table && !aligned(table, 4)) return IPV_ERR_ALIGN;
+  if (streams < 1 || cols < 1) return IPV_ERR_SHAPE;
+  if (!table && (cols != 1 || streams > s->pages)) return IPV_ERR_SHAPE;
+  p->K = static_cast<char*>(const_cast<void*>(K));
+  p->V = static_cast<char*>(const_cast<void*>(V));
+  p->Ks = const_cast<uint8_t*>(Ks);
+  p->Vs = const_cast<uint8_t*>(Vs);
+  p->table = table;
+  p->cols = cols;
+  p->pages = s->pages;
+  p->layer_rows = (int64_t)s->kv_heads * s->page_rows;
+  p->page_rows_all = (int64_t)s->layers * p->layer_rows;
+  p->T = make_fastdiv((uint32_t)s->page_rows);
+  return IPV_OK;
+}
+
+// Rows that a stream's table covers (at most: positions stay in 31 bits).
+int64_t table_rows(const ipv_page_shape* s, int32_t cols) {
+  return std::min<int64_t>((int64_t)cols * s->page_rows, kMaxPosition);
+}
+
+ipv_status check_strides(const int64_t* strides, int n) {
+  if (!strides) return IPV_ERR_NULL;
+  for (int i = 0; i < n; ++i)
+    if (strides[i] % 8 != 0) return IPV_ERR_ALIGN;
+  return IPV_OK;
+}
+
+ipv_status check_word(const void* ws, size_t ws_bytes, size_t need) {
+  if (!ws) return IPV_ERR_WORKSPACE;
+  if (!aligned(ws, 256)) return IPV_ERR_ALIGN;
+  return ws_bytes < need ? IPV_ERR_WORKSPACE : IPV_OK;
+}
+
+template <bool WRITE, int F, int X, int D>
+hipError_t page_launch(const PageCall& c, dim3 grid, hipStream_t st) {
+  if constexpr (WRITE) k_page_write<F, X, D><<<grid, dim3(kPageThreads), 0, st>>>(c);
+  else k_page_read<F, X, D><<<grid, dim3(kPageThreads), 0, st>>>(c);
+  return hipGetLastError();
+}
+
+template <bool WRITE, int F, int X>
+hipError_t page_launch_d(int D, const PageCall& c, int32_t rows, hipStream_t st, int32_t streams) {
+  const int per = kPageThreads / (D / 16);
+  const int64_t items = (int64_t)rows * ((c.LH + kPageSlices - 1) / kPageSlices);
+  const dim3 grid((uint32_t)((items + per - 1) / per), 2, (uint32_t)streams);
+  switch (D) {
+    case 32: return page_launch<WRITE, F, X, 32>(c, grid, st);
+    case 64: return page_launch<WRITE, F, X, 64>(c, grid, st);
+    case 128: return page_launch<WRITE, F, X, 128>(c, grid, st);
+    default: return page_launch<WRITE, F, X, 256>(c, grid, st);
+  }
+}
+
+template <bool WRITE, int F>
+hipError_t page_launch_f(int dtype, int D, const PageCall& c, int32_t rows, hipStream_t st, int32_t streams) {
+  return dtype == IPV_BF16 ? page_launch_d<WRITE, F, kFmtBf16>(D, c, rows, st, streams)
+                           : page_launch_d<WRITE, F, kFmtF32>(D, c, rows, st, streams);
+}
+
+// ipv_page_write and ipv_page_read: the same checks, the same split.
+template <bool WRITE>
+ipv_status page_rows(const ipv_page_shape* s, const void* K_pages, const void* V_pages, const uint8_t* Ks, const uint8_t* Vs,
+                     const int32_t* table, int32_t cols, int32_t streams, const int32_t* first, const int32_t* rows,
+                     int32_t first_layer, int32_t layers, const void* K, const void* V, int32_t dtype,
+                     const int64_t* strides, const float* rotary, int32_t rotary_rows, void* ws, size_t ws_bytes,
+                     void* stream) {
+  PageCall c;
+  IPV_TRY(check_pool(s, K_pages, V_pages, Ks, Vs, table, cols, streams, &c.pool));
+  if (!first || !rows || !K || !V) return IPV_ERR_NULL;
+  if (dtype != IPV_BF16 && dtype != IPV_F32) return IPV_ERR_DTYPE;
+  if (!aligned(K, 16) || !aligned(V, 16) || (rotary && !aligned(rotary, 16))) return IPV_ERR_ALIGN;
+  IPV_TRY(check_strides(strides, 4));
+  if (first_layer < 0 || layers < 1 || layers > s->layers - first_layer) return IPV_ERR_SHAPE;
+  const int64_t slices = (int64_t)layers * s->kv_heads, groups = (slices + kPageSlices - 1) / kPageSlices;
+  if (slices > kMaxPosition) return IPV_ERR_SHAPE;
+  for (int32_t b = 0; b < streams; ++b) {
+    if (rows[b] < 0 || first[b] < 0) return IPV_ERR_SHAPE;
+    const int64_t end = (int64_t)first[b] + rows[b];
+    if (rows[b] > 0 && end > table_rows(s, cols)) return IPV_ERR_SHAPE;
+    if (rows[b] > 0 && rotary && end > rotary_rows) return IPV_ERR_ARG;
+    if (rows[b] * groups > kMaxPosition) return IPV_ERR_SHAPE;
+  }
+  IPV_TRY(check_word(ws, ws_bytes, kWsHeader));
+  c.K = static_cast<char*>(const_cast<void*>(K));
+  c.V = static_cast<char*>(const_cast<void*>(V));
+  c.sb = strides[0], c.sl = strides[1], c.sh = strides[2], c.sr = strides[3];
+  c.rotary = rotary;
+  c.err = static_cast<uint32_t*>(ws);
+  c.H = s->kv_heads;
+  c.LH = (int32_t)slices;
+  c.first_slice = (int64_t)first_layer * c.pool.layer_rows;
+  c.H_div = make_fastdiv((uint32_t)s->kv_heads);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  for (int32_t b0 = 0; b0 < streams; b0 += kPageStreams) {
+    const int32_t nb = std::min(kPageStreams, streams - b0);
+    int32_t most = 0;
+    for (int32_t i = 0; i < nb; ++i) {
+      c.first[i] = first[b0 + i], c.rows[i] = rows[b0 + i];
+      most = std::max(most, rows[b0 + i]);
+    }
+    if (most == 0) continue;
+    c.b0 = b0;
+    hipError_t e;
+    switch (s->format) {
+      case IPV_PAGES_BF16: e = page_launch_f<WRITE, kFmtBf16>(dtype, s->head_dim, c, most, st, nb); break;
+      case IPV_PAGES_F32: e = page_launch_f<WRITE, kFmtF32>(dtype, s->head_dim, c, most, st, nb); break;
+      case IPV_PAGES_FP8: e = page_launch_f<WRITE, kFmtFp8>(dtype, s->head_dim, c, most, st, nb); break;
+      default: e = page_launch_f<WRITE, kFmtFp4>(dtype, s->head_dim, c, most, st, nb); break;
+    }
+    IPV_TRY(launched(e));
+  }
+  return IPV_OK;
+}
+
+// ------------------------------------------------------------ attention
+// Workgroups that fill the card: below this number, key ranges are split.
+constexpr int32_t kFill = 512;
+
+// The kernel for a call whose widest stream has `rows` rows a KV head.
+AttendKind attend_kind(int format, int64_t rows) {
+  if (format == IPV_PAGES_F32) return kF32;
+  return rows <= 16 ? kFew1 : rows <= 32 ? kFew2 : kTile;
+}
+
+size_t part_bytes(AttendKind k, int D) { return (size_t)(2 * kFill) * attend_rows(k) * (size_t)(D + 2) * sizeof(float); }
+
+ipv_status check_heads(const ipv_page_shape* s, int32_t streams, int32_t q_heads, int32_t max_rows) {
+  if (streams < 1 || q_heads < 1 || max_rows < 1 || q_heads % s->kv_heads != 0) return IPV_ERR_SHAPE;
+  if ((int64_t)q_heads * max_rows > kMaxPosition) return IPV_ERR_SHAPE;
+  return IPV_OK;
+}
+
+// The split of one launch's streams: row tiles, parts of the key ranges, and
+// the first workgroup of each. A key range is split when the row tiles alone
+// leave the card unfilled, into parts of about equal length that give kFill
+// workgroups (few: at least a tile for each wave).
+void plan(AttendArgs* a, AttendKind kind) {
+  const int32_t BM = attend_rows(kind), BN = attend_keys(kind);
+  const bool few = kind == kFew1 || kind == kFew2;
+  int64_t base = 0, work = 0;
+  int32_t count[kAttendStreams];
+  for (int32_t i = 0; i < a->streams; ++i) {
+    AttendStream& s = a->s[i];
+    s.tiles = (int32_t)(((int64_t)s.rows * a->G + BM - 1) / BM);
+    s.splits = 1;
+    // the longest of its row tiles' key ranges: the last one's, with the span of one tile
+    const int32_t span = (BM + a->G - 1) / a->G + 1, p_hi = s.first + s.rows - 1;
+    count[i] = s.rows > 0 ? KeyTiles(s.n, std::max(s.first, p_hi - span + 1), p_hi, a->window, a->sinks, BN).count : 0;
+    base += (int64_t)a->H * s.tiles;
+    work += (int64_t)a->H * s.tiles * count[i];
+  }
+  if (base < kFill) {
+    int64_t per = std::max<int64_t>((work + kFill - 1) / kFill, few ? kFewWaves : 2);
+    if (few) per = (per + kFewWaves - 1) / kFewWaves * kFewWaves;
+    for (int32_t i = 0; i < a->streams; ++i)
+      a->s[i].splits = (int32_t)std::min<int64_t>(std::max<int64_t>((count[i] + per - 1) / per, 1), kMaxSplits);
+  }
+  int64_t at = 0;
+  for (int32_t i = 0; i < a->streams; ++i) {
+    a->s[i].start = (int32_t)at;
+    at += (int64_t)a->H * a->s[i].tiles * a->s[i].splits;
+  }
+  a->blocks = (int32_t)at;
+}
+
+template <int D>
+void join_launch(bool f32, dim3 grid, int32_t BM, const AttendArgs& a, hipStream_t st) {
+  if (f32) k_attend_join<D, true><<<grid, dim3(256), 0, st>>>(a, BM);
+  else k_attend_join<D, false><<<grid, dim3(256), 0, st>>>(a, BM);
+}
+
+}  // namespace
+
+hipError_t ipv::launch_join(int D, bool f32, uint32_t rows, int32_t BM, const AttendArgs& a, hipStream_t st) {
+  const dim3 grid((rows + 3) / 4, (uint32_t)a.streams);
+  switch (D) {
+    case 32: join_launch<32>(f32, grid, BM, a, st); break;
+    case 64: join_launch<64>(f32, grid, BM, a, st); break;
+    case 128: join_launch<128>(f32, grid, BM, a, st); break;
+    default: join_launch<256>(f32, grid, BM, a, st); break;
+  }
+  return hipGetLastError();
+}
+
+extern "C" {
+
+ipv_status ipv_page_write(const ipv_page_shape* pool, void* K_pages, void* V_pages, uint8_t* K_scales,
+                          uint8_t* V_scales, const int32_t* page_table, int32_t table_cols, int32_t streams,
+                          const int32_t* first_row, const int32_t* rows, int32_t first_layer, int32_t layers,
+                          const void* K, const void* V, int32_t dtype, const int64_t* strides, const float* rotary,
+                          int32_t rotary_rows, void* ws, size_t ws_bytes, void* stream) {
+  return page_rows<true>(pool, K_pages, V_pages, K_scales, V_scales, page_table, table_cols, streams, first_row, rows,
+                         first_layer, layers, K, V, dtype, strides, rotary, rotary_rows, ws, ws_bytes, stream);
+}
+
+ipv_status ipv_page_read(const ipv_page_shape* pool, const void* K_pages, const void* V_pages, const uint8_t* K_scales,
+                         const uint8_t* V_scales, const int32_t* page_table, int32_t table_cols, int32_t streams,
+                         const int32_t* first_row, const int32_t* rows, int32_t first_layer, int32_t layers, void* K,
+                         void* V, int32_t dtype, const int64_t* strides, const float* rotary, int32_t rotary_rows,
+                         void* ws, size_t ws_bytes, void* stream) {
+  return page_rows<false>(pool, K_pages, V_pages, K_scales, V_scales, page_table, table_cols, streams, first_row, rows,
+                          first_layer, layers, K, V, dtype, strides, rotary, rotary_rows, ws, ws_bytes, stream);
+}
+
+ipv_status ipv_attend_workspace_bytes(const ipv_page_shape* pool, int32_t streams, int32_t q_heads, int32_t max_rows,
+                                      size_t* bytes) {
+  if (!bytes) return IPV_ERR_NULL;
+  IPV_TRY(check_pool_shape(pool));
+  IPV_TRY(check_heads(pool, streams, q_heads, max_rows));
+  // a call of fewer rows may take a kernel of narrower tiles: the widest covers them all
+  *bytes = kWsHeader + part_bytes(attend_kind(pool->format, (int64_t)max_rows * (q_heads / pool->kv_heads)), pool->head_dim);
+  return IPV_OK;
+}
+
+ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const void* V_pages, const uint8_t* K_scales,
+                      const uint8_t* V_scales, const int32_t* page_table, int32_t table_cols, int32_t streams,
+                      const int32_t* n_tokens, const int32_t* q_first, const int32_t* q_rows, int32_t layer,
+                      const void* q, const int64_t* q_strides, int32_t q_heads, int32_t max_rows, double scale,
+                      int32_t window, int32_t sinks, void* out, const int64_t* out_strides, float* lse, void* ws,
+                      size_t ws_bytes, void* stream) {
+  AttendArgs a;
+  IPV_TRY(check_pool(pool, K_pages, V_pages, K_scales, V_scales, page_table, table_cols, streams, &a.pool));
+  if (!n_tokens || !q_first || !q_rows || !q || !out) return IPV_ERR_NULL;
+  IPV_TRY(check_heads(pool, streams, q_heads, max_rows));
+  if (!aligned(q, 16) || !aligned(out, 16) || (lse && !aligned(lse, 4))) return IPV_ERR_ALIGN;
+  IPV_TRY(check_strides(q_strides, 3));
+  IPV_TRY(check_strides(out_strides, 3));
+  if (layer < 0 || layer >= pool->layers) return IPV_ERR_SHAPE;
+  if (!(scale > 0) || !std::isfinite(scale) || !std::isnormal((float)(scale * 1.4426950408889634)) || window < 0 ||
+      sinks < 0)
+    return IPV_ERR_ARG;
+  for (int32_t b = 0; b < streams; ++b) {
+    if (n_tokens[b] < 0 || n_tokens[b] > table_rows(pool, table_cols)) return IPV_ERR_SHAPE;
+    if (q_rows[b] < 0 || q_rows[b] > max_rows || q_first[b] < 0 || q_first[b] > kMaxPosition - q_rows[b]) return IPV_ERR_SHAPE;
+  }
+  size_t need = 0;
+  IPV_TRY(ipv_attend_workspace_bytes(pool, streams, q_heads, max_rows, &need));
+  IPV_TRY(check_word(ws, ws_bytes, need));
+
+  a.layer_row = (int64_t)layer * a.pool.layer_rows;
+  a.q = static_cast<const char*>(q);
+  a.out = static_cast<char*>(out);
+  a.lse = lse;
+  a.q_b = q_strides[0], a.q_h = q_strides[1], a.q_m = q_strides[2];
+  a.o_b = out_strides[0], a.o_h = out_strides[1], a.o_m = out_strides[2];
+  a.H = pool->kv_heads;
+  a.G = q_heads / pool->kv_heads;
+  a.max_rows = max_rows;
+  a.G_div = make_fastdiv((uint32_t)a.G);
+  a.c = (float)(scale * 1.4426950408889634);
+  a.window = window;
+  a.sinks = sinks;
+  a.err = static_cast<uint32_t*>(ws);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  for (int32_t b0 = 0; b0 < streams; b0 += kAttendStreams) {
+    a.b0 = b0;
+    a.streams = std::min(kAttendStreams, streams - b0);
+    int32_t most = 0;
+    for (int32_t i = 0; i < a.streams; ++i) {
+      a.s[i].n = n_tokens[b0 + i], a.s[i].first = q_first[b0 + i], a.s[i].rows = q_rows[b0 + i];
+      most = std::max(most, q_rows[b0 + i]);
+    }
+    if (most == 0) continue;
+    const AttendKind kind = attend_kind(pool->format, (int64_t)most * a.G);
+    plan(&a, kind);
+    a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + kWsHeader);
+    a.part = a.part_ml + (size_t)(2 * kFill) * attend_rows(kind) * 2;
+    const uint32_t grid = (uint32_t)(a.blocks + 7) / 8u * 8u;
+    hipError_t e;
+    switch (pool->format) {
+      case IPV_PAGES_BF16: e = launch_attend<kFmtBf16>(pool->head_dim, kind, grid, a, st); break;
+      case IPV_PAGES_F32: e = launch_attend<kFmtF32>(pool->head_dim, kind, grid, a, st); break;
+      case IPV_PAGES_FP8: e = launch_attend<kFmtFp8>(pool->head_dim, kind, grid, a, st); break;
+      default: e = launch_attend<kFmtFp4>(pool->head_dim, kind, grid, a, st); break;
+    }
+    IPV_TRY(launched(e));
+    bool split = false;
+    for (int32_t i = 0; i < a.streams; ++i) split |= a.s[i].splits > 1;
+    if (split)
+      IPV_TRY(launched(launch_join(pool->head_dim, pool->format == IPV_PAGES_F32, (uint32_t)most * (uint32_t)q_heads,
+                                   attend_rows(kind), a, st)));
+  }
+  return IPV_OK;
+}
+
+}  // extern "C"

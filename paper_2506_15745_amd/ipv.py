@@ -13,6 +13,9 @@ Tensor layouts (all contiguous, on the same GPU):
   tar, van    [B, L, H, S]     torch.float32
   keep_idx    [B, L, H, C]     torch.int32
   pool_size   [B, L]           torch.int32
+The paged cache (:class:`PagePool`, ``ipv_page_write``, ``ipv_page_read``,
+``ipv_attend``) takes rows and queries of any strides whose last dimension is
+contiguous; its layouts stand at those functions.
 """
 from __future__ import annotations
 
@@ -27,12 +30,18 @@ LIB_PATH = os.path.join(HERE, "libipv.so")
 
 OK, ERR_NULL, ERR_ALIGN, ERR_SHAPE, ERR_DTYPE, ERR_BUDGET, ERR_ARG, ERR_WORKSPACE, ERR_HIP = range(9)
 BF16, F32 = 0, 1
-DEV_BAD_PATCH, DEV_BAD_FRAMES, DEV_RECENT_OVER, DEV_BAD_KEEP, DEV_NAN, DEV_WAIT_TIMEOUT = 1, 2, 4, 8, 16, 32
+DEV_BAD_PATCH, DEV_BAD_FRAMES, DEV_RECENT_OVER, DEV_BAD_KEEP, DEV_NAN, DEV_WAIT_TIMEOUT, DEV_BAD_PAGE = 1, 2, 4, 8, 16, 32, 64
 # `mode` bits: reversed TaR / VaN stages, consecutive-frame TaR, head-shared
 # selection, Uniform Select (frames at regular intervals, no scores)
 TAR_REVERSE, VAN_REVERSE, TAR_ADJACENT, HEAD_SHARED, UNIFORM_SELECT = 1, 2, 4, 8, 16
 
-EXPORTS = ("ipv_workspace_bytes", "ipv_tar_scores", "ipv_van_scores", "ipv_select", "ipv_compact",
+# page formats (a pool's K and V: bf16, fp32, e4m3 or e2m1 elements with a scale for each 32)
+PAGES_BF16, PAGES_F32, PAGES_FP8, PAGES_FP4 = range(4)
+SCALE_BLOCK = 32
+
+PAGED_EXPORTS = ("ipv_page_write", "ipv_page_read", "ipv_attend_workspace_bytes", "ipv_attend")
+EXPORTS = PAGED_EXPORTS + (
+           "ipv_workspace_bytes", "ipv_tar_scores", "ipv_van_scores", "ipv_select", "ipv_compact",
            "ipv_compress", "ipv_compress_timed", "ipv_compress_noalloc", "ipv_append", "ipv_ckv_step", "ipv_ckv_stream",
            "ipv_clear_device_errors",
            "ipv_read_device_errors", "ipv_status_str")
@@ -47,6 +56,10 @@ class IpvError(RuntimeError):
 class Shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("streams", "layers", "kv_heads", "head_dim", "capacity", "grid_h", "grid_w", "dtype")]
+
+
+class PageShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("pages", "layers", "kv_heads", "page_rows", "head_dim", "format")]
 
 
 class Events(ctypes.Structure):
@@ -91,10 +104,32 @@ def lib() -> ctypes.CDLL:
         L.ipv_read_device_errors.argtypes = [vp, sz, vp, ctypes.POINTER(ctypes.c_uint32)]
         L.ipv_status_str.argtypes = [ctypes.c_int]
         L.ipv_status_str.restype = ctypes.c_char_p
-        for name in EXPORTS[:-1]:
+        for name in EXPORTS[len(PAGED_EXPORTS):-1]:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
+
+
+_paged_lib = None
+
+
+def _paged() -> ctypes.CDLL:
+    """The library with the paged cache's calls described."""
+    global _paged_lib
+    L = lib()
+    if _paged_lib is not L:
+        vp, i32, f64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_double, ctypes.c_size_t
+        ps = ctypes.POINTER(PageShape)
+        rows = [ps, vp, vp, vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, sz, vp]
+        L.ipv_page_write.argtypes = rows
+        L.ipv_page_read.argtypes = rows
+        L.ipv_attend_workspace_bytes.argtypes = [ps, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+        L.ipv_attend.argtypes = [ps, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, i32, vp, vp, i32, i32, f64, i32, i32, vp,
+                                 vp, vp, vp, sz, vp]
+        for name in PAGED_EXPORTS:
+            getattr(L, name).restype = ctypes.c_int
+        _paged_lib = L
+    return L
 
 
 def status_str(status: int) -> str:
@@ -461,6 +496,176 @@ def ipv_read_device_errors(ws, stream=None) -> int:
     _check(lib().ipv_read_device_errors(_ptr(ws), _ws_bytes(ws), _stream(stream), ctypes.byref(out)),
            "ipv_read_device_errors")
     return out.value
+
+
+# ---------------------------------------------------------------- paged cache
+class PagePool:
+    """Pages of cache rows: K, V [P, L, H, T, X] in GPU memory, contiguous, X = D
+    elements of bf16 or fp32, or with K_scales, V_scales (uint8 [P, L, H, T,
+    D / 32]) D bytes of e4m3 or D / 2 bytes of e2m1 elements (torch.uint8). A
+    cache K, V [B, L, H, S, D] of this module is a pool of B pages of S rows (its
+    calls then take page_table None)."""
+
+    def __init__(self, K, V, K_scales=None, V_scales=None):
+        if K.dim() != 5:
+            raise IpvError(ERR_SHAPE, "K must be [P, L, H, T, X]")
+        P, L, H, T, X = K.shape
+        _expect("V", V, K.shape, K.dtype, K.device)
+        if K.dtype == torch.uint8:
+            if K_scales is None or V_scales is None:
+                raise IpvError(ERR_NULL, "8- and 4-bit pages need K_scales and V_scales")
+            if K_scales.dim() != 5:
+                raise IpvError(ERR_SHAPE, "K_scales must be [P, L, H, T, D / 32]")
+            D = K_scales.shape[4] * SCALE_BLOCK
+            if X not in (D, D // 2):
+                raise IpvError(ERR_SHAPE, "rows of %d bytes do not go with %d scales" % (X, K_scales.shape[4]))
+            fmt = PAGES_FP8 if X == D else PAGES_FP4
+            for what, t in (("K_scales", K_scales), ("V_scales", V_scales)):
+                _expect(what, t, (P, L, H, T, D // SCALE_BLOCK), torch.uint8, K.device)
+        else:
+            if K_scales is not None or V_scales is not None:
+                raise IpvError(ERR_ARG, "bf16 and fp32 pages have no scales")
+            fmt, D = _dtype_code(K), X
+        self.K, self.V, self.K_scales, self.V_scales = K, V, K_scales, V_scales
+        self.format, self.head_dim, self.device = fmt, D, K.device
+        self.dtype = torch.float32 if fmt == PAGES_F32 else torch.bfloat16  # of queries and outputs
+        self.shape = PageShape(P, L, H, T, D, fmt)
+        self._args = (ctypes.byref(self.shape), _ptr(K), _ptr(V), _ptr(K_scales), _ptr(V_scales))
+
+    @classmethod
+    def empty(cls, pages, layers, kv_heads, page_rows, head_dim, format, device="cuda"):  # noqa: A002
+        """A pool of zeroed pages."""
+        rows = (pages, layers, kv_heads, page_rows)
+        if format in (PAGES_BF16, PAGES_F32):
+            kind = torch.bfloat16 if format == PAGES_BF16 else torch.float32
+            return cls(*(torch.zeros(rows + (head_dim,), dtype=kind, device=device) for _ in range(2)))
+        if format not in (PAGES_FP8, PAGES_FP4):
+            raise IpvError(ERR_DTYPE, "page format %r" % (format,))
+        width = (head_dim, head_dim, head_dim // SCALE_BLOCK, head_dim // SCALE_BLOCK) if format == PAGES_FP8 else \
+            (head_dim // 2, head_dim // 2, head_dim // SCALE_BLOCK, head_dim // SCALE_BLOCK)
+        return cls(*(torch.zeros(rows + (w,), dtype=torch.uint8, device=device) for w in width))
+
+
+def _counts_ptr(values, streams, what):
+    """(address, keeper) of a host array with one count per stream, from an int or a sequence."""
+    if isinstance(values, int):
+        values = (values,) * streams
+    elif len(values) != streams:
+        raise IpvError(ERR_SHAPE, "%s needs one count per stream (%d)" % (what, streams))
+    return (ctypes.c_int32 * streams)(*values)
+
+
+def _table(pool, table, streams):
+    """(pointer, columns) of a page table [B, cols], or of none (stream b's rows are page b)."""
+    if table is None:
+        return None, 1
+    if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != streams:
+        raise IpvError(ERR_SHAPE, "page_table must be int32 [%d, columns]" % streams)
+    if table.get_device() != pool.K.get_device():
+        raise IpvError(ERR_ARG, "page_table is on %s, the pool on %s" % (table.device, pool.device))
+    return _ptr(table), table.shape[1]
+
+
+def _strides(what, t, dims):
+    """Strides (elements) of all but the last dimension, which must be contiguous; 0 for a dimension of one."""
+    st, sh = t.stride(), t.shape
+    if st[-1] != 1:
+        raise IpvError(ERR_SHAPE, "%s's last dimension must be contiguous" % what)
+    return (ctypes.c_int64 * dims)(*[st[i] if sh[i] > 1 else 0 for i in range(dims)])
+
+
+def _same_gpu(pool, ws, **tensors):
+    dev = pool.K.get_device()
+    for what, t in tensors.items():
+        if t is not None and t.get_device() != dev:
+            raise IpvError(ERR_ARG, "%s is on %s, the pool on %s" % (what, t.device, pool.device))
+    if ws is None:
+        raise IpvError(ERR_WORKSPACE, "a workspace is required")
+    if ws.get_device() != dev:
+        raise IpvError(ERR_ARG, "the workspace is on %s, the pool on %s" % (ws.device, pool.device))
+
+
+def alloc_page_workspace(device) -> torch.Tensor:
+    """A zeroed workspace for ipv_page_write and ipv_page_read (the device error word)."""
+    return torch.zeros(256, dtype=torch.uint8, device=device)
+
+
+def attend_workspace_bytes(pool: PagePool, streams: int, q_heads: int, max_rows: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_paged().ipv_attend_workspace_bytes(pool._args[0], streams, q_heads, max_rows, ctypes.byref(out)),
+           "ipv_attend_workspace_bytes")
+    return out.value
+
+
+def alloc_attend_workspace(pool: PagePool, streams: int, q_heads: int, max_rows: int) -> torch.Tensor:
+    """A zeroed workspace for ipv_attend calls of at most these sizes."""
+    return torch.zeros(attend_workspace_bytes(pool, streams, q_heads, max_rows), dtype=torch.uint8, device=pool.device)
+
+
+def _page_rows(name, pool, page_table, first_row, K, V, ws, rows, first_layer, rotary, stream):
+    if K.dim() != 5 or V.shape != K.shape or K.shape[2] != pool.shape.kv_heads or K.shape[4] != pool.head_dim:
+        raise IpvError(ERR_SHAPE, "K and V must be [B, layers, %d, rows, %d]" % (pool.shape.kv_heads, pool.head_dim))
+    if V.dtype != K.dtype:
+        raise IpvError(ERR_DTYPE, "K and V must have one dtype")
+    B, L, _, N, D = K.shape
+    st = _strides("K", K, 4)
+    if V.stride() != K.stride() and list(_strides("V", V, 4)) != list(st):
+        raise IpvError(ERR_SHAPE, "K and V must have the same strides")
+    if isinstance(rows, int) or rows is None:
+        rows = N if rows is None else rows
+        longest = rows
+    else:
+        longest = max(rows)
+    if longest > N:
+        raise IpvError(ERR_SHAPE, "%d rows of a tensor of %d" % (longest, N))
+    if rotary is not None and (rotary.dtype != torch.float32 or rotary.dim() != 3 or tuple(rotary.shape[1:]) != (D // 2, 2)):
+        raise IpvError(ERR_SHAPE, "rotary must be fp32 [positions, %d, 2]" % (D // 2))
+    table, cols = _table(pool, page_table, B)
+    _same_gpu(pool, ws, K=K, V=V, rotary=rotary)
+    first, rows = _counts_ptr(first_row, B, "first_row"), _counts_ptr(rows, B, "rows")
+    _check(getattr(_paged(), name)(*pool._args, table, cols, B, first, rows, first_layer, L, K.data_ptr(), V.data_ptr(),
+                                   _dtype_code(K), st, None if rotary is None else _ptr(rotary),
+                                   0 if rotary is None else rotary.shape[0], _ptr(ws), _ws_bytes(ws), _stream(stream)), name)
+
+
+def ipv_page_write(pool, page_table, first_row, K, V, ws, rows=None, first_layer=0, rotary=None, stream=None):
+    """Rows K/V ([B, layers, H, rows, D], bf16 or fp32) of layers first_layer, ...
+    into the pool at positions first_row[b], first_row[b] + 1, ... (ints, or a
+    sequence with one per stream; rows: all, or how many of each stream);
+    rotary (fp32 [positions, D / 2, 2], cosine and sine) turns the keys to
+    their positions. page_table: int32 [B, columns], or None."""
+    _page_rows("ipv_page_write", pool, page_table, first_row, K, V, ws, rows, first_layer, rotary, stream)
+
+
+def ipv_page_read(pool, page_table, first_row, K, V, ws, rows=None, first_layer=0, rotary=None, stream=None):
+    """Rows of the pool into K/V (as for ipv_page_write), keys turned back where rotary is given."""
+    _page_rows("ipv_page_read", pool, page_table, first_row, K, V, ws, rows, first_layer, rotary, stream)
+
+
+def ipv_attend(pool, page_table, n_tokens, q_first, layer, q, out, ws, q_rows=None, scale=None, window=0, sinks=0,
+               lse=None, stream=None):
+    """Attention of q ([B, q_heads, M, D], in the pool's dtype) over the first
+    n_tokens[b] rows of one layer, into out (the same shape); query i of stream b
+    stands at position q_first[b] + i and sees the rows up to there, with a
+    window only the last `window` of them and the first `sinks` rows. scale:
+    1 / sqrt(D) if None. q_rows: queries of each stream (M if None). lse: fp32
+    [B, q_heads, M] that receives the logarithm of each softmax's sum, or None."""
+    if q.dim() != 4 or q.shape[3] != pool.head_dim:
+        raise IpvError(ERR_SHAPE, "q must be [B, q_heads, rows, %d]" % pool.head_dim)
+    if q.dtype != pool.dtype or out.dtype != pool.dtype:
+        raise IpvError(ERR_DTYPE, "q and out must be %s" % pool.dtype)
+    if out.shape != q.shape:
+        raise IpvError(ERR_SHAPE, "out must have q's shape")
+    B, A, M, D = q.shape
+    if lse is not None:
+        _expect("lse", lse, (B, A, M), torch.float32, pool.device)
+    table, cols = _table(pool, page_table, B)
+    _same_gpu(pool, ws, q=q, out=out)
+    n, first = _counts_ptr(n_tokens, B, "n_tokens"), _counts_ptr(q_first, B, "q_first")
+    _check(_paged().ipv_attend(*pool._args, table, cols, B, n, first, _counts_ptr(M if q_rows is None else q_rows, B, "q_rows"),
+                               layer, q.data_ptr(), _strides("q", q, 3), A, M, D ** -0.5 if scale is None else scale, window,
+                               sinks, out.data_ptr(), _strides("out", out, 3), _ptr(lse), _ptr(ws), _ws_bytes(ws),
+                               _stream(stream)), "ipv_attend")
 
 
 class Compressor:
