@@ -17,6 +17,8 @@
 // r % G), so the cache is read once for them.
 #pragma once
 
+#include <type_traits>
+
 #include "ipv_pages.hpp"
 
 namespace ipv {
@@ -44,6 +46,7 @@ struct AttendArgs {
   float* part;     // unnormalised sums of a split's rows, [workgroup][row][D]
   float* part_ml;  // their maxima and sums of weights, [workgroup][row][2]
   uint32_t* err;
+  uint32_t* arrived;  // workgroups of a row tile that have left their part: zero before and after a call
   int32_t streams, blocks;
   AttendStream s[kAttendStreams];
 };
@@ -64,18 +67,35 @@ struct KeyTiles {
     count = sink_tiles + (main_last > main_first ? main_last - main_first : 0);
   }
   __device__ int32_t tile(int32_t t) const { return t < sink_tiles ? t : main_first + t - sink_tiles; }
-  __device__ bool some(int32_t j) const { return j < hi && (j >= lo || j < sink_end); }
+  __device__ bool some(int32_t j) const { return (j < hi) & ((j >= lo) | (j < sink_end)); }
 };
 
 // Whether a query at p sees row j of n.
 __device__ __forceinline__ bool sees(int32_t j, int32_t p, int32_t n, int32_t window, int32_t sinks) {
-  return j <= p && j < n && (window <= 0 || j > p - window || j < sinks);
+  return (j <= p) & (j < n) & ((window <= 0) | (j > p - window) | (j < sinks));
 }
 // Whether every query of [p_lo, p_hi] sees all rows of [j0, j1).
 __device__ __forceinline__ bool all_see(int32_t j0, int32_t j1, int32_t p_lo, int32_t p_hi, int32_t n, int32_t window,
                                         int32_t sinks) {
-  return j1 - 1 <= p_lo && j1 <= n && (window <= 0 || j0 > p_hi - window || j1 <= sinks);
+  return (j1 - 1 <= p_lo) & (j1 <= n) & ((window <= 0) | (j0 > p_hi - window) | (j1 <= sinks));
 }
+
+// The rows of a tile from j0 on that a query sees, as limits on the row's place x
+// in the tile: x <= hi and (x > lo or x < first), without branches. The asm keeps
+// the limits, and with them the comparisons, in the branch that needs them.
+struct Limits {
+  int32_t hi, lo, first;
+  __device__ __forceinline__ Limits(int32_t j0, int32_t p, int32_t n, int32_t window, int32_t sinks) {
+    hi = min(p, n - 1) - j0;
+    lo = window > 0 ? p - window - j0 : -1;
+    first = sinks - j0;
+    asm volatile("" : "+v"(hi), "+v"(lo), "+v"(first));
+  }
+  __device__ __forceinline__ bool operator()(int32_t x) const { return (x <= hi) & ((x > lo) | (x < first)); }
+};
+
+// Keeps a rare branch a branch: its body is not computed ahead and selected.
+__device__ __forceinline__ void rare() { asm volatile("" ::: "memory"); }
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
@@ -125,6 +145,7 @@ __device__ __forceinline__ U32x2 lds_column4(const char* p) {
 // places, so the tiles and parts that read one head's rows share its L2.
 struct Place {
   int32_t slot, b, h, tile, split;
+  int32_t first;  // slot of the row tile's first part
 };
 __device__ __forceinline__ Place place_of(const AttendArgs& a) {
   const uint32_t per = (uint32_t)(a.blocks + 7) / 8u;
@@ -145,6 +166,7 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a) {
   const AttendStream& s = a.s[lo];
   uint32_t x = (uint32_t)(p.slot - s.start);
   p.split = (int32_t)(x % (uint32_t)s.splits);
+  p.first = p.slot - p.split;
   x /= (uint32_t)s.splits;
   // the last row tile first: under a causal mask it has the most keys
   p.tile = s.tiles - 1 - (int32_t)(x % (uint32_t)s.tiles);
@@ -152,21 +174,42 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a) {
   return p;
 }
 
-__device__ __forceinline__ bool bf16_special(uint32_t w) {  // an infinity or NaN in either half
-  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+// Stored elements of a row that some query does not see: nothing of them if none
+// does, else without infinities and NaN (a product with a weight of zero would
+// be NaN). Whether any were taken out of a row that some see.
+template <int F>
+__device__ __forceinline__ bool clean(uint32_t (&x)[4], uint64_t& scales, int block, bool some) {
+  bool special = false, nan = false;
+  asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));  // nothing of this outside the branch that needs it
+  if constexpr (fmt_scaled(F)) {
+    nan = ((scales >> (8 * block)) & 255u) == 255u;
+    special = nan && some;
+    if (nan) scales = 0;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (!some || nan) x[e] = 0;
+    if constexpr (F == kFmtBf16) {
+      if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u, special = true;
+      if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu, special = true;
+    } else if constexpr (F == kFmtFp8) {
+#pragma unroll
+      for (int k = 0; k < 32; k += 8)
+        if (((x[e] >> k) & 0x7fu) == 0x7fu) x[e] &= ~(0xffu << k), special = true;
+    }
+  }
+  return special;
 }
 
-// Zero the infinities and NaN among eight bf16; whether there were any.
-__device__ __forceinline__ bool clear_special(Raw16& r) {
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (!bf16_special(r.w[i])) continue;
-    any = true;
-    if ((r.w[i] & 0x7f80u) == 0x7f80u) r.w[i] &= 0xffff0000u;
-    if ((r.w[i] & 0x7f800000u) == 0x7f800000u) r.w[i] &= 0xffffu;
-  }
-  return any;
+// Parts that another workgroup, maybe on another XCD, will read: stored and loaded
+// past this XCD's L2.
+__device__ __forceinline__ void store_part(float* p, float a, float b) {
+  const uint64_t v = ((uint64_t)__float_as_uint(b) << 32) | __float_as_uint(a);
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void load_part(const float* p, float& a, float& b) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  a = __uint_as_float((uint32_t)v), b = __uint_as_float((uint32_t)(v >> 32));
 }
 
 // One element of V, for the rare rows that need care.
@@ -241,21 +284,37 @@ struct FewCfg {
   }
 };
 
+// Workgroups of a CU, by registers.
+constexpr int few_per_cu(int F, int D, int NB) { return NB * D > 256 ? 1 : fmt_scaled(F) && NB * D <= 128 ? 3 : 2; }
+
 template <int D, int NB>
 constexpr size_t few_wave_lds() {
   const size_t tile = (size_t)kFewKeys * D * 2, join = (size_t)16 * NB * (D + 4) * 4;
   return tile > join ? tile : join;
 }
 
+// Four elements of row r's result, and its lse: v, sum and top are the weighted
+// sum, the sum of the weights and the maximum they are relative to.
+template <int D>
+__device__ __forceinline__ void few_out(const AttendArgs& a, int b, int h, int r, int d, const F32x4& v, float top, float sum) {
+  const int tok = (int)fast_div((uint32_t)r, a.G_div), head = h * a.G + r - tok * a.G;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  *reinterpret_cast<U32x2*>(a.out + 2 * ((int64_t)b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m + d)) =
+      U32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
+  if (d == 0 && a.lse)
+    a.lse[((int64_t)b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (top + log2_hw(sum)) * kLn2;
+}
+
 template <int F, int D, int NB>
-__global__ __launch_bounds__(64 * kFewWaves) void k_attend_few(AttendArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend_few(AttendArgs a) {
   using C = FewCfg<F, D>;
   __shared__ __attribute__((aligned(16))) char lds[kFewWaves][few_wave_lds<D, NB>()];
   __shared__ float lds_ml[kFewWaves][16 * NB][2];
   const Place pl = place_of(a);
   if (pl.slot < 0) return;  // the whole workgroup
   const AttendStream st = a.s[pl.b];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, g = lane / 16, l16 = lane % 16;
+  const int lane = threadIdx.x % kWave, g = lane / 16, l16 = lane % 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int32_t n = st.n, p_lo = st.first, p_hi = st.first + st.rows - 1, R = st.rows * a.G;
   const int b = a.b0 + pl.b;
   const int64_t head_row = a.layer_row + (int64_t)pl.h * a.pool.T.d;
@@ -288,9 +347,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_attend_few(AttendArgs a) {
   }
 
   bool bad = false;
-  // row (in the pool) of the tile's key lane % 32; a key past the last is the last
-  auto row_of = [&](int32_t tt) {
-    const int32_t j = kt.tile(min(tt, kt.count - 1)) * kFewKeys + lane % 32;
+  // pages that hold whole tiles: a tile's rows follow each other
+  const bool whole = a.pool.T.d % kFewKeys == 0;
+  // row (in the pool) of the tile's key lane % 32, or of its first; a key past the last is the last
+  auto row_of = [&](int32_t tt) __attribute__((always_inline)) {
+    const int32_t j = kt.tile(min(tt, kt.count - 1)) * kFewKeys + (whole ? 0 : lane % 32);
     bool x;
     const int64_t r = pool_row(a.pool, b, (uint32_t)min(j, n - 1), &x) + head_row;
     bad |= x;
@@ -298,28 +359,39 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_attend_few(AttendArgs a) {
   };
   uint32_t kr[2][C::KQ / 4], vr[C::NV][4];
   uint64_t ks[2], vs[C::NV];
-  auto fetch = [&](int64_t row) {
+  auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+    int64_t kw[2], vw[C::NV];  // the rows (of the pool) of this lane's pieces
+    if (whole) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) kw[kb] = row + (kb * 16 + l16);
+#pragma unroll
+      for (int i = 0; i < C::NV; ++i) vw[i] = row + (i * kWave + lane) / C::CPR % kFewKeys;
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) kw[kb] = shfl64(row, kb * 16 + l16);
+#pragma unroll
+      for (int i = 0; i < C::NV; ++i) vw[i] = shfl64(row, (i * kWave + lane) / C::CPR % kFewKeys);
+    }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      const int64_t r = shfl64(row, kb * 16 + l16);
-      const char* p = a.pool.K + r * C::RB + g * C::KB;
+      const char* p = a.pool.K + kw[kb] * C::RB + g * C::KB;
 #pragma unroll
       for (int c = 0; c < C::KN; ++c) load_piece<C::KB>(p + c * 4 * C::KB, kr[kb] + c * (C::KB / 4));
-      if (fmt_scaled(F)) ks[kb] = load_scales<D>(a.pool.Ks, r);
+      if (fmt_scaled(F)) ks[kb] = load_scales<D>(a.pool.Ks, kw[kb]);
     }
 #pragma unroll
     for (int i = 0; i < C::NV; ++i) {
-      const int x = i * kWave + lane, key = (x / C::CPR) % kFewKeys;
-      const int64_t r = shfl64(row, key);
-      load_piece<16>(a.pool.V + r * C::RB + (x % C::CPR) * 16, vr[i]);
-      if (fmt_scaled(F)) vs[i] = load_scales<D>(a.pool.Vs, r);
+      load_piece<16>(a.pool.V + vw[i] * C::RB + lane % C::CPR * 16, vr[i]);
+      if (fmt_scaled(F)) vs[i] = load_scales<D>(a.pool.Vs, vw[i]);
     }
   };
 
   char* tile = lds[wave];
-  int64_t row = 0, next = 0;
+  int64_t next = 0;
+  bool special = false;  // V held infinities or NaN in rows that only some queries see
+  const int32_t t_begin = t;
   if (t < t_end) {
-    row = row_of(t);
+    const int64_t row = row_of(t);
     next = row_of(t + kFewWaves);
     fetch(row);
   }
@@ -344,39 +416,41 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_attend_few(AttendArgs a) {
         }
     }
     // V into LDS as bf16; rows that no query sees become zeros, and what is
-    // infinite or NaN in rows that only some see is taken out and added below
-    bool special = false;
+    // infinite or NaN in rows that only some see is taken out and added at the end
+    if (!full) {
+      int32_t jv = j0;
+      asm volatile("" : "+v"(jv));
+#pragma unroll
+      for (int i = 0; i < C::NV; ++i) {
+        const int x = i * kWave + lane;
+        special |= clean<F>(vr[i], vs[i], x % C::CPR * C::VE / kScaleBlock, kt.some(jv + x / C::CPR));
+      }
+    }
 #pragma unroll
     for (int i = 0; i < C::NV; ++i) {
       const int x = i * kWave + lane, key = x / C::CPR, col = x % C::CPR;
       if (C::CPR == 1 && x >= kFewKeys) continue;
       const float scale = fmt_scaled(F) ? scale_at(vs[i], col * C::VE / kScaleBlock) : 0.f;
 #pragma unroll
-      for (int s = 0; s < C::VE / 8; ++s) {
-        Raw16 v = piece8<F>(vr[i], s, scale);
-        if (!full) {
-          if (!kt.some(j0 + key)) v = Raw16{0, 0, 0, 0};
-          else special |= clear_special(v);
-        }
-        *reinterpret_cast<Raw16*>(tile + key * (D * 2) + 16 * ((col * (C::VE / 8) + s) ^ C::swz(key))) = v;
-      }
+      for (int e = 0; e < C::VE / 8; ++e)
+        *reinterpret_cast<Raw16*>(tile + key * (D * 2) + 16 * ((col * (C::VE / 8) + e) ^ C::swz(key))) = piece8<F>(vr[i], e, scale);
     }
-    const int64_t here = row;
     if (t + kFewWaves < t_end) {
-      row = next;
-      fetch(row);
+      fetch(next);
       next = row_of(t + 2 * kFewWaves);
     }
     // softmax: weights of 8 keys a lane, keys 4 g + i and 16 + 4 g + i
     Bf16x8 w[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      if (!full)
+      if (!full) {
+        const Limits in(j0 + 4 * g, pos[nb], n, a.window, a.sinks);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!sees(j0 + kb * 16 + 4 * g + i, pos[nb], n, a.window, a.sinks)) sc[nb][kb][i] = -INFINITY;
+            if (!in(kb * 16 + i)) sc[nb][kb][i] = -INFINITY;
+      }
       float top = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, sc[nb][0][i]), sc[nb][1][i]);
@@ -408,11 +482,17 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_attend_few(AttendArgs a) {
         o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf16x8, r), w[nb], o[nb][db], 0, 0, 0);
     }
     __builtin_amdgcn_wave_barrier();
-    if (!full && __ballot(special) != 0) {
+  }
+  if (__ballot(special) != 0) {
+#pragma unroll 1
+    for (int32_t tt = t_begin; tt < t_end; tt += kFewWaves) {
+      const int32_t j0 = kt.tile(tt) * kFewKeys;
+      if (all_see(j0, j0 + kFewKeys, p_lo, p_hi, n, a.window, a.sinks)) continue;
+      const int64_t row = row_of(tt);
 #pragma unroll 1
       for (int key = 0; key < kFewKeys; ++key) {
         if (!kt.some(j0 + key)) continue;
-        const int64_t r = shfl64(here, key);
+        const int64_t r = whole ? row + key : shfl64(row, key);
 #pragma unroll
         for (int db = 0; db < D / 16; ++db)
 #pragma unroll
@@ -459,26 +539,74 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_attend_few(AttendArgs a) {
       v += *reinterpret_cast<const F32x4*>(reinterpret_cast<const float*>(lds[w]) + r * STRIDE + d);
     }
     if (st.splits > 1) {
-      *reinterpret_cast<F32x4*>(a.part + ((int64_t)pl.slot * (16 * NB) + r) * D + d) = v;
-      if (d == 0) {
-        float* ml = a.part_ml + ((int64_t)pl.slot * (16 * NB) + r) * 2;
-        ml[0] = top, ml[1] = sum;
-      }
+      float* at = a.part + ((int64_t)pl.slot * (16 * NB) + r) * D + d;
+      store_part(at, v[0], v[1]);
+      store_part(at + 2, v[2], v[3]);
+      if (d == 0) store_part(a.part_ml + ((int64_t)pl.slot * (16 * NB) + r) * 2, top, sum);
     } else {
-      const int tok = (int)fast_div((uint32_t)r, a.G_div), head = pl.h * a.G + r - tok * a.G;
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      uint32_t* at = reinterpret_cast<uint32_t*>(a.out + 2 * ((int64_t)b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m + d));
-      at[0] = pack_bf16(v[0] * inv, v[1] * inv), at[1] = pack_bf16(v[2] * inv, v[3] * inv);
-      if (d == 0 && a.lse)
-        a.lse[((int64_t)b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (top + log2_hw(sum)) * kLn2;
+      few_out<D>(a, b, pl.h, r, d, v, top, sum);
     }
+  }
+  if (st.splits <= 1) return;
+
+  // the row tile's last workgroup to come joins all its parts, in their order
+  __shared__ uint32_t lds_last;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's parts are written
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t* count = a.arrived + pl.first;
+    const uint32_t before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    lds_last = before + 1 == (uint32_t)st.splits;
+    if (lds_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!lds_last) return;
+  // weights of the parts, by row: lane s has part s
+  float(*weight)[kMaxSplits] = reinterpret_cast<float(*)[kMaxSplits]>(lds[0]);
+  static_assert(sizeof(lds) >= sizeof(float) * 16 * NB * kMaxSplits, "the parts' weights fit where the sums were");
+  const int rows = min(R, 16 * NB);
+  for (int r = wave; r < rows; r += kFewWaves) {
+    float pm = -INFINITY, ps = 0.f;
+    if (lane < st.splits) load_part(a.part_ml + ((int64_t)(pl.first + lane) * (16 * NB) + r) * 2, pm, ps);
+    float top = pm;
+#pragma unroll
+    for (int k = 1; k < kWave; k *= 2) top = fmaxf(top, __shfl_xor(top, k, kWave));
+    const float f = exp2_hw(pm - shift_of(top));
+    float sum = ps * f;
+#pragma unroll
+    for (int k = 1; k < kWave; k *= 2) sum += __shfl_xor(sum, k, kWave);
+    weight[r][lane] = f;
+    if (lane == 0) lds_ml[0][r][0] = top, lds_ml[0][r][1] = sum;
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < rows * (D / 4); x += 64 * kFewWaves) {
+    const int r = x / (D / 4), d = x % (D / 4) * 4;
+    const float* at = a.part + ((int64_t)pl.first * (16 * NB) + r) * D + d;
+    F32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < st.splits; k0 += 8) {
+      float y[8][4];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {  // the last again past the last, with no weight
+        const float* from = at + (int64_t)min(k0 + k, st.splits - 1) * (16 * NB) * D;
+        load_part(from, y[k][0], y[k][1]);
+        load_part(from + 2, y[k][2], y[k][3]);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float f = k0 + k < st.splits ? weight[r][k0 + k] : 0.f;
+        if (k0 + k < st.splits) v += F32x4{y[k][0], y[k][1], y[k][2], y[k][3]} * f;
+      }
+    }
+    few_out<D>(a, b, pl.h, r, d, v, lds_ml[0][r][0], lds_ml[0][r][1]);
   }
 }
 
 // ---------------------------------------------------------------- many rows
-// Row tiles of 32 * NQ * W rows, keys in tiles of 64 through LDS, where all waves
-// read them; the next tile's rows are in flight meanwhile.
+// Row tiles of 32 rows a wave, keys in tiles of 64 through LDS, where all waves
+// read them; the next tiles' rows are in flight meanwhile. Two waves a SIMD, or one
+// for D = 256, whose sums and queries alone take 192 registers.
 constexpr int kTileKeys = 64;
+__host__ __device__ constexpr int tile_waves(int D) { return D <= 128 ? 8 : 4; }
 
 template <int F, int D, int W>
 struct TileCfg {
@@ -489,7 +617,7 @@ struct TileCfg {
   static constexpr int E = 128 / fmt_bits(F);                          // elements a chunk
   // LDS places of 16-byte chunks of bf16: K is read 16 bytes a lane from 32
   // rows, V by transposing reads of 4 rows and 32 columns
-  static __device__ int kswz(int row) { return D >= 64 ? row & 7 : (row >> 2) & 3; }
+  static __device__ int kswz(int row) { return D >= 128 ? row & 15 : D == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
   static __device__ int vswz(int row) { return D >= 128 ? 4 * (row & 3) : D == 64 ? 4 * ((row >> 1) & 1) : 0; }
 };
 
@@ -497,13 +625,13 @@ struct TileCfg {
 // below 2^8, which costs no bit of their bf16 or of the fp32 sums.
 constexpr float kLazy = 8.f;
 
-template <int F, int D, int W, int NQ>
-__global__ __launch_bounds__(64 * W) void k_attend_tile(AttendArgs a) {
+template <int F, int D>
+__global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_attend_tile(AttendArgs a) {
+  constexpr int W = tile_waves(D), BM = 32 * W, BN = kTileKeys;
   using C = TileCfg<F, D, W>;
-  constexpr int BM = 32 * NQ * W, BN = kTileKeys;
   __shared__ __attribute__((aligned(16))) char ldsK[2][BN * D * 2];
   __shared__ __attribute__((aligned(16))) char ldsV[2][BN * D * 2];
-  __shared__ int32_t lds_special[2];
+  __shared__ int32_t lds_special;
   const Place pl = place_of(a);
   if (pl.slot < 0) return;
   const AttendStream st = a.s[pl.b];
@@ -518,186 +646,261 @@ __global__ __launch_bounds__(64 * W) void k_attend_tile(AttendArgs a) {
   const int32_t t_end = (int32_t)((int64_t)kt.count * (pl.split + 1) / st.splits);
   int32_t t = (int32_t)((int64_t)kt.count * pl.split / st.splits);
 
-  Bf16x8 q[NQ][D / 16];
-  int32_t pos[NQ];
-#pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    const int r = min(r0 + (wave * NQ + nq) * 32 + l32, R - 1), tok = (int)fast_div((uint32_t)r, a.G_div);
-    pos[nq] = st.first + tok;
+  Bf16x8 q[D / 16];
+  int32_t pos;
+  {
+    const int r = min(r0 + wave * 32 + l32, R - 1), tok = (int)fast_div((uint32_t)r, a.G_div);
+    pos = st.first + tok;
     const char* at = a.q + 2 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + r - tok * a.G) * a.q_h + (int64_t)tok * a.q_m);
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) q[nq][kk] = __builtin_bit_cast(Bf16x8, load16(at + 2 * (16 * kk + 8 * h)));
+    for (int kk = 0; kk < D / 16; ++kk) q[kk] = __builtin_bit_cast(Bf16x8, load16(at + 2 * (16 * kk + 8 * h)));
   }
   // the wave's own positions
-  const int32_t pw_lo = st.first + (int32_t)fast_div((uint32_t)min(r0 + wave * NQ * 32, R - 1), a.G_div);
-  const int32_t pw_hi = st.first + (int32_t)fast_div((uint32_t)min(r0 + (wave + 1) * NQ * 32 - 1, R - 1), a.G_div);
+  const int32_t pw_lo = st.first + (int32_t)fast_div((uint32_t)min(r0 + wave * 32, R - 1), a.G_div);
+  const int32_t pw_hi = st.first + (int32_t)fast_div((uint32_t)min(r0 + wave * 32 + 31, R - 1), a.G_div);
 
-  F32x16 o[NQ][D / 32];
-  float m[NQ], l[NQ];
+  F32x16 o[D / 32];
+  float m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    m[nq] = -INFINITY, l[nq] = 0.f;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-      for (int k = 0; k < 16; ++k) o[nq][i][k] = 0.f;
-  }
-  if (threadIdx.x < 2) lds_special[threadIdx.x] = -1;
+  for (int i = 0; i < D / 32; ++i) o[i] = F32x16{};
+  if (threadIdx.x == 0) lds_special = 0;
 
   bool bad = false;
-  auto row_of = [&](int32_t tt) {  // the pool's row of the tile's key `lane`
-    const int32_t j = kt.tile(min(tt, kt.count - 1)) * BN + lane;
+  // pages that hold whole tiles: a tile's rows follow each other
+  const bool whole = a.pool.T.d % BN == 0;
+  auto row_of = [&](int32_t tt) {  // the pool's row of the tile's key `lane` (whole: of its first key)
+    const int32_t j = kt.tile(min(tt, kt.count - 1)) * BN + (whole ? 0 : lane);
     bool x;
     const int64_t r = pool_row(a.pool, b, (uint32_t)min(j, n - 1), &x) + head_row;
     bad |= x;
     return r;
   };
-  uint32_t kr[C::NL][4], vr[C::NL][4];
-  uint64_t ks[C::NL], vs[C::NL];
-  auto fetch = [&](int64_t row) {
+  // rows on their way to LDS (D = 256 has no registers for both: V's are fetched when K's are there)
+  constexpr bool BOTH = D <= 128;
+  uint32_t kr[C::NL][4], vx[BOTH ? C::NL : 1][4];
+  uint64_t ks[C::NL], vsx[BOTH ? C::NL : 1];
+  auto& vr = [&]() -> auto& { if constexpr (BOTH) return vx; else return kr; }();
+  auto& vs = [&]() -> auto& { if constexpr (BOTH) return vsx; else return ks; }();
+  // this thread's chunks: column threadIdx.x % CPR of rows key0 + i * 64 W / CPR
+  const int key0 = threadIdx.x / C::CPR % BN;
+  constexpr int STEP = 64 * W / C::CPR;
+  auto load_tile = [&](const char* pages, const uint8_t* scales, int64_t row, uint32_t (&x)[C::NL][4], uint64_t (&xs)[C::NL]) __attribute__((always_inline)) {
+    int64_t r[C::NL];
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < C::NL; ++i) r[i] = row + (key0 + i * STEP);
+    } else {
+#pragma unroll
+      for (int i = 0; i < C::NL; ++i) r[i] = shfl64(row, key0 + i * STEP);
+    }
 #pragma unroll
     for (int i = 0; i < C::NL; ++i) {
-      const int x = i * 64 * W + threadIdx.x, key = (x / C::CPR) % BN;
-      const int64_t r = shfl64(row, key);
-      load_piece<16>(a.pool.K + r * C::RB + (x % C::CPR) * 16, kr[i]);
-      load_piece<16>(a.pool.V + r * C::RB + (x % C::CPR) * 16, vr[i]);
-      if (fmt_scaled(F)) ks[i] = load_scales<D>(a.pool.Ks, r), vs[i] = load_scales<D>(a.pool.Vs, r);
+      load_piece<16>(pages + r[i] * C::RB + threadIdx.x % C::CPR * 16, x[i]);
+      if (fmt_scaled(F)) xs[i] = load_scales<D>(scales, r[i]);
     }
   };
-  auto stage = [&](int32_t tt, int buf) {
-    const int32_t j0 = kt.tile(tt) * BN;
-    const bool full = all_see(j0, j0 + BN, p_lo, p_hi, n, a.window, a.sinks);
-    bool special = false;
+  auto fetch_k = [&](int64_t row) __attribute__((always_inline)) { load_tile(a.pool.K, a.pool.Ks, row, kr, ks); };
+  auto fetch_v = [&](int64_t row) __attribute__((always_inline)) { load_tile(a.pool.V, a.pool.Vs, row, vr, vs); };
+  const int col = threadIdx.x % C::CPR, block = col * C::E / kScaleBlock;
+  const bool mine = C::CHUNKS >= 64 * W || (int)threadIdx.x < C::CHUNKS;
+  auto stage_k = [&](int buf) __attribute__((always_inline)) {
+    if (!mine) return;
 #pragma unroll
     for (int i = 0; i < C::NL; ++i) {
-      const int x = i * 64 * W + threadIdx.x, key = x / C::CPR, col = x % C::CPR;
-      if (C::CHUNKS < 64 * W && x >= C::CHUNKS) continue;
-      const int block = col * C::E / kScaleBlock;
+      const int key = key0 + i * STEP;
 #pragma unroll
-      for (int s = 0; s < C::E / 8; ++s) {
-        const int ch = col * (C::E / 8) + s;
-        *reinterpret_cast<Raw16*>(ldsK[buf] + key * (D * 2) + 16 * (ch ^ C::kswz(key))) =
-            piece8<F>(kr[i], s, fmt_scaled(F) ? scale_at(ks[i], block) : 0.f);
-        Raw16 v = piece8<F>(vr[i], s, fmt_scaled(F) ? scale_at(vs[i], block) : 0.f);
-        if (!full) {
-          if (!kt.some(j0 + key)) v = Raw16{0, 0, 0, 0};
-          else special |= clear_special(v);
-        }
-        *reinterpret_cast<Raw16*>(ldsV[buf] + key * (D * 2) + 16 * (ch ^ C::vswz(key))) = v;
-      }
+      for (int e = 0; e < C::E / 8; ++e)
+        *reinterpret_cast<Raw16*>(ldsK[buf] + key * (D * 2) + 16 * ((col * (C::E / 8) + e) ^ C::kswz(key))) =
+            piece8<F>(kr[i], e, fmt_scaled(F) ? scale_at(ks[i], block) : 0.f);
     }
-    if (special) lds_special[buf] = tt;
+  };
+  auto stage_v = [&](int32_t tt, int buf) __attribute__((always_inline)) {
+    if (!mine) return;
+    const int32_t j0 = kt.tile(tt) * BN;
+    if (!all_see(j0, j0 + BN, p_lo, p_hi, n, a.window, a.sinks)) {
+      // rows that no query sees become zeros, and what is infinite or NaN in
+      // rows that only some see is taken out here and added at the end
+      int32_t jv = j0;
+      asm volatile("" : "+v"(jv));
+      bool special = false;
+#pragma unroll
+      for (int i = 0; i < C::NL; ++i) special |= clean<F>(vr[i], vs[i], block, kt.some(jv + key0 + i * STEP));
+      if (special) lds_special = 1;
+    }
+#pragma unroll
+    for (int i = 0; i < C::NL; ++i) {
+      const int key = key0 + i * STEP;
+#pragma unroll
+      for (int e = 0; e < C::E / 8; ++e)
+        *reinterpret_cast<Raw16*>(ldsV[buf] + key * (D * 2) + 16 * ((col * (C::E / 8) + e) ^ C::vswz(key))) =
+            piece8<F>(vr[i], e, fmt_scaled(F) ? scale_at(vs[i], block) : 0.f);
+    }
   };
 
-  int64_t row = 0, next = 0;
-  if (t < t_end) {
-    row = row_of(t);
-    next = row_of(t + 1);
-    fetch(row);
+  // LDS addresses of a lane's operands: the rest is the same for all lanes
+  int kat[D / 16], vat[D / 32];
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) kat[kk] = l32 * (D * 2) + 16 * ((2 * kk + h) ^ C::kswz(l32));
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) {
+    const int k0 = 4 * h + (lane % 16) / 4, ch = 4 * db + 2 * ((lane / 16) % 2) + (lane % 4) / 2;
+    vat[db] = k0 * (D * 2) + 16 * (ch ^ C::vswz(k0)) + 8 * (lane & 1);
   }
-  __syncthreads();
-  if (t < t_end) stage(t, 0);
-  int buf = 0;
-  for (; t < t_end; ++t, buf ^= 1) {
-    const int64_t here = row;
-    const bool more = t + 1 < t_end;
-    if (more) {
-      row = next;
-      fetch(row);
-      next = row_of(t + 2);
-    }
-    __syncthreads();  // tile t is in LDS, and no wave reads the other buffer any more
+  // A tile's scores, a lane's largest of them, and the weights made from them.
+  F32x16 s[2];
+  float most = -INFINITY;
+  const auto k_operand = [&](int kbuf, int i) __attribute__((always_inline)) {  // of the i-th product of a tile's scores
+    return __builtin_bit_cast(Bf16x8, load16(ldsK[kbuf] + i / (D / 16) * 32 * (D * 2) + kat[i % (D / 16)]));
+  };
+  const auto v_operand = [&](int vbuf, int i) __attribute__((always_inline)) {  // of the i-th product with the weights
+    const char* at = ldsV[vbuf] + i / (D / 32) * 16 * (D * 2) + vat[i % (D / 32)];
+    const U32x2 x = lds_column4(at), y = lds_column4(at + 8 * (D * 2));
+    return __builtin_bit_cast(Bf16x8, Raw16{x.x, x.y, y.x, y.y});
+  };
+  const auto largest = [&](const F32x16 (&x)[2], int i0, int i1, float v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = i0; i < i1; ++i) v = fmaxf(fmaxf(v, x[0][i]), x[1][i]);
+    return v;
+  };
+  // Tile t: its scores are there, its V is in buffer BUF. The scores of tile
+  // t + 1 are computed beside its softmax. A product takes the matrix unit 32 cycles
+  // in which the vector unit is free: the source has between two products what
+  // fits there, and their operands' reads two or three products ahead.
+  int64_t row = 0, next = 0;  // rows of tiles t + 1, t + 2
+  const int32_t t_begin = t;
+  auto step = [&](auto bufc) __attribute__((always_inline)) {
+    constexpr int BUF = decltype(bufc)::value;
+    constexpr int NS = D / 8, NP = D / 8, HALF = NP / 2;  // products for the scores, and with the weights
+    __syncthreads();  // K of t + 1 and V of t are in LDS, and no wave reads what is written below
+    fetch_k(next);
+    if constexpr (BOTH) fetch_v(row);
+    const int64_t later = row_of(t + 3);
     const int32_t j0 = kt.tile(t) * BN;
-    const bool full = all_see(j0, j0 + BN, pw_lo, pw_hi, n, a.window, a.sinks);
-    // nothing of the tile is seen by this wave's queries
-    const bool none = j0 > pw_hi || (a.window > 0 && j0 + BN - 1 <= pw_lo - a.window && j0 >= a.sinks);
-    if (!none) {
-      F32x16 s[NQ][2];
+    if (!all_see(j0, j0 + BN, pw_lo, pw_hi, n, a.window, a.sinks)) {
+      const Limits in(j0 + 4 * h, pos, n, a.window, a.sinks);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int nq = 0; nq < NQ; ++nq)
+        for (int i = 0; i < 16; ++i)
+          if (!in(kb * 32 + 8 * (i / 4) + i % 4)) s[kb][i] = -INFINITY;
+      most = largest(s, 0, 16, -INFINITY);
+    }
+    float top = lanes_max<2>(most) * a.c;
+    if (__ballot(top > m + kLazy) != 0) {
+      rare();
+      top = fmaxf(top, m);
+      const float old = exp2_hw(m - shift_of(top));
+      m = top;
+      l *= old;
 #pragma unroll
-          for (int k = 0; k < 16; ++k) s[nq][kb][k] = 0.f;
-        const int key = kb * 32 + l32;
-        const char* at = ldsK[buf] + key * (D * 2);
+      for (int i = 0; i < D / 32; ++i) o[i] *= old;
+    }
+    const float shift = shift_of(m);
+    Bf16x8 w[4];
+    // pairs [p0, p1) of block kb's 16 weights
+    const auto weights = [&](int kb, int p0, int p1) __attribute__((always_inline)) {
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const Bf16x8 k = __builtin_bit_cast(Bf16x8, load16(at + 16 * ((2 * kk + h) ^ C::kswz(key))));
-#pragma unroll
-          for (int nq = 0; nq < NQ; ++nq) s[nq][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[nq][kk], s[nq][kb], 0, 0, 0);
-        }
+      for (int p = p0; p < p1; ++p) {
+        const float x = exp2_hw(__builtin_fmaf(s[kb][2 * p], a.c, -shift));
+        const float y = exp2_hw(__builtin_fmaf(s[kb][2 * p + 1], a.c, -shift));
+        w[kb * 2 + p / 4][p % 4 * 2] = (__bf16)x;
+        w[kb * 2 + p / 4][p % 4 * 2 + 1] = (__bf16)y;
+        l += x + y;  // (as fp32: the sum also gives the lse)
       }
-      Bf16x8 w[NQ][4];
+    };
+    F32x16 ahead[2];
+    // operands in flight: KA products ahead of the first, VA of the second
+    constexpr int KA = D > 128 ? 3 : NS < 5 ? NS : 5, VA = D > 128 ? 2 : NP < 4 ? NP : 4;
+    Bf16x8 kf[KA + 1], vf[VA + 1];
 #pragma unroll
-      for (int nq = 0; nq < NQ; ++nq) {
-        if (!full)
+    for (int i = 0; i < KA; ++i) kf[i] = k_operand(BUF ^ 1, i);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+    for (int i = 0; i < NS; ++i) {
+      if (i + KA < NS) kf[(i + KA) % (KA + 1)] = k_operand(BUF ^ 1, i + KA);
+      else if (i + KA - NS < VA) vf[i + KA - NS] = v_operand(BUF, i + KA - NS);
+      const int kb = i / (D / 16), kk = i % (D / 16);
+      ahead[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % (KA + 1)], q[kk], kk == 0 ? F32x16{} : ahead[kb], 0, 0, 0);
+      weights(0, 8 * i / NS, 8 * (i + 1) / NS);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (!BOTH) {
+      stage_k(BUF);
+      fetch_v(row);
+    }
+    float biggest = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (!sees(j0 + kb * 32 + 8 * (i / 4) + 4 * h + i % 4, pos[nq], n, a.window, a.sinks)) s[nq][kb][i] = -INFINITY;
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(fmaxf(top, s[nq][0][i]), s[nq][1][i]);
-        top = lanes_max<2>(top) * a.c;
-        if (__ballot(top > m[nq] + kLazy || (m[nq] == -INFINITY && top != -INFINITY)) != 0) {
-          top = fmaxf(top, m[nq]);
-          const float old = exp2_hw(m[nq] - shift_of(top));
-          m[nq] = top;
-          l[nq] *= old;
-#pragma unroll
-          for (int i = 0; i < D / 32; ++i) o[nq][i] *= old;
-        }
-        const float shift = shift_of(m[nq]);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float e = exp2_hw(__builtin_fmaf(s[nq][kb][i], a.c, -shift));
-            l[nq] += e;
-            w[nq][kb * 2 + i / 8][i % 8] = (__bf16)e;
-          }
+    for (int i = 0; i < NP; ++i) {
+      if (i + VA < NP) vf[(i + VA) % (VA + 1)] = v_operand(BUF, i + VA);
+      const int ks4 = i / (D / 32), db = i % (D / 32);
+      o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % (VA + 1)], w[ks4], o[db], 0, 0, 0);
+      if (i < HALF) {
+        weights(1, 8 * i / HALF, 8 * (i + 1) / HALF);
+      } else {
+        biggest = largest(ahead, 16 * (i - HALF) / HALF, 16 * (i - HALF + 1) / HALF, biggest);
+        asm volatile("" : "+v"(biggest));  // here, not where it is next used
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (BOTH) stage_k(BUF);
+    stage_v(t + 1, BUF ^ 1);
+    s[0] = ahead[0], s[1] = ahead[1];
+    most = biggest;
+    row = next, next = later;
+    ++t;
+  };
+  if (t < t_end) {
+    // tiles past the last are read as the last again, and not used
+    const int64_t here = row_of(t);
+    row = row_of(t + 1), next = row_of(t + 2);
+    fetch_k(here);
+    __syncthreads();  // lds_special is set
+    stage_k(0);
+    fetch_v(here);
+    stage_v(t, 0);
+    fetch_k(row);
+    __syncthreads();
 #pragma unroll
-      for (int ks4 = 0; ks4 < 4; ++ks4)
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) {
-          const int k0 = ks4 * 16 + 4 * h + (lane % 16) / 4;
-          const int ch = 4 * db + 2 * ((lane / 16) % 2) + (lane % 4) / 2, in = 8 * (lane & 1);
-          const U32x2 x = lds_column4(ldsV[buf] + k0 * (D * 2) + 16 * (ch ^ C::vswz(k0)) + in);
-          const U32x2 y = lds_column4(ldsV[buf] + (k0 + 8) * (D * 2) + 16 * (ch ^ C::vswz(k0 + 8)) + in);
-          const Raw16 r = {x.x, x.y, y.x, y.y};
-#pragma unroll
-          for (int nq = 0; nq < NQ; ++nq)
-            o[nq][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Bf16x8, r), w[nq][ks4], o[nq][db], 0, 0, 0);
-        }
-      if (lds_special[buf] == t) {
+    for (int i = 0; i < D / 8; ++i) {
+      const int kb = i / (D / 16), kk = i % (D / 16);
+      s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(0, i), q[kk], kk == 0 ? F32x16{} : s[kb], 0, 0, 0);
+    }
+    most = largest(s, 0, 16, -INFINITY);
+    stage_k(1);
+    for (;;) {
+      step(std::integral_constant<int, 0>());
+      if (t >= t_end) break;
+      step(std::integral_constant<int, 1>());
+      if (t >= t_end) break;
+    }
+    __syncthreads();
+    if (lds_special) {
+#pragma unroll 1
+      for (int32_t tt = t_begin; tt < t_end; ++tt) {
+        const int32_t j0 = kt.tile(tt) * BN;
+        if (all_see(j0, j0 + BN, p_lo, p_hi, n, a.window, a.sinks)) continue;
+        const int64_t tile_row = row_of(tt);
 #pragma unroll 1
         for (int key = 0; key < BN; ++key) {
           if (!kt.some(j0 + key)) continue;
-          const int64_t r = shfl64(here, key);
+          const int64_t r = whole ? tile_row + key : shfl64(tile_row, key);
 #pragma unroll
           for (int db = 0; db < D / 32; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const float v = v_element<F, D>(a.pool, r, 32 * db + 8 * (i / 4) + 4 * h + i % 4);
-#pragma unroll
-              for (int nq = 0; nq < NQ; ++nq)
-                if (!(fabsf(v) < INFINITY) && sees(j0 + key, pos[nq], n, a.window, a.sinks)) o[nq][db][i] += v;
+              if (!(fabsf(v) < INFINITY) && sees(j0 + key, pos, n, a.window, a.sinks)) o[db][i] += v;
             }
         }
       }
     }
-    if (more) stage(t + 1, buf ^ 1);
   }
   if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, kDevBadPage);
 
-#pragma unroll
-  for (int nq = 0; nq < NQ; ++nq) {
-    const int rr = (wave * NQ + nq) * 32 + l32, r = r0 + rr;
-    const float sum = lanes_sum<2>(l[nq]);
-    if (r >= R) continue;
+  {
+    const int rr = wave * 32 + l32, r = r0 + rr;
+    const float sum = lanes_sum<2>(l);
+    if (r >= R) return;
     if (st.splits > 1) {
       float* at = a.part + ((int64_t)pl.slot * BM + rr) * D;
 #pragma unroll
@@ -705,10 +908,10 @@ __global__ __launch_bounds__(64 * W) void k_attend_tile(AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           *reinterpret_cast<F32x4*>(at + 32 * db + 8 * i + 4 * h) =
-              F32x4{o[nq][db][4 * i], o[nq][db][4 * i + 1], o[nq][db][4 * i + 2], o[nq][db][4 * i + 3]};
+              F32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
       if (h == 0) {
         float* ml = a.part_ml + ((int64_t)pl.slot * BM + rr) * 2;
-        ml[0] = m[nq], ml[1] = sum;
+        ml[0] = m, ml[1] = sum;
       }
     } else {
       const int tok = (int)fast_div((uint32_t)r, a.G_div), head = pl.h * a.G + r - tok * a.G;
@@ -719,10 +922,10 @@ __global__ __launch_bounds__(64 * W) void k_attend_tile(AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           *reinterpret_cast<U32x2*>(at + 2 * (32 * db + 8 * i + 4 * h)) =
-              U32x2{pack_bf16(o[nq][db][4 * i] * inv, o[nq][db][4 * i + 1] * inv),
-                    pack_bf16(o[nq][db][4 * i + 2] * inv, o[nq][db][4 * i + 3] * inv)};
+              U32x2{pack_bf16(o[db][4 * i] * inv, o[db][4 * i + 1] * inv),
+                    pack_bf16(o[db][4 * i + 2] * inv, o[db][4 * i + 3] * inv)};
       if (h == 0 && a.lse)
-        a.lse[((int64_t)b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (m[nq] + log2_hw(sum)) * kLn2;
+        a.lse[((int64_t)b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (m + log2_hw(sum)) * kLn2;
     }
   }
 }
@@ -873,10 +1076,18 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int32_t BM) {
 #pragma unroll
   for (int e = 0; e < E; ++e) v[e] = 0.f;
   const float* p = a.part + (slot * BM + rr) * D + (lane * E) % D;
-  for (int s = 0; s < st.splits; ++s) {
-    const float f = __shfl(w, s, kWave);
+  for (int s0 = 0; s0 < st.splits; s0 += 8) {
+    float y[8][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] += f * p[(int64_t)s * BM * D + e];
+    for (int k = 0; k < 8; ++k)  // the last again past the last, with no weight
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[k][e] = p[(int64_t)min(s0 + k, st.splits - 1) * BM * D + e];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float f = __shfl(w, min(s0 + k, st.splits - 1), kWave);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = s0 + k < st.splits ? v[e] + f * y[k][e] : v[e];
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const int32_t tok = (int32_t)fast_div((uint32_t)r, a.G_div), head = h * a.G + r - tok * a.G;
@@ -898,8 +1109,7 @@ enum AttendKind { kFew1, kFew2, kTile, kF32 };
 template <int F>
 hipError_t launch_attend(int D, AttendKind kind, uint32_t grid, const AttendArgs& a, hipStream_t st);
 hipError_t launch_join(int D, bool f32, uint32_t rows, int32_t BM, const AttendArgs& a, hipStream_t st);
-constexpr int kTileW = 4, kTileNQ = 1;
-inline int attend_rows(AttendKind k) { return k == kFew1 ? 16 : k == kFew2 ? 32 : k == kF32 ? 32 : 32 * kTileW * kTileNQ; }
+inline int attend_rows(AttendKind k, int D) { return k == kFew1 ? 16 : k == kFew2 || k == kF32 ? 32 : 32 * tile_waves(D); }
 inline int attend_keys(AttendKind k) { return k == kTile ? kTileKeys : 32; }
 
 }  // namespace ipv

@@ -12,7 +12,7 @@ hipError_t launch_attend_d(AttendKind kind, uint32_t grid, const AttendArgs& a, 
   } else {
     if (kind == kFew1) k_attend_few<F, D, 1><<<dim3(grid), dim3(64 * kFewWaves), 0, st>>>(a);
     else if (kind == kFew2) k_attend_few<F, D, 2><<<dim3(grid), dim3(64 * kFewWaves), 0, st>>>(a);
-    else k_attend_tile<F, D, kTileW, kTileNQ><<<dim3(grid), dim3(64 * kTileW), 0, st>>>(a);
+    else k_attend_tile<F, D><<<dim3(grid), dim3(64 * tile_waves(D)), 0, st>>>(a);
   }
   return hipGetLastError();
 }

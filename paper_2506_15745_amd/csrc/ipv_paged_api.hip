@@ -163,8 +163,12 @@ ipv_status page_rows(const ipv_page_shape* s, const void* K_pages, const void* V
 }
 
 // ------------------------------------------------------------ attention
-// Workgroups that fill the card: below this number, key ranges are split.
-constexpr int32_t kFill = 512;
+// Workgroups that the card's 256 CUs hold at once: with fewer row tiles than that,
+// key ranges are split.
+int32_t attend_fill(AttendKind k, int D, int format) {
+  return 256 * (k == kTile ? 1 : k == kF32 ? 4 : few_per_cu(format, D, k == kFew1 ? 1 : 2));
+}
+constexpr int32_t kMaxParts = 1024;  // workgroups of a launch that splits, at most
 
 // The kernel for a call whose widest stream has `rows` rows a KV head.
 AttendKind attend_kind(int format, int64_t rows) {
@@ -172,7 +176,7 @@ AttendKind attend_kind(int format, int64_t rows) {
   return rows <= 16 ? kFew1 : rows <= 32 ? kFew2 : kTile;
 }
 
-size_t part_bytes(AttendKind k, int D) { return (size_t)(2 * kFill) * attend_rows(k) * (size_t)(D + 2) * sizeof(float); }
+size_t part_bytes(AttendKind k, int D) { return (size_t)kMaxParts * attend_rows(k, D) * (size_t)(D + 2) * sizeof(float); }
 
 ipv_status check_heads(const ipv_page_shape* s, int32_t streams, int32_t q_heads, int32_t max_rows) {
   if (streams < 1 || q_heads < 1 || max_rows < 1 || q_heads % s->kv_heads != 0) return IPV_ERR_SHAPE;
@@ -182,10 +186,10 @@ ipv_status check_heads(const ipv_page_shape* s, int32_t streams, int32_t q_heads
 
 // The split of one launch's streams: row tiles, parts of the key ranges, and
 // the first workgroup of each. A key range is split when the row tiles alone
-// leave the card unfilled, into parts of about equal length that give kFill
-// workgroups (few: at least a tile for each wave).
-void plan(AttendArgs* a, AttendKind kind) {
-  const int32_t BM = attend_rows(kind), BN = attend_keys(kind);
+// leave the card unfilled, into parts of about equal length that give about as many
+// workgroups as it holds (few: at least a tile for each wave).
+void plan(AttendArgs* a, AttendKind kind, int D, int format) {
+  const int32_t BM = attend_rows(kind, D), BN = attend_keys(kind);
   const bool few = kind == kFew1 || kind == kFew2;
   int64_t base = 0, work = 0;
   int32_t count[kAttendStreams];
@@ -199,11 +203,20 @@ void plan(AttendArgs* a, AttendKind kind) {
     base += (int64_t)a->H * s.tiles;
     work += (int64_t)a->H * s.tiles * count[i];
   }
-  if (base < kFill) {
-    int64_t per = std::max<int64_t>((work + kFill - 1) / kFill, few ? kFewWaves : 2);
-    if (few) per = (per + kFewWaves - 1) / kFewWaves * kFewWaves;
-    for (int32_t i = 0; i < a->streams; ++i)
-      a->s[i].splits = (int32_t)std::min<int64_t>(std::max<int64_t>((count[i] + per - 1) / per, 1), kMaxSplits);
+  const int32_t fill = attend_fill(kind, D, format);
+  if (base < fill) {
+    // parts of `per` tiles: the shortest that make no more workgroups than fit at once
+    const int64_t unit = few ? kFewWaves : 1;
+    int64_t per = std::max<int64_t>((work + fill - 1) / fill, few ? kFewWaves : 2);
+    per = (per + unit - 1) / unit * unit;
+    for (;; per += std::max(unit, per / 16 / unit * unit)) {
+      int64_t blocks = 0;
+      for (int32_t i = 0; i < a->streams; ++i) {
+        a->s[i].splits = (int32_t)std::min<int64_t>(std::max<int64_t>((count[i] + per - 1) / per, 1), kMaxSplits);
+        blocks += (int64_t)a->H * a->s[i].tiles * a->s[i].splits;
+      }
+      if (blocks <= fill || blocks == base) break;
+    }
   }
   int64_t at = 0;
   for (int32_t i = 0; i < a->streams; ++i) {
@@ -257,8 +270,12 @@ ipv_status ipv_attend_workspace_bytes(const ipv_page_shape* pool, int32_t stream
   if (!bytes) return IPV_ERR_NULL;
   IPV_TRY(check_pool_shape(pool));
   IPV_TRY(check_heads(pool, streams, q_heads, max_rows));
-  // a call of fewer rows may take a kernel of narrower tiles: the widest covers them all
-  *bytes = kWsHeader + part_bytes(attend_kind(pool->format, (int64_t)max_rows * (q_heads / pool->kv_heads)), pool->head_dim);
+  // a call of fewer rows may take a kernel of narrower tiles
+  const AttendKind widest = attend_kind(pool->format, (int64_t)max_rows * (q_heads / pool->kv_heads));
+  size_t parts = 0;
+  for (AttendKind k : {kFew1, kFew2, kTile, kF32})
+    if (k <= widest && (k == kF32) == (widest == kF32)) parts = std::max(parts, part_bytes(k, pool->head_dim));
+  *bytes = kWsHeader + kMaxParts * sizeof(uint32_t) + parts;
   return IPV_OK;
 }
 
@@ -312,9 +329,10 @@ ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const voi
     }
     if (most == 0) continue;
     const AttendKind kind = attend_kind(pool->format, (int64_t)most * a.G);
-    plan(&a, kind);
-    a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + kWsHeader);
-    a.part = a.part_ml + (size_t)(2 * kFill) * attend_rows(kind) * 2;
+    plan(&a, kind, pool->head_dim, pool->format);
+    a.arrived = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + kWsHeader);
+    a.part_ml = reinterpret_cast<float*>(a.arrived + kMaxParts);
+    a.part = a.part_ml + (size_t)kMaxParts * attend_rows(kind, pool->head_dim) * 2;
     const uint32_t grid = (uint32_t)(a.blocks + 7) / 8u * 8u;
     hipError_t e;
     switch (pool->format) {
@@ -324,11 +342,11 @@ ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const voi
       default: e = launch_attend<kFmtFp4>(pool->head_dim, kind, grid, a, st); break;
     }
     IPV_TRY(launched(e));
-    bool split = false;
+    bool split = false;  // the kernel of few rows joins its parts itself
     for (int32_t i = 0; i < a.streams; ++i) split |= a.s[i].splits > 1;
-    if (split)
+    if (split && (kind == kTile || kind == kF32))
       IPV_TRY(launched(launch_join(pool->head_dim, pool->format == IPV_PAGES_F32, (uint32_t)most * (uint32_t)q_heads,
-                                   attend_rows(kind), a, st)));
+                                   attend_rows(kind, pool->head_dim), a, st)));
   }
   return IPV_OK;
 }
