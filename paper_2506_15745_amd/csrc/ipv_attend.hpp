@@ -284,25 +284,111 @@ struct FewCfg {
   }
 };
 
+// LDS of the joining: each wave's sums of its keys, [row][D + 4] a wave, relative to
+// the workgroup's maximum of the row; their maxima and sums of weights.
+template <int D, int NR>
+struct JoinLds {
+  static constexpr int STRIDE = D + 4;
+  static constexpr size_t kWaveBytes = (size_t)NR * STRIDE * 4;
+};
+
 // Workgroups of a CU, by registers.
 constexpr int few_per_cu(int F, int D, int NB) { return NB * D > 256 ? 1 : fmt_scaled(F) && NB * D <= 128 ? 3 : 2; }
 
 template <int D, int NB>
 constexpr size_t few_wave_lds() {
-  const size_t tile = (size_t)kFewKeys * D * 2, join = (size_t)16 * NB * (D + 4) * 4;
+  constexpr size_t tile = (size_t)kFewKeys * D * 2, join = JoinLds<D, 16 * NB>::kWaveBytes;
   return tile > join ? tile : join;
 }
 
 // Four elements of row r's result, and its lse: v, sum and top are the weighted
 // sum, the sum of the weights and the maximum they are relative to.
-template <int D>
-__device__ __forceinline__ void few_out(const AttendArgs& a, int b, int h, int r, int d, const F32x4& v, float top, float sum) {
+template <int D, bool F32OUT>
+__device__ __forceinline__ void row_out(const AttendArgs& a, int b, int h, int r, int d, const F32x4& v, float top, float sum) {
   const int tok = (int)fast_div((uint32_t)r, a.G_div), head = h * a.G + r - tok * a.G;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  *reinterpret_cast<U32x2*>(a.out + 2 * ((int64_t)b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m + d)) =
-      U32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
+  const int64_t at = (int64_t)b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m + d;
+  if (F32OUT) *reinterpret_cast<F32x4*>(a.out + 4 * at) = v * inv;
+  else *reinterpret_cast<U32x2*>(a.out + 2 * at) = U32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
   if (d == 0 && a.lse)
     a.lse[((int64_t)b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (top + log2_hw(sum)) * kLn2;
+}
+
+// The waves' sums are in LDS: their total is the result of the first `rows` rows of the
+// row tile (rows r0, ... of the stream) or, where the keys are split, a part of it. The row
+// tile's last workgroup to come joins its parts, in their order.
+template <int D, int NR, bool F32OUT, size_t BYTES>
+__device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendStream& st, const Place& pl, int b, int r0, int rows,
+                                           char (&lds)[kFewWaves][BYTES], float (&lds_ml)[kFewWaves][NR][2], uint32_t* lds_last) {
+  constexpr int STRIDE = JoinLds<D, NR>::STRIDE;
+  static_assert(BYTES >= JoinLds<D, NR>::kWaveBytes && kFewWaves * BYTES >= sizeof(float) * NR * kMaxSplits, "LDS of the joining");
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  for (int x = threadIdx.x; x < rows * (D / 4); x += 64 * kFewWaves) {
+    const int r = x / (D / 4), d = x % (D / 4) * 4;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, lds_ml[w][r][0]);
+    F32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      sum += lds_ml[w][r][1] * exp2_hw(lds_ml[w][r][0] - shift_of(top));
+      v += *reinterpret_cast<const F32x4*>(reinterpret_cast<const float*>(lds[w]) + r * STRIDE + d);
+    }
+    if (st.splits > 1) {
+      float* at = a.part + ((int64_t)pl.slot * NR + r) * D + d;
+      store_part(at, v[0], v[1]);
+      store_part(at + 2, v[2], v[3]);
+      if (d == 0) store_part(a.part_ml + ((int64_t)pl.slot * NR + r) * 2, top, sum);
+    } else {
+      row_out<D, F32OUT>(a, b, pl.h, r0 + r, d, v, top, sum);
+    }
+  }
+  if (st.splits <= 1) return;
+
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's parts are written
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t* count = a.arrived + pl.first;
+    const uint32_t before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *lds_last = before + 1 == (uint32_t)st.splits;
+    if (*lds_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!*lds_last) return;
+  // weights of the parts, by row: lane s has part s
+  float(*weight)[kMaxSplits] = reinterpret_cast<float(*)[kMaxSplits]>(&lds[0][0]);
+  for (int r = wave; r < rows; r += kFewWaves) {
+    float pm = -INFINITY, ps = 0.f;
+    if (lane < st.splits) load_part(a.part_ml + ((int64_t)(pl.first + lane) * NR + r) * 2, pm, ps);
+    float top = pm;
+#pragma unroll
+    for (int k = 1; k < kWave; k *= 2) top = fmaxf(top, __shfl_xor(top, k, kWave));
+    const float f = exp2_hw(pm - shift_of(top));
+    float sum = ps * f;
+#pragma unroll
+    for (int k = 1; k < kWave; k *= 2) sum += __shfl_xor(sum, k, kWave);
+    weight[r][lane] = f;
+    if (lane == 0) lds_ml[0][r][0] = top, lds_ml[0][r][1] = sum;
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < rows * (D / 4); x += 64 * kFewWaves) {
+    const int r = x / (D / 4), d = x % (D / 4) * 4;
+    const float* at = a.part + ((int64_t)pl.first * NR + r) * D + d;
+    F32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < st.splits; k0 += 8) {
+      float y[8][4];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {  // the last again past the last, with no weight
+        const float* from = at + (int64_t)min(k0 + k, st.splits - 1) * NR * D;
+        load_part(from, y[k][0], y[k][1]);
+        load_part(from + 2, y[k][2], y[k][3]);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k0 + k < st.splits) v += F32x4{y[k][0], y[k][1], y[k][2], y[k][3]} * weight[r][k0 + k];
+    }
+    row_out<D, F32OUT>(a, b, pl.h, r0 + r, d, v, lds_ml[0][r][0], lds_ml[0][r][1]);
+  }
 }
 
 template <int F, int D, int NB>
@@ -310,6 +396,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
   using C = FewCfg<F, D>;
   __shared__ __attribute__((aligned(16))) char lds[kFewWaves][few_wave_lds<D, NB>()];
   __shared__ float lds_ml[kFewWaves][16 * NB][2];
+  __shared__ uint32_t lds_last;
   const Place pl = place_of(a);
   if (pl.slot < 0) return;  // the whole workgroup
   const AttendStream st = a.s[pl.b];
@@ -500,7 +587,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
             const float v = v_element<F, D>(a.pool, r, 16 * db + 4 * g + i);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
-              if (!(fabsf(v) < INFINITY) && sees(j0 + key, pos[nb], n, a.window, a.sinks)) o[nb][db][i] += v;
+              if (!(fabsf(v) < INFINITY) & sees(j0 + key, pos[nb], n, a.window, a.sinks)) o[nb][db][i] += v;
           }
       }
     }
@@ -514,7 +601,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
     if (lane < 16) lds_ml[wave][nb * 16 + lane][0] = m[nb], lds_ml[wave][nb * 16 + lane][1] = l[nb];
   }
   __syncthreads();
-  constexpr int STRIDE = D + 4;
+  constexpr int STRIDE = JoinLds<D, 16 * NB>::STRIDE;
   float* mine = reinterpret_cast<float*>(lds[wave]);
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
@@ -527,78 +614,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
       *reinterpret_cast<F32x4*>(mine + (nb * 16 + l16) * STRIDE + 16 * db + 4 * g) = o[nb][db] * f;
   }
   __syncthreads();
-  for (int x = threadIdx.x; x < min(R, 16 * NB) * (D / 4); x += 64 * kFewWaves) {
-    const int r = x / (D / 4), d = x % (D / 4) * 4;
-    float top = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, lds_ml[w][r][0]);
-    F32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) {
-      sum += lds_ml[w][r][1] * exp2_hw(lds_ml[w][r][0] - shift_of(top));
-      v += *reinterpret_cast<const F32x4*>(reinterpret_cast<const float*>(lds[w]) + r * STRIDE + d);
-    }
-    if (st.splits > 1) {
-      float* at = a.part + ((int64_t)pl.slot * (16 * NB) + r) * D + d;
-      store_part(at, v[0], v[1]);
-      store_part(at + 2, v[2], v[3]);
-      if (d == 0) store_part(a.part_ml + ((int64_t)pl.slot * (16 * NB) + r) * 2, top, sum);
-    } else {
-      few_out<D>(a, b, pl.h, r, d, v, top, sum);
-    }
-  }
-  if (st.splits <= 1) return;
-
-  // the row tile's last workgroup to come joins all its parts, in their order
-  __shared__ uint32_t lds_last;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's parts are written
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    uint32_t* count = a.arrived + pl.first;
-    const uint32_t before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    lds_last = before + 1 == (uint32_t)st.splits;
-    if (lds_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  if (!lds_last) return;
-  // weights of the parts, by row: lane s has part s
-  float(*weight)[kMaxSplits] = reinterpret_cast<float(*)[kMaxSplits]>(lds[0]);
-  static_assert(sizeof(lds) >= sizeof(float) * 16 * NB * kMaxSplits, "the parts' weights fit where the sums were");
-  const int rows = min(R, 16 * NB);
-  for (int r = wave; r < rows; r += kFewWaves) {
-    float pm = -INFINITY, ps = 0.f;
-    if (lane < st.splits) load_part(a.part_ml + ((int64_t)(pl.first + lane) * (16 * NB) + r) * 2, pm, ps);
-    float top = pm;
-#pragma unroll
-    for (int k = 1; k < kWave; k *= 2) top = fmaxf(top, __shfl_xor(top, k, kWave));
-    const float f = exp2_hw(pm - shift_of(top));
-    float sum = ps * f;
-#pragma unroll
-    for (int k = 1; k < kWave; k *= 2) sum += __shfl_xor(sum, k, kWave);
-    weight[r][lane] = f;
-    if (lane == 0) lds_ml[0][r][0] = top, lds_ml[0][r][1] = sum;
-  }
-  __syncthreads();
-  for (int x = threadIdx.x; x < rows * (D / 4); x += 64 * kFewWaves) {
-    const int r = x / (D / 4), d = x % (D / 4) * 4;
-    const float* at = a.part + ((int64_t)pl.first * (16 * NB) + r) * D + d;
-    F32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < st.splits; k0 += 8) {
-      float y[8][4];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {  // the last again past the last, with no weight
-        const float* from = at + (int64_t)min(k0 + k, st.splits - 1) * (16 * NB) * D;
-        load_part(from, y[k][0], y[k][1]);
-        load_part(from + 2, y[k][2], y[k][3]);
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float f = k0 + k < st.splits ? weight[r][k0 + k] : 0.f;
-        if (k0 + k < st.splits) v += F32x4{y[k][0], y[k][1], y[k][2], y[k][3]} * f;
-      }
-    }
-    few_out<D>(a, b, pl.h, r, d, v, lds_ml[0][r][0], lds_ml[0][r][1]);
-  }
+  join_parts<D, 16 * NB, false>(a, st, pl, b, 0, min(R, 16 * NB), lds, lds_ml, &lds_last);
 }
 
 // ---------------------------------------------------------------- many rows
@@ -889,7 +905,7 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const float v = v_element<F, D>(a.pool, r, 32 * db + 8 * (i / 4) + 4 * h + i % 4);
-              if (!(fabsf(v) < INFINITY) && sees(j0 + key, pos, n, a.window, a.sinks)) o[db][i] += v;
+              if (!(fabsf(v) < INFINITY) & sees(j0 + key, pos, n, a.window, a.sinks)) o[db][i] += v;
             }
         }
       }
@@ -931,16 +947,22 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
 }
 
 // ---------------------------------------------------------------- fp32 pools
-// One wave has 32 rows and a part of the keys, 32 at a time, with the fp32 matrix
-// instruction (an eighteenth of the bf16 one's rate, so rows are read straight
-// from the caches into its operands, without LDS).
+// Row tiles of 32 rows; the four waves share the keys, 32 at a time, with the fp32
+// matrix instruction. It has a sixteenth of the bf16 one's rate, so rows are read
+// straight from the caches into its operands, without LDS. Its operands take one
+// element a lane: half h of the wave holds the elements h * D / 2 + k of a key, and
+// S^T leaves the weights as the second product's operand as they stand.
 template <int D>
-__global__ __launch_bounds__(64) void k_attend_f32(AttendArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(AttendArgs a) {
   constexpr int BN = 32;
+  __shared__ __attribute__((aligned(16))) char lds[kFewWaves][JoinLds<D, 32>::kWaveBytes];
+  __shared__ float lds_ml[kFewWaves][32][2];
+  __shared__ uint32_t lds_last;
   const Place pl = place_of(a);
   if (pl.slot < 0) return;
   const AttendStream st = a.s[pl.b];
-  const int lane = threadIdx.x, h = lane / 32, l32 = lane % 32;
+  const int lane = threadIdx.x % kWave, h = lane / 32, l32 = lane % 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int32_t n = st.n, R = st.rows * a.G, r0 = pl.tile * 32;
   const int b = a.b0 + pl.b;
   const int64_t head_row = a.layer_row + (int64_t)pl.h * a.pool.T.d;
@@ -948,11 +970,10 @@ __global__ __launch_bounds__(64) void k_attend_f32(AttendArgs a) {
   const int32_t p_hi = st.first + (int32_t)fast_div((uint32_t)(min(r0 + 32, R) - 1), a.G_div);
   const KeyTiles kt(n, p_lo, p_hi, a.window, a.sinks, BN);
   const int32_t t_end = (int32_t)((int64_t)kt.count * (pl.split + 1) / st.splits);
+  const int32_t t_begin = (int32_t)((int64_t)kt.count * pl.split / st.splits) + wave;
   const int32_t r = min(r0 + l32, R - 1), tok = (int32_t)fast_div((uint32_t)r, a.G_div), pos = st.first + tok;
-  const int32_t head = pl.h * a.G + r - tok * a.G;
-  // half h of the wave holds the elements h * D / 2 + k
   float q[D / 2];
-  const char* qa = a.q + 4 * ((int64_t)b * a.q_b + (int64_t)head * a.q_h + (int64_t)tok * a.q_m + h * (D / 2));
+  const char* qa = a.q + 4 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + r - tok * a.G) * a.q_h + (int64_t)tok * a.q_m + h * (D / 2));
 #pragma unroll
   for (int k = 0; k < D / 2; k += 4) {
     const F32x4 v = *reinterpret_cast<const F32x4*>(qa + 4 * k);
@@ -961,30 +982,44 @@ __global__ __launch_bounds__(64) void k_attend_f32(AttendArgs a) {
   F32x16 o[D / 32];
   float m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int k = 0; k < 16; ++k) o[i][k] = 0.f;
-  bool bad = false;
-  for (int32_t t = (int32_t)((int64_t)kt.count * pl.split / st.splits); t < t_end; ++t) {
-    const int32_t j0 = kt.tile(t) * BN;
+  for (int i = 0; i < D / 32; ++i) o[i] = F32x16{};
+  bool bad = false, special = false;
+  auto row_of = [&](int32_t t) __attribute__((always_inline)) {  // the pool's row of the tile's key l32
     bool x;
-    const int64_t row = pool_row(a.pool, b, (uint32_t)min(j0 + l32, n - 1), &x) + head_row;
+    const int64_t at = pool_row(a.pool, b, (uint32_t)min(kt.tile(t) * BN + l32, n - 1), &x) + head_row;
     bad |= x;
+    return at;
+  };
+  for (int32_t t = t_begin; t < t_end; t += kFewWaves) {
+    const int32_t j0 = kt.tile(t) * BN;
+    const int64_t row = row_of(t);
     const bool full = all_see(j0, j0 + BN, p_lo, p_hi, n, a.window, a.sinks);
     const F32x4* ka = reinterpret_cast<const F32x4*>(a.pool.K + 4 * (row * D + h * (D / 2)));
-    F32x16 s;
+    F32x4 kx[D / 8];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s[k] = 0.f;
+    for (int k = 0; k < D / 8; ++k) kx[k] = ka[k];
+    // V's rows are on their way while the scores are computed (up to D = 128)
+    constexpr bool EARLY = D <= 128;
+    float vx[EARLY ? 16 : 1][D / 32];
+    const auto load_v = [&](int i, float (&v)[D / 32]) __attribute__((always_inline)) {
+      const float* va = reinterpret_cast<const float*>(a.pool.V) + shfl64(row, 8 * (i / 4) + 4 * h + i % 4) * D + l32;
 #pragma unroll
-    for (int k = 0; k < D / 8; ++k) {
-      const F32x4 v = ka[k];
+      for (int db = 0; db < D / 32; ++db) v[db] = va[32 * db];
+    };
+    if constexpr (EARLY)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(v[i], q[4 * k + i], s, 0, 0, 0);
-    }
-    if (!full)
+      for (int i = 0; i < 16; ++i) load_v(i, vx[i]);
+    F32x16 s = {};
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kx[k][i], q[4 * k + i], s, 0, 0, 0);
+    if (!full) {
+      const Limits in(j0 + 4 * h, pos, n, a.window, a.sinks);
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (!sees(j0 + 8 * (i / 4) + 4 * h + i % 4, pos, n, a.window, a.sinks)) s[i] = -INFINITY;
+        if (!in(8 * (i / 4) + i % 4)) s[i] = -INFINITY;
+    }
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
@@ -994,64 +1029,68 @@ __global__ __launch_bounds__(64) void k_attend_f32(AttendArgs a) {
     l *= old;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) o[i] *= old;
-    bool special = false;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int key = 8 * (i / 4) + 4 * h + i % 4;
       const float e = exp2_hw(__builtin_fmaf(s[i], a.c, -shift));
       l += e;
-      const float* va = reinterpret_cast<const float*>(a.pool.V) + shfl64(row, key) * D + l32;
-      const bool some = full || kt.some(j0 + key);
+      if constexpr (!EARLY) load_v(i, vx[0]);
+      float(&v)[D / 32] = vx[EARLY ? i : 0];
+      if (!full) {  // as in the other kernels: nothing of rows that nobody sees, infinities and NaN at the end
+        const bool some = kt.some(j0 + 8 * (i / 4) + 4 * h + i % 4);
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        float v = va[32 * db];
-        if (!full) {
-          if (!some) v = 0.f;
-          else if (!(fabsf(v) < INFINITY)) v = 0.f, special = true;
+        for (int db = 0; db < D / 32; ++db) {
+          if (!some) v[db] = 0.f;
+          if (!(fabsf(v[db]) < INFINITY)) v[db] = 0.f, special = true;
         }
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, e, o[db], 0, 0, 0);
       }
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[db], e, o[db], 0, 0, 0);
     }
-    if (!full && __ballot(special) != 0) {
+  }
+  if (__ballot(special) != 0) {
+#pragma unroll 1
+    for (int32_t t = t_begin; t < t_end; t += kFewWaves) {
+      const int32_t j0 = kt.tile(t) * BN;
+      if (all_see(j0, j0 + BN, p_lo, p_hi, n, a.window, a.sinks)) continue;
+      const int64_t row = row_of(t);
 #pragma unroll 1
       for (int key = 0; key < BN; ++key) {
-        if (!kt.some(j0 + key)) continue;
         const int64_t rv = shfl64(row, key);
+        if (!kt.some(j0 + key)) continue;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const float v = reinterpret_cast<const float*>(a.pool.V)[rv * D + 32 * db + 8 * (i / 4) + 4 * h + i % 4];
-            if (!(fabsf(v) < INFINITY) && sees(j0 + key, pos, n, a.window, a.sinks)) o[db][i] += v;
+            if (!(fabsf(v) < INFINITY) & sees(j0 + key, pos, n, a.window, a.sinks)) o[db][i] += v;
           }
       }
     }
   }
   if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, kDevBadPage);
-  const float sum = lanes_sum<2>(l);
-  if (r0 + l32 >= R) return;
-  const bool parts = st.splits > 1;
-  const float f = parts ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
-  float* at = parts ? a.part + ((int64_t)pl.slot * 32 + l32) * D
-                    : reinterpret_cast<float*>(a.out) + (int64_t)b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m;
+
+  l = lanes_sum<2>(l);
+  if (h == 0) lds_ml[wave][l32][0] = m, lds_ml[wave][l32][1] = l;
+  __syncthreads();
+  float top = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, lds_ml[w][l32][0]);
+  const float f = exp2_hw(m - shift_of(top));
+  float* mine = reinterpret_cast<float*>(lds[wave]) + l32 * JoinLds<D, 32>::STRIDE;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<F32x4*>(at + 32 * db + 8 * i + 4 * h) =
+      *reinterpret_cast<F32x4*>(mine + 32 * db + 8 * i + 4 * h) =
           F32x4{o[db][4 * i] * f, o[db][4 * i + 1] * f, o[db][4 * i + 2] * f, o[db][4 * i + 3] * f};
-  if (h != 0) return;
-  if (parts) {
-    a.part_ml[((int64_t)pl.slot * 32 + l32) * 2] = m, a.part_ml[((int64_t)pl.slot * 32 + l32) * 2 + 1] = sum;
-  } else if (a.lse) {
-    a.lse[((int64_t)b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (m + log2_hw(sum)) * kLn2;
-  }
+  __syncthreads();
+  join_parts<D, 32, true>(a, st, pl, b, r0, min(R - r0, 32), lds, lds_ml, &lds_last);
 }
 
-// ---------------------------------------------------------------- joining splits
+// ---------------------------------------------------------------- joining splits of many rows
 // One wave a row: lane s has split s's maximum and sum, then every lane a part
 // of the row's elements over the splits in order.
-template <int D, bool F32OUT>
+template <int D>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int32_t BM) {
   const AttendStream st = a.s[blockIdx.y];
   if (st.splits <= 1) return;
@@ -1094,10 +1133,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int32_t BM) {
   const int64_t b = a.b0 + blockIdx.y, at = b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m + lane * E;
   if (lane * E < D) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if (F32OUT) reinterpret_cast<float*>(a.out)[at + e] = v[e] * inv;
-      else reinterpret_cast<__bf16*>(a.out)[at + e] = (__bf16)(v[e] * inv);
-    }
+    for (int e = 0; e < E; ++e) reinterpret_cast<__bf16*>(a.out)[at + e] = (__bf16)(v[e] * inv);
   }
   if (lane == 0 && a.lse)
     a.lse[(b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (top + log2_hw(sum)) * kLn2;
@@ -1108,7 +1144,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int32_t BM) {
 enum AttendKind { kFew1, kFew2, kTile, kF32 };
 template <int F>
 hipError_t launch_attend(int D, AttendKind kind, uint32_t grid, const AttendArgs& a, hipStream_t st);
-hipError_t launch_join(int D, bool f32, uint32_t rows, int32_t BM, const AttendArgs& a, hipStream_t st);
+hipError_t launch_join(int D, uint32_t rows, int32_t BM, const AttendArgs& a, hipStream_t st);
 inline int attend_rows(AttendKind k, int D) { return k == kFew1 ? 16 : k == kFew2 || k == kF32 ? 32 : 32 * tile_waves(D); }
 inline int attend_keys(AttendKind k) { return k == kTile ? kTileKeys : 32; }
 

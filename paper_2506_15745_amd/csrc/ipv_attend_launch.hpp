@@ -8,7 +8,7 @@ namespace ipv {
 template <int F, int D>
 hipError_t launch_attend_d(AttendKind kind, uint32_t grid, const AttendArgs& a, hipStream_t st) {
   if constexpr (F == kFmtF32) {
-    k_attend_f32<D><<<dim3(grid), dim3(64), 0, st>>>(a);
+    k_attend_f32<D><<<dim3(grid), dim3(64 * kFewWaves), 0, st>>>(a);
   } else {
     if (kind == kFew1) k_attend_few<F, D, 1><<<dim3(grid), dim3(64 * kFewWaves), 0, st>>>(a);
     else if (kind == kFew2) k_attend_few<F, D, 2><<<dim3(grid), dim3(64 * kFewWaves), 0, st>>>(a);

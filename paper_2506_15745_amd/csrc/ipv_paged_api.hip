@@ -166,7 +166,7 @@ ipv_status page_rows(const ipv_page_shape* s, const void* K_pages, const void* V
 // Workgroups that the card's 256 CUs hold at once: with fewer row tiles than that,
 // key ranges are split.
 int32_t attend_fill(AttendKind k, int D, int format) {
-  return 256 * (k == kTile ? 1 : k == kF32 ? 4 : few_per_cu(format, D, k == kFew1 ? 1 : 2));
+  return 256 * (k == kTile ? 1 : k == kF32 ? (D <= 64 ? 2 : 1) : few_per_cu(format, D, k == kFew1 ? 1 : 2));
 }
 constexpr int32_t kMaxParts = 1024;  // workgroups of a launch that splits, at most
 
@@ -190,7 +190,7 @@ ipv_status check_heads(const ipv_page_shape* s, int32_t streams, int32_t q_heads
 // workgroups as it holds (few: at least a tile for each wave).
 void plan(AttendArgs* a, AttendKind kind, int D, int format) {
   const int32_t BM = attend_rows(kind, D), BN = attend_keys(kind);
-  const bool few = kind == kFew1 || kind == kFew2;
+  const bool few = kind != kTile;  // waves share a workgroup's keys
   int64_t base = 0, work = 0;
   int32_t count[kAttendStreams];
   for (int32_t i = 0; i < a->streams; ++i) {
@@ -226,21 +226,15 @@ void plan(AttendArgs* a, AttendKind kind, int D, int format) {
   a->blocks = (int32_t)at;
 }
 
-template <int D>
-void join_launch(bool f32, dim3 grid, int32_t BM, const AttendArgs& a, hipStream_t st) {
-  if (f32) k_attend_join<D, true><<<grid, dim3(256), 0, st>>>(a, BM);
-  else k_attend_join<D, false><<<grid, dim3(256), 0, st>>>(a, BM);
-}
-
 }  // namespace
 
-hipError_t ipv::launch_join(int D, bool f32, uint32_t rows, int32_t BM, const AttendArgs& a, hipStream_t st) {
-  const dim3 grid((rows + 3) / 4, (uint32_t)a.streams);
+hipError_t ipv::launch_join(int D, uint32_t rows, int32_t BM, const AttendArgs& a, hipStream_t st) {
+  const dim3 grid((rows + 3) / 4, (uint32_t)a.streams), block(256);
   switch (D) {
-    case 32: join_launch<32>(f32, grid, BM, a, st); break;
-    case 64: join_launch<64>(f32, grid, BM, a, st); break;
-    case 128: join_launch<128>(f32, grid, BM, a, st); break;
-    default: join_launch<256>(f32, grid, BM, a, st); break;
+    case 32: k_attend_join<32><<<grid, block, 0, st>>>(a, BM); break;
+    case 64: k_attend_join<64><<<grid, block, 0, st>>>(a, BM); break;
+    case 128: k_attend_join<128><<<grid, block, 0, st>>>(a, BM); break;
+    default: k_attend_join<256><<<grid, block, 0, st>>>(a, BM); break;
   }
   return hipGetLastError();
 }
@@ -342,11 +336,10 @@ ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const voi
       default: e = launch_attend<kFmtFp4>(pool->head_dim, kind, grid, a, st); break;
     }
     IPV_TRY(launched(e));
-    bool split = false;  // the kernel of few rows joins its parts itself
+    if (kind != kTile) continue;  // the others join their parts themselves
+    bool split = false;
     for (int32_t i = 0; i < a.streams; ++i) split |= a.s[i].splits > 1;
-    if (split && (kind == kTile || kind == kF32))
-      IPV_TRY(launched(launch_join(pool->head_dim, pool->format == IPV_PAGES_F32, (uint32_t)most * (uint32_t)q_heads,
-                                   attend_rows(kind, pool->head_dim), a, st)));
+    if (split) IPV_TRY(launched(launch_join(pool->head_dim, (uint32_t)most * (uint32_t)q_heads, attend_rows(kind, pool->head_dim), a, st)));
   }
   return IPV_OK;
 }

@@ -22,6 +22,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+from array import array
 
 import torch
 
@@ -546,13 +547,16 @@ class PagePool:
         return cls(*(torch.zeros(rows + (w,), dtype=torch.uint8, device=device) for w in width))
 
 
-def _counts_ptr(values, streams, what):
-    """(address, keeper) of a host array with one count per stream, from an int or a sequence."""
+# What these calls cost on the host is their checks and conversions: counts go through
+# array (a third of a ctypes array's time), stride arrays are kept by value, and a
+# pool's own arguments are made with it.
+def _host_counts(values, streams, what):
+    """A host array with one count per stream, from an int or a sequence."""
     if isinstance(values, int):
-        values = (values,) * streams
-    elif len(values) != streams:
+        return array("i", (values,) * streams)
+    if len(values) != streams:
         raise IpvError(ERR_SHAPE, "%s needs one count per stream (%d)" % (what, streams))
-    return (ctypes.c_int32 * streams)(*values)
+    return array("i", values)
 
 
 def _table(pool, table, streams):
@@ -566,12 +570,16 @@ def _table(pool, table, streams):
     return _ptr(table), table.shape[1]
 
 
-def _strides(what, t, dims):
+@functools.lru_cache(maxsize=256)
+def _stride_array(strides, sizes):
+    if strides[-1] != 1:
+        raise IpvError(ERR_SHAPE, "the last dimension of rows and queries must be contiguous")
+    return (ctypes.c_int64 * (len(sizes) - 1))(*[st if n > 1 else 0 for st, n in zip(strides[:-1], sizes)])
+
+
+def _strides(t):
     """Strides (elements) of all but the last dimension, which must be contiguous; 0 for a dimension of one."""
-    st, sh = t.stride(), t.shape
-    if st[-1] != 1:
-        raise IpvError(ERR_SHAPE, "%s's last dimension must be contiguous" % what)
-    return (ctypes.c_int64 * dims)(*[st[i] if sh[i] > 1 else 0 for i in range(dims)])
+    return _stride_array(t.stride(), t.shape)
 
 
 def _same_gpu(pool, ws, **tensors):
@@ -608,8 +616,8 @@ def _page_rows(name, pool, page_table, first_row, K, V, ws, rows, first_layer, r
     if V.dtype != K.dtype:
         raise IpvError(ERR_DTYPE, "K and V must have one dtype")
     B, L, _, N, D = K.shape
-    st = _strides("K", K, 4)
-    if V.stride() != K.stride() and list(_strides("V", V, 4)) != list(st):
+    st = _strides(K)
+    if V.stride() != K.stride() and list(_strides(V)) != list(st):
         raise IpvError(ERR_SHAPE, "K and V must have the same strides")
     if isinstance(rows, int) or rows is None:
         rows = N if rows is None else rows
@@ -622,9 +630,9 @@ def _page_rows(name, pool, page_table, first_row, K, V, ws, rows, first_layer, r
         raise IpvError(ERR_SHAPE, "rotary must be fp32 [positions, %d, 2]" % (D // 2))
     table, cols = _table(pool, page_table, B)
     _same_gpu(pool, ws, K=K, V=V, rotary=rotary)
-    first, rows = _counts_ptr(first_row, B, "first_row"), _counts_ptr(rows, B, "rows")
-    _check(getattr(_paged(), name)(*pool._args, table, cols, B, first, rows, first_layer, L, K.data_ptr(), V.data_ptr(),
-                                   _dtype_code(K), st, None if rotary is None else _ptr(rotary),
+    first, rows = _host_counts(first_row, B, "first_row"), _host_counts(rows, B, "rows")
+    _check(getattr(_paged(), name)(*pool._args, table, cols, B, first.buffer_info()[0], rows.buffer_info()[0], first_layer, L,
+                                   K.data_ptr(), V.data_ptr(), _dtype_code(K), st, None if rotary is None else _ptr(rotary),
                                    0 if rotary is None else rotary.shape[0], _ptr(ws), _ws_bytes(ws), _stream(stream)), name)
 
 
@@ -661,10 +669,11 @@ def ipv_attend(pool, page_table, n_tokens, q_first, layer, q, out, ws, q_rows=No
         _expect("lse", lse, (B, A, M), torch.float32, pool.device)
     table, cols = _table(pool, page_table, B)
     _same_gpu(pool, ws, q=q, out=out)
-    n, first = _counts_ptr(n_tokens, B, "n_tokens"), _counts_ptr(q_first, B, "q_first")
-    _check(_paged().ipv_attend(*pool._args, table, cols, B, n, first, _counts_ptr(M if q_rows is None else q_rows, B, "q_rows"),
-                               layer, q.data_ptr(), _strides("q", q, 3), A, M, D ** -0.5 if scale is None else scale, window,
-                               sinks, out.data_ptr(), _strides("out", out, 3), _ptr(lse), _ptr(ws), _ws_bytes(ws),
+    n, first = _host_counts(n_tokens, B, "n_tokens"), _host_counts(q_first, B, "q_first")
+    rows = _host_counts(M if q_rows is None else q_rows, B, "q_rows")
+    _check(_paged().ipv_attend(*pool._args, table, cols, B, n.buffer_info()[0], first.buffer_info()[0], rows.buffer_info()[0],
+                               layer, q.data_ptr(), _strides(q), A, M, D ** -0.5 if scale is None else scale, window, sinks,
+                               out.data_ptr(), _strides(out), None if lse is None else _ptr(lse), _ptr(ws), _ws_bytes(ws),
                                _stream(stream)), "ipv_attend")
 
 
