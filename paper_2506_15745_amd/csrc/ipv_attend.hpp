@@ -126,6 +126,16 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Maximum and sum over the wave, in all lanes.
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, dpp_f32<kDppXor1>(v));
+  v = fmaxf(v, dpp_f32<kDppXor2>(v));
+  v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
+  v = fmaxf(v, dpp_f32<kDppRowMirror>(v));
+  return lanes_max<4>(v);
+}
+__device__ __forceinline__ float wave_sum(float v) { return lanes_sum<4>(group_sum<16>(v)); }
+
 __device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
   const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)v, lane, kWave);
   const uint32_t hi = (uint32_t)__shfl((int)(uint32_t)((uint64_t)v >> 32), lane, kWave);
@@ -202,12 +212,19 @@ __device__ __forceinline__ bool clean(uint32_t (&x)[4], uint64_t& scales, int bl
 }
 
 // Parts that another workgroup, maybe on another XCD, will read: stored and loaded
-// past this XCD's L2.
-__device__ __forceinline__ void store_part(float* p, float a, float b) {
+// past this XCD's L2 (the cache policy of agent scope), 16 and 8 bytes at a time.
+constexpr int kAgentScope = 16;  // the sc1 bit of a buffer instruction
+__device__ __forceinline__ void store_part(__amdgpu_buffer_rsrc_t parts, uint32_t offset, const F32x4& v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(U32x4, v), parts, (int)offset, 0, kAgentScope);
+}
+__device__ __forceinline__ F32x4 load_part(__amdgpu_buffer_rsrc_t parts, uint32_t offset) {
+  return __builtin_bit_cast(F32x4, __builtin_amdgcn_raw_buffer_load_b128(parts, (int)offset, 0, kAgentScope));
+}
+__device__ __forceinline__ void store_pair(float* p, float a, float b) {
   const uint64_t v = ((uint64_t)__float_as_uint(b) << 32) | __float_as_uint(a);
   __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ void load_part(const float* p, float& a, float& b) {
+__device__ __forceinline__ void load_pair(const float* p, float& a, float& b) {
   const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   a = __uint_as_float((uint32_t)v), b = __uint_as_float((uint32_t)(v >> 32));
 }
@@ -323,6 +340,8 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendStre
   constexpr int STRIDE = JoinLds<D, NR>::STRIDE;
   static_assert(BYTES >= JoinLds<D, NR>::kWaveBytes && kFewWaves * BYTES >= sizeof(float) * NR * kMaxSplits, "LDS of the joining");
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  // the row tile's parts, [part][row][D]
+  const __amdgpu_buffer_rsrc_t parts = buffer_rsrc(a.part + (int64_t)pl.first * NR * D, (uint32_t)(st.splits * NR * D * 4));
   for (int x = threadIdx.x; x < rows * (D / 4); x += 64 * kFewWaves) {
     const int r = x / (D / 4), d = x % (D / 4) * 4;
     float top = -INFINITY, sum = 0.f;
@@ -335,10 +354,8 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendStre
       v += *reinterpret_cast<const F32x4*>(reinterpret_cast<const float*>(lds[w]) + r * STRIDE + d);
     }
     if (st.splits > 1) {
-      float* at = a.part + ((int64_t)pl.slot * NR + r) * D + d;
-      store_part(at, v[0], v[1]);
-      store_part(at + 2, v[2], v[3]);
-      if (d == 0) store_part(a.part_ml + ((int64_t)pl.slot * NR + r) * 2, top, sum);
+      store_part(parts, (uint32_t)((pl.split * NR + r) * D + d) * 4, v);
+      if (d == 0) store_pair(a.part_ml + ((int64_t)pl.slot * NR + r) * 2, top, sum);
     } else {
       row_out<D, F32OUT>(a, b, pl.h, r0 + r, d, v, top, sum);
     }
@@ -355,37 +372,38 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendStre
   }
   __syncthreads();
   if (!*lds_last) return;
+  // Each thread has four elements of a row and takes 16 parts at a time, the first
+  // ones on their way while the parts' weights are made (a trip to another XCD's
+  // data takes over a microsecond).
+  constexpr int ROUND = 16;
+  F32x4 y[ROUND];
+  const auto load_round = [&](int x, int k0) __attribute__((always_inline)) {
+    const uint32_t at = (uint32_t)(min(x / (D / 4), rows - 1) * D + x % (D / 4) * 4) * 4;
+#pragma unroll
+    for (int k = 0; k < ROUND; ++k) y[k] = load_part(parts, at + (uint32_t)((k0 + k) * NR * D * 4));  // (zeros past the last)
+  };
+  load_round(threadIdx.x, 0);
   // weights of the parts, by row: lane s has part s
   float(*weight)[kMaxSplits] = reinterpret_cast<float(*)[kMaxSplits]>(&lds[0][0]);
   for (int r = wave; r < rows; r += kFewWaves) {
     float pm = -INFINITY, ps = 0.f;
-    if (lane < st.splits) load_part(a.part_ml + ((int64_t)(pl.first + lane) * NR + r) * 2, pm, ps);
-    float top = pm;
-#pragma unroll
-    for (int k = 1; k < kWave; k *= 2) top = fmaxf(top, __shfl_xor(top, k, kWave));
-    const float f = exp2_hw(pm - shift_of(top));
-    float sum = ps * f;
-#pragma unroll
-    for (int k = 1; k < kWave; k *= 2) sum += __shfl_xor(sum, k, kWave);
+    if (lane < st.splits) load_pair(a.part_ml + ((int64_t)(pl.first + lane) * NR + r) * 2, pm, ps);
+    const float top = wave_max(pm), f = exp2_hw(pm - shift_of(top)), sum = wave_sum(ps * f);
     weight[r][lane] = f;
     if (lane == 0) lds_ml[0][r][0] = top, lds_ml[0][r][1] = sum;
   }
   __syncthreads();
   for (int x = threadIdx.x; x < rows * (D / 4); x += 64 * kFewWaves) {
     const int r = x / (D / 4), d = x % (D / 4) * 4;
-    const float* at = a.part + ((int64_t)pl.first * NR + r) * D + d;
+    if (x != (int)threadIdx.x) load_round(x, 0);
     F32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < st.splits; k0 += 8) {
-      float y[8][4];
+    for (int k0 = 0;;) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {  // the last again past the last, with no weight
-        const float* from = at + (int64_t)min(k0 + k, st.splits - 1) * NR * D;
-        load_part(from, y[k][0], y[k][1]);
-        load_part(from + 2, y[k][2], y[k][3]);
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k0 + k < st.splits) v += F32x4{y[k][0], y[k][1], y[k][2], y[k][3]} * weight[r][k0 + k];
+      for (int k = 0; k < ROUND; ++k)
+        if (k0 + k < st.splits) v += y[k] * weight[r][k0 + k];
+      k0 += ROUND;
+      if (k0 >= st.splits) break;
+      load_round(x, k0);
     }
     row_out<D, F32OUT>(a, b, pl.h, r0 + r, d, v, lds_ml[0][r][0], lds_ml[0][r][1]);
   }

@@ -206,8 +206,11 @@ void plan(AttendArgs* a, AttendKind kind, int D, int format) {
   const int32_t fill = attend_fill(kind, D, format);
   if (base < fill) {
     // parts of `per` tiles: the shortest that make no more workgroups than fit at once
+    // (waves that share a workgroup's keys: and no shorter than a square root of the range, where a
+    // step of four tiles, 0.65 us, costs what the parts it saves cost the last workgroup, 0.1 us each)
     const int64_t unit = few ? kFewWaves : 1;
-    int64_t per = std::max<int64_t>((work + fill - 1) / fill, few ? kFewWaves : 2);
+    const int64_t least = few ? std::max<int64_t>(kFewWaves, (int64_t)std::sqrt(0.6 * *std::max_element(count, count + a->streams))) : 2;
+    int64_t per = std::max<int64_t>((work + fill - 1) / fill, least);
     per = (per + unit - 1) / unit * unit;
     for (;; per += std::max(unit, per / 16 / unit * unit)) {
       int64_t blocks = 0;

@@ -531,6 +531,7 @@ class PagePool:
         self.format, self.head_dim, self.device = fmt, D, K.device
         self.dtype = torch.float32 if fmt == PAGES_F32 else torch.bfloat16  # of queries and outputs
         self.shape = PageShape(P, L, H, T, D, fmt)
+        self._dev = K.get_device()
         self._args = (ctypes.byref(self.shape), _ptr(K), _ptr(V), _ptr(K_scales), _ptr(V_scales))
 
     @classmethod
@@ -572,14 +573,10 @@ def _table(pool, table, streams):
 
 @functools.lru_cache(maxsize=256)
 def _stride_array(strides, sizes):
+    """Strides (elements) of all but the last dimension, which must be contiguous; 0 for a dimension of one."""
     if strides[-1] != 1:
         raise IpvError(ERR_SHAPE, "the last dimension of rows and queries must be contiguous")
     return (ctypes.c_int64 * (len(sizes) - 1))(*[st if n > 1 else 0 for st, n in zip(strides[:-1], sizes)])
-
-
-def _strides(t):
-    """Strides (elements) of all but the last dimension, which must be contiguous; 0 for a dimension of one."""
-    return _stride_array(t.stride(), t.shape)
 
 
 def _same_gpu(pool, ws, **tensors):
@@ -611,29 +608,34 @@ def alloc_attend_workspace(pool: PagePool, streams: int, q_heads: int, max_rows:
 
 
 def _page_rows(name, pool, page_table, first_row, K, V, ws, rows, first_layer, rotary, stream):
-    if K.dim() != 5 or V.shape != K.shape or K.shape[2] != pool.shape.kv_heads or K.shape[4] != pool.head_dim:
+    shape, dev, table, cols, angles = K.shape, pool._dev, None, 1, 0
+    if len(shape) != 5 or V.shape != shape or shape[2] != pool.shape.kv_heads or shape[4] != pool.head_dim:
         raise IpvError(ERR_SHAPE, "K and V must be [B, layers, %d, rows, %d]" % (pool.shape.kv_heads, pool.head_dim))
-    if V.dtype != K.dtype:
+    if V.dtype is not K.dtype:
         raise IpvError(ERR_DTYPE, "K and V must have one dtype")
-    B, L, _, N, D = K.shape
-    st = _strides(K)
-    if V.stride() != K.stride() and list(_strides(V)) != list(st):
+    B, L, _, N, D = shape
+    strides = _stride_array(K.stride(), shape)
+    if V.stride() != K.stride() and list(_stride_array(V.stride(), shape)) != list(strides):
         raise IpvError(ERR_SHAPE, "K and V must have the same strides")
-    if isinstance(rows, int) or rows is None:
-        rows = N if rows is None else rows
-        longest = rows
-    else:
-        longest = max(rows)
-    if longest > N:
-        raise IpvError(ERR_SHAPE, "%d rows of a tensor of %d" % (longest, N))
-    if rotary is not None and (rotary.dtype != torch.float32 or rotary.dim() != 3 or tuple(rotary.shape[1:]) != (D // 2, 2)):
-        raise IpvError(ERR_SHAPE, "rotary must be fp32 [positions, %d, 2]" % (D // 2))
-    table, cols = _table(pool, page_table, B)
-    _same_gpu(pool, ws, K=K, V=V, rotary=rotary)
-    first, rows = _host_counts(first_row, B, "first_row"), _host_counts(rows, B, "rows")
-    _check(getattr(_paged(), name)(*pool._args, table, cols, B, first.buffer_info()[0], rows.buffer_info()[0], first_layer, L,
-                                   K.data_ptr(), V.data_ptr(), _dtype_code(K), st, None if rotary is None else _ptr(rotary),
-                                   0 if rotary is None else rotary.shape[0], _ptr(ws), _ws_bytes(ws), _stream(stream)), name)
+    if rows is None:
+        rows = N
+    elif (rows if isinstance(rows, int) else max(rows, default=0)) > N:
+        raise IpvError(ERR_SHAPE, "more rows than the tensor's %d" % N)
+    if rotary is not None:
+        if rotary.dtype is not torch.float32 or rotary.dim() != 3 or tuple(rotary.shape[1:]) != (D // 2, 2):
+            raise IpvError(ERR_SHAPE, "rotary must be fp32 [positions, %d, 2]" % (D // 2))
+        angles = rotary.shape[0]
+    if page_table is not None:
+        table, cols = _table(pool, page_table, B)
+    if ws is None or ws.get_device() != dev or K.get_device() != dev or V.get_device() != dev or \
+            (rotary is not None and rotary.get_device() != dev):
+        _same_gpu(pool, ws, K=K, V=V, rotary=rotary)
+    first, counts_ = _host_counts(first_row, B, "first_row"), _host_counts(rows, B, "rows")
+    rc = getattr(_paged(), name)(*pool._args, table, cols, B, first.buffer_info()[0], counts_.buffer_info()[0], first_layer, L,
+                                 K.data_ptr(), V.data_ptr(), _dtype_code(K), strides,
+                                 None if rotary is None else _ptr(rotary), angles, _ptr(ws), _ws_bytes(ws), _stream(stream))
+    if rc != OK:
+        _check(rc, name)
 
 
 def ipv_page_write(pool, page_table, first_row, K, V, ws, rows=None, first_layer=0, rotary=None, stream=None):
@@ -658,23 +660,29 @@ def ipv_attend(pool, page_table, n_tokens, q_first, layer, q, out, ws, q_rows=No
     window only the last `window` of them and the first `sinks` rows. scale:
     1 / sqrt(D) if None. q_rows: queries of each stream (M if None). lse: fp32
     [B, q_heads, M] that receives the logarithm of each softmax's sum, or None."""
-    if q.dim() != 4 or q.shape[3] != pool.head_dim:
+    shape, dev, table, cols = q.shape, pool._dev, None, 1
+    if len(shape) != 4 or shape[3] != pool.head_dim:
         raise IpvError(ERR_SHAPE, "q must be [B, q_heads, rows, %d]" % pool.head_dim)
-    if q.dtype != pool.dtype or out.dtype != pool.dtype:
+    if q.dtype is not pool.dtype or out.dtype is not pool.dtype:
         raise IpvError(ERR_DTYPE, "q and out must be %s" % pool.dtype)
-    if out.shape != q.shape:
+    if out.shape != shape:
         raise IpvError(ERR_SHAPE, "out must have q's shape")
-    B, A, M, D = q.shape
+    B, A, M, D = shape
     if lse is not None:
         _expect("lse", lse, (B, A, M), torch.float32, pool.device)
-    table, cols = _table(pool, page_table, B)
-    _same_gpu(pool, ws, q=q, out=out)
+    if page_table is not None:
+        table, cols = _table(pool, page_table, B)
+    if ws is None or ws.get_device() != dev or q.get_device() != dev or out.get_device() != dev:
+        _same_gpu(pool, ws, q=q, out=out)
     n, first = _host_counts(n_tokens, B, "n_tokens"), _host_counts(q_first, B, "q_first")
     rows = _host_counts(M if q_rows is None else q_rows, B, "q_rows")
-    _check(_paged().ipv_attend(*pool._args, table, cols, B, n.buffer_info()[0], first.buffer_info()[0], rows.buffer_info()[0],
-                               layer, q.data_ptr(), _strides(q), A, M, D ** -0.5 if scale is None else scale, window, sinks,
-                               out.data_ptr(), _strides(out), None if lse is None else _ptr(lse), _ptr(ws), _ws_bytes(ws),
-                               _stream(stream)), "ipv_attend")
+    rc = _paged().ipv_attend(*pool._args, table, cols, B, n.buffer_info()[0], first.buffer_info()[0], rows.buffer_info()[0],
+                             layer, q.data_ptr(), _stride_array(q.stride(), shape), A, M,
+                             D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(),
+                             _stride_array(out.stride(), shape), None if lse is None else _ptr(lse), _ptr(ws), _ws_bytes(ws),
+                             _stream(stream))
+    if rc != OK:
+        _check(rc, "ipv_attend")
 
 
 class Compressor:
