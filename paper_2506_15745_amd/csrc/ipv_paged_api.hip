@@ -91,8 +91,7 @@ hipError_t page_launch(const PageCall& c, dim3 grid, hipStream_t st) {
 template <bool WRITE, int F, int X>
 hipError_t page_launch_d(int D, const PageCall& c, int32_t rows, hipStream_t st, int32_t streams) {
   const int per = kPageThreads / (D / 16);
-  const int64_t items = (int64_t)rows * ((c.LH + kPageSlices - 1) / kPageSlices);
-  const dim3 grid((uint32_t)((items + per - 1) / per), 2, (uint32_t)streams);
+  const dim3 grid((uint32_t)((rows + per - 1) / per), (uint32_t)(2 * ((c.LH + kPageSlices - 1) / kPageSlices)), (uint32_t)streams);
   switch (D) {
     case 32: return page_launch<WRITE, F, X, 32>(c, grid, st);
     case 64: return page_launch<WRITE, F, X, 64>(c, grid, st);
@@ -122,13 +121,12 @@ ipv_status page_rows(const ipv_page_shape* s, const void* K_pages, const void* V
   IPV_TRY(check_strides(strides, 4));
   if (first_layer < 0 || layers < 1 || layers > s->layers - first_layer) return IPV_ERR_SHAPE;
   const int64_t slices = (int64_t)layers * s->kv_heads, groups = (slices + kPageSlices - 1) / kPageSlices;
-  if (slices > kMaxPosition) return IPV_ERR_SHAPE;
+  if (2 * groups > 65535) return IPV_ERR_SHAPE;  // a grid's second dimension
   for (int32_t b = 0; b < streams; ++b) {
     if (rows[b] < 0 || first[b] < 0) return IPV_ERR_SHAPE;
     const int64_t end = (int64_t)first[b] + rows[b];
     if (rows[b] > 0 && end > table_rows(s, cols)) return IPV_ERR_SHAPE;
     if (rows[b] > 0 && rotary && end > rotary_rows) return IPV_ERR_ARG;
-    if (rows[b] * groups > kMaxPosition) return IPV_ERR_SHAPE;
   }
   IPV_TRY(check_word(ws, ws_bytes, kWsHeader));
   c.K = static_cast<char*>(const_cast<void*>(K));
