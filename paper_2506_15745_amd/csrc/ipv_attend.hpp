@@ -642,6 +642,16 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
 constexpr int kTileKeys = 64;
 __host__ __device__ constexpr int tile_waves(int D) { return D <= 128 ? 8 : 4; }
 
+// Sixteen bytes a lane from memory straight into LDS: lane i's to `at` + 16 i, `at` the
+// same in all lanes. No register waits for them: copies_done() does, for all of the wave's.
+__device__ __forceinline__ void copy_to_lds(const char* from, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const char* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+
 template <int F, int D, int W>
 struct TileCfg {
   static constexpr int RB = fmt_row_bytes(F, D);
@@ -663,7 +673,11 @@ template <int F, int D>
 __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_attend_tile(AttendArgs a) {
   constexpr int W = tile_waves(D), BM = 32 * W, BN = kTileKeys;
   using C = TileCfg<F, D, W>;
-  __shared__ __attribute__((aligned(16))) char ldsK[2][BN * D * 2];
+  // bf16 rows are copied straight into LDS; the others pass through registers, as bf16
+  constexpr bool COPY = F == kFmtBf16;
+  // K is staged two tiles ahead of its use where there is room, V one
+  constexpr int KAHEAD = COPY && D <= 128 ? 1 : 1, KBUF = 2 * KAHEAD;
+  __shared__ __attribute__((aligned(16))) char ldsK[KBUF][BN * D * 2];
   __shared__ __attribute__((aligned(16))) char ldsV[2][BN * D * 2];
   __shared__ int32_t lds_special;
   const Place pl = place_of(a);
@@ -709,17 +723,19 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
     bad |= x;
     return r;
   };
-  // rows on their way to LDS (D = 256 has no registers for both: V's are fetched when K's are there)
-  constexpr bool BOTH = D <= 128;
-  uint32_t kr[C::NL][4], vx[BOTH ? C::NL : 1][4];
-  uint64_t ks[C::NL], vsx[BOTH ? C::NL : 1];
+  // rows on their way through registers (D = 256 has none for both: V's are fetched when K's are there)
+  constexpr bool BOTH = COPY || D <= 128;
+  constexpr int NK = COPY ? 1 : C::NL, NV = COPY || !BOTH ? 1 : C::NL;
+  uint32_t kr[NK][4], vx[NV][4];
+  uint64_t ks[NK], vsx[NV];
   auto& vr = [&]() -> auto& { if constexpr (BOTH) return vx; else return kr; }();
   auto& vs = [&]() -> auto& { if constexpr (BOTH) return vsx; else return ks; }();
   // this thread's chunks: column threadIdx.x % CPR of rows key0 + i * 64 W / CPR
   const int key0 = threadIdx.x / C::CPR % BN;
   constexpr int STEP = 64 * W / C::CPR;
-  auto load_tile = [&](const char* pages, const uint8_t* scales, int64_t row, uint32_t (&x)[C::NL][4], uint64_t (&xs)[C::NL]) __attribute__((always_inline)) {
-    int64_t r[C::NL];
+  const int col = threadIdx.x % C::CPR, block = col * C::E / kScaleBlock;
+  const bool mine = C::CHUNKS >= 64 * W || (int)threadIdx.x < C::CHUNKS;  // (whole waves)
+  const auto tile_rows = [&](int64_t row, int64_t (&r)[C::NL]) __attribute__((always_inline)) {
     if (whole) {
 #pragma unroll
       for (int i = 0; i < C::NL; ++i) r[i] = row + (key0 + i * STEP);
@@ -727,48 +743,90 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
 #pragma unroll
       for (int i = 0; i < C::NL; ++i) r[i] = shfl64(row, key0 + i * STEP);
     }
+  };
+  // fetch: rows of a tile set out; stage: they are in LDS buffer `buf` when it is done
+  // (copied rows set out with their buffer known; the source column makes up for the place)
+  const auto fetch_k = [&](int64_t row, int buf) __attribute__((always_inline)) {
+    int64_t r[C::NL];
+    tile_rows(row, r);
+    if constexpr (COPY) {
+      const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(ldsK[buf]) + wave * 1024);
 #pragma unroll
-    for (int i = 0; i < C::NL; ++i) {
-      load_piece<16>(pages + r[i] * C::RB + threadIdx.x % C::CPR * 16, x[i]);
-      if (fmt_scaled(F)) xs[i] = load_scales<D>(scales, r[i]);
+      for (int i = 0; i < C::NL; ++i)
+        if (mine) copy_to_lds(a.pool.K + r[i] * C::RB + 16 * (col ^ C::kswz(key0 + i * STEP)), at + i * 1024 * W);
+    } else {
+#pragma unroll
+      for (int i = 0; i < C::NL; ++i) {
+        load_piece<16>(a.pool.K + r[i] * C::RB + col * 16, kr[i]);
+        if (fmt_scaled(F)) ks[i] = load_scales<D>(a.pool.Ks, r[i]);
+      }
     }
   };
-  auto fetch_k = [&](int64_t row) __attribute__((always_inline)) { load_tile(a.pool.K, a.pool.Ks, row, kr, ks); };
-  auto fetch_v = [&](int64_t row) __attribute__((always_inline)) { load_tile(a.pool.V, a.pool.Vs, row, vr, vs); };
-  const int col = threadIdx.x % C::CPR, block = col * C::E / kScaleBlock;
-  const bool mine = C::CHUNKS >= 64 * W || (int)threadIdx.x < C::CHUNKS;
-  auto stage_k = [&](int buf) __attribute__((always_inline)) {
-    if (!mine) return;
+  const auto fetch_v = [&](int64_t row, int buf) __attribute__((always_inline)) {
+    int64_t r[C::NL];
+    tile_rows(row, r);
+    if constexpr (COPY) {
+      const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(ldsV[buf]) + wave * 1024);
 #pragma unroll
-    for (int i = 0; i < C::NL; ++i) {
-      const int key = key0 + i * STEP;
+      for (int i = 0; i < C::NL; ++i)
+        if (mine) copy_to_lds(a.pool.V + r[i] * C::RB + 16 * (col ^ C::vswz(key0 + i * STEP)), at + i * 1024 * W);
+    } else {
 #pragma unroll
-      for (int e = 0; e < C::E / 8; ++e)
-        *reinterpret_cast<Raw16*>(ldsK[buf] + key * (D * 2) + 16 * ((col * (C::E / 8) + e) ^ C::kswz(key))) =
-            piece8<F>(kr[i], e, fmt_scaled(F) ? scale_at(ks[i], block) : 0.f);
+      for (int i = 0; i < C::NL; ++i) {
+        load_piece<16>(a.pool.V + r[i] * C::RB + col * 16, vr[i]);
+        if (fmt_scaled(F)) vs[i] = load_scales<D>(a.pool.Vs, r[i]);
+      }
     }
   };
-  auto stage_v = [&](int32_t tt, int buf) __attribute__((always_inline)) {
+  const auto stage_k = [&](int buf) __attribute__((always_inline)) {
+    if constexpr (!COPY) {
+      if (!mine) return;
+#pragma unroll
+      for (int i = 0; i < C::NL; ++i) {
+        const int key = key0 + i * STEP;
+#pragma unroll
+        for (int e = 0; e < C::E / 8; ++e)
+          *reinterpret_cast<Raw16*>(ldsK[buf] + key * (D * 2) + 16 * ((col * (C::E / 8) + e) ^ C::kswz(key))) =
+              piece8<F>(kr[i], e, scale_at(ks[i], block));
+      }
+    }
+  };
+  // After the wave's copies are done. Where some query does not see all of the tile, rows that no
+  // query sees become zeros, and what is infinite or NaN in rows that only some see is
+  // taken out here and added at the end.
+  const auto stage_v = [&](int32_t tt, int buf) __attribute__((always_inline)) {
+    if constexpr (COPY) copies_done();
     if (!mine) return;
     const int32_t j0 = kt.tile(tt) * BN;
     if (!all_see(j0, j0 + BN, p_lo, p_hi, n, a.window, a.sinks)) {
-      // rows that no query sees become zeros, and what is infinite or NaN in
-      // rows that only some see is taken out here and added at the end
       int32_t jv = j0;
       asm volatile("" : "+v"(jv));
       bool special = false;
 #pragma unroll
-      for (int i = 0; i < C::NL; ++i) special |= clean<F>(vr[i], vs[i], block, kt.some(jv + key0 + i * STEP));
+      for (int i = 0; i < C::NL; ++i) {
+        const bool some = kt.some(jv + key0 + i * STEP);
+        if constexpr (COPY) {
+          Raw16* p = reinterpret_cast<Raw16*>(ldsV[buf] + (threadIdx.x + i * 64 * W) * 16);  // as this thread copied it
+          const Raw16 v = *p;
+          uint32_t x[4] = {v.w[0], v.w[1], v.w[2], v.w[3]};
+          uint64_t none = 0;
+          special |= clean<F>(x, none, 0, some);
+          *p = Raw16{x[0], x[1], x[2], x[3]};
+        } else {
+          special |= clean<F>(vr[i], vs[i], block, some);
+        }
+      }
       if (special) lds_special = 1;
     }
+    if constexpr (!COPY)
 #pragma unroll
-    for (int i = 0; i < C::NL; ++i) {
-      const int key = key0 + i * STEP;
+      for (int i = 0; i < C::NL; ++i) {
+        const int key = key0 + i * STEP;
 #pragma unroll
-      for (int e = 0; e < C::E / 8; ++e)
-        *reinterpret_cast<Raw16*>(ldsV[buf] + key * (D * 2) + 16 * ((col * (C::E / 8) + e) ^ C::vswz(key))) =
-            piece8<F>(vr[i], e, fmt_scaled(F) ? scale_at(vs[i], block) : 0.f);
-    }
+        for (int e = 0; e < C::E / 8; ++e)
+          *reinterpret_cast<Raw16*>(ldsV[buf] + key * (D * 2) + 16 * ((col * (C::E / 8) + e) ^ C::vswz(key))) =
+              piece8<F>(vr[i], e, scale_at(vs[i], block));
+      }
   };
 
   // LDS addresses of a lane's operands: the rest is the same for all lanes
@@ -800,15 +858,43 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
   // t + 1 are computed beside its softmax. A product takes the matrix unit 32 cycles
   // in which the vector unit is free: the source has between two products what
   // fits there, and their operands' reads two or three products ahead.
-  int64_t row = 0, next = 0;  // rows of tiles t + 1, t + 2
+  int64_t rows[KAHEAD + 1];  // of the tiles t + 1, ...
   const int32_t t_begin = t;
+  constexpr int NS = D / 8, NP = D / 8, HALF = NP / 2;  // products for the scores, and with the weights
+  // operands in flight: KA products ahead of the first kind's, VA of the second's
+  constexpr int KA = D > 128 ? 3 : NS < 5 ? NS : 5, VA = D > 128 ? 2 : NP < 4 ? NP : 4;
+  Bf16x8 kf[KA + 1];
   auto step = [&](auto bufc) __attribute__((always_inline)) {
-    constexpr int BUF = decltype(bufc)::value;
-    constexpr int NS = D / 8, NP = D / 8, HALF = NP / 2;  // products for the scores, and with the weights
-    __syncthreads();  // K of t + 1 and V of t are in LDS, and no wave reads what is written below
-    fetch_k(next);
-    if constexpr (BOTH) fetch_v(row);
-    const int64_t later = row_of(t + 3);
+    constexpr int BUF = decltype(bufc)::value, KB = BUF % KBUF, VB = BUF % 2;  // tile t's buffers
+    // Tile t + 1's K (for KAHEAD = 2: t + 2's) and t's V are in LDS, and no wave reads
+    // what is written below.
+    __syncthreads();
+    if constexpr (KAHEAD == 1)
+#pragma unroll
+      for (int i = 0; i < KA; ++i) kf[i] = k_operand((KB + 1) % KBUF, i);
+    F32x16 ahead[2];
+    const auto score = [&](int i) __attribute__((always_inline)) {  // the i-th product of tile t + 1's scores
+      const int kb = i / (D / 16), kk = i % (D / 16);
+      ahead[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % (KA + 1)], q[kk], kk == 0 ? F32x16{} : ahead[kb], 0, 0, 0);
+    };
+    Bf16x8 vf[VA + 1];
+    const auto operand = [&](int i) __attribute__((always_inline)) {  // of the scores' i-th product, then of the weights' first ones
+      if (i < NS) kf[i % (KA + 1)] = k_operand((KB + 1) % KBUF, i);
+      else if (i - NS < VA) vf[i - NS] = v_operand(VB, i - NS);
+    };
+    // The first products need nothing of tile t: its mask, its maximum and the next
+    // tiles' loads go beside them.
+    constexpr int FIRST = 3;
+    static_assert(FIRST < NS && FIRST <= KA, "products before the softmax");
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < FIRST; ++i) {
+      operand(i + KA);
+      score(i);
+    }
+    fetch_k(rows[KAHEAD], (KB + KAHEAD + 1) % KBUF);
+    if constexpr (BOTH) fetch_v(rows[0], VB ^ 1);
+    const int64_t later = row_of(t + KAHEAD + 2);
     const int32_t j0 = kt.tile(t) * BN;
     if (!all_see(j0, j0 + BN, pw_lo, pw_hi, n, a.window, a.sinks)) {
       const Limits in(j0 + 4 * h, pos, n, a.window, a.sinks);
@@ -842,30 +928,24 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
         l += x + y;  // (as fp32: the sum also gives the lse)
       }
     };
-    F32x16 ahead[2];
-    // operands in flight: KA products ahead of the first, VA of the second
-    constexpr int KA = D > 128 ? 3 : NS < 5 ? NS : 5, VA = D > 128 ? 2 : NP < 4 ? NP : 4;
-    Bf16x8 kf[KA + 1], vf[VA + 1];
-#pragma unroll
-    for (int i = 0; i < KA; ++i) kf[i] = k_operand(BUF ^ 1, i);
+    __builtin_amdgcn_s_setprio(1);  // of two waves, the one among its products first (2% of a long prompt)
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      if (i + KA < NS) kf[(i + KA) % (KA + 1)] = k_operand(BUF ^ 1, i + KA);
-      else if (i + KA - NS < VA) vf[i + KA - NS] = v_operand(BUF, i + KA - NS);
-      const int kb = i / (D / 16), kk = i % (D / 16);
-      ahead[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % (KA + 1)], q[kk], kk == 0 ? F32x16{} : ahead[kb], 0, 0, 0);
-      weights(0, 8 * i / NS, 8 * (i + 1) / NS);
+    for (int i = FIRST; i < NS; ++i) {
+      operand(i + KA);
+      score(i);
+      weights(0, 8 * (i - FIRST) / (NS - FIRST), 8 * (i - FIRST + 1) / (NS - FIRST));
       __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (!BOTH) {
-      stage_k(BUF);
-      fetch_v(row);
+      stage_k((KB + KAHEAD + 1) % KBUF);
+      fetch_v(rows[0], VB ^ 1);
     }
     float biggest = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      if (i + VA < NP) vf[(i + VA) % (VA + 1)] = v_operand(BUF, i + VA);
+      if (i + VA < NP) vf[(i + VA) % (VA + 1)] = v_operand(VB, i + VA);
+      else if (KAHEAD == 2 && i + VA - NP < KA) kf[i + VA - NP] = k_operand((KB + 2) % KBUF, i + VA - NP);
       const int ks4 = i / (D / 32), db = i % (D / 32);
       o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % (VA + 1)], w[ks4], o[db], 0, 0, 0);
       if (i < HALF) {
@@ -876,36 +956,53 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (BOTH) stage_k(BUF);
-    stage_v(t + 1, BUF ^ 1);
+    if constexpr (KAHEAD == 2)
+#pragma unroll
+      for (int i = VA < KA ? VA : KA; i < KA; ++i) kf[i] = k_operand((KB + 2) % KBUF, i);
+    __builtin_amdgcn_s_setprio(0);
+    if constexpr (BOTH) stage_k((KB + KAHEAD + 1) % KBUF);
+    stage_v(t + 1, VB ^ 1);
     s[0] = ahead[0], s[1] = ahead[1];
     most = biggest;
-    row = next, next = later;
+#pragma unroll
+    for (int i = 0; i < KAHEAD; ++i) rows[i] = rows[i + 1];
+    rows[KAHEAD] = later;
     ++t;
   };
   if (t < t_end) {
     // tiles past the last are read as the last again, and not used
     const int64_t here = row_of(t);
-    row = row_of(t + 1), next = row_of(t + 2);
-    fetch_k(here);
+#pragma unroll
+    for (int i = 0; i <= KAHEAD; ++i) rows[i] = row_of(t + 1 + i);
     __syncthreads();  // lds_special is set
-    stage_k(0);
-    fetch_v(here);
+#pragma unroll
+    for (int i = 0; i <= KAHEAD; ++i) {
+      fetch_k(i == 0 ? here : rows[i - 1], i);
+      stage_k(i);
+    }
+    fetch_v(here, 0);
     stage_v(t, 0);
-    fetch_k(row);
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
+    for (int i = 0; i < NS; ++i) {
       const int kb = i / (D / 16), kk = i % (D / 16);
       s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(0, i), q[kk], kk == 0 ? F32x16{} : s[kb], 0, 0, 0);
     }
     most = largest(s, 0, 16, -INFINITY);
-    stage_k(1);
+    if constexpr (KAHEAD == 2)
+#pragma unroll
+      for (int i = 0; i < KA; ++i) kf[i] = k_operand(1, i);
     for (;;) {
       step(std::integral_constant<int, 0>());
       if (t >= t_end) break;
       step(std::integral_constant<int, 1>());
       if (t >= t_end) break;
+      if constexpr (KBUF == 4) {
+        step(std::integral_constant<int, 2>());
+        if (t >= t_end) break;
+        step(std::integral_constant<int, 3>());
+        if (t >= t_end) break;
+      }
     }
     __syncthreads();
     if (lds_special) {
