@@ -430,16 +430,12 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
   // queries: lane's row and, in its pieces' order, its elements
   Bf16x8 q[NB][D / 32];
   int32_t pos[NB];
+  const char* q_at[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    const int r = nb * 16 + l16, tok = (int)fast_div((uint32_t)min(r, R - 1), a.G_div);
+    const int r = min(nb * 16 + l16, R - 1), tok = (int)fast_div((uint32_t)r, a.G_div);
     pos[nb] = p_lo + tok;
-    const char* at = a.q + 2 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + min(r, R - 1) - tok * a.G) * a.q_h + (int64_t)tok * a.q_m);
-#pragma unroll
-    for (int c = 0; c < C::KN; ++c)
-#pragma unroll
-      for (int s = 0; s < C::KE / 8; ++s)
-        q[nb][c * (C::KE / 8) + s] = __builtin_bit_cast(Bf16x8, load16(at + 2 * ((c * 4 + g) * C::KE + 8 * s)));
+    q_at[nb] = a.q + 2 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + r - tok * a.G) * a.q_h + (int64_t)tok * a.q_m);
   }
 
   F32x4 o[NB][D / 16];
@@ -499,6 +495,14 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
     const int64_t row = row_of(t);
     next = row_of(t + kFewWaves);
     fetch(row);
+    // (after the rows, whose addresses took a trip to the table)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int c = 0; c < C::KN; ++c)
+#pragma unroll
+        for (int s = 0; s < C::KE / 8; ++s)
+          q[nb][c * (C::KE / 8) + s] = __builtin_bit_cast(Bf16x8, load16(q_at[nb] + 2 * ((c * 4 + g) * C::KE + 8 * s)));
   }
   for (; t < t_end; t += kFewWaves) {
     const int32_t j0 = kt.tile(t) * kFewKeys;
@@ -695,14 +699,8 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
   int32_t t = (int32_t)((int64_t)kt.count * pl.split / st.splits);
 
   Bf16x8 q[D / 16];
-  int32_t pos;
-  {
-    const int r = min(r0 + wave * 32 + l32, R - 1), tok = (int)fast_div((uint32_t)r, a.G_div);
-    pos = st.first + tok;
-    const char* at = a.q + 2 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + r - tok * a.G) * a.q_h + (int64_t)tok * a.q_m);
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) q[kk] = __builtin_bit_cast(Bf16x8, load16(at + 2 * (16 * kk + 8 * h)));
-  }
+  const int qr = min(r0 + wave * 32 + l32, R - 1), tok = (int)fast_div((uint32_t)qr, a.G_div);
+  const int32_t pos = st.first + tok;
   // the wave's own positions
   const int32_t pw_lo = st.first + (int32_t)fast_div((uint32_t)min(r0 + wave * 32, R - 1), a.G_div);
   const int32_t pw_hi = st.first + (int32_t)fast_div((uint32_t)min(r0 + wave * 32 + 31, R - 1), a.G_div);
@@ -981,6 +979,9 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
       stage_k(i);
     }
     fetch_v(here, 0);
+    const char* q_at = a.q + 2 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + qr - tok * a.G) * a.q_h + (int64_t)tok * a.q_m);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) q[kk] = __builtin_bit_cast(Bf16x8, load16(q_at + 2 * (16 * kk + 8 * h)));
     stage_v(t, 0);
     __syncthreads();
 #pragma unroll
@@ -1045,7 +1046,7 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
         ml[0] = m, ml[1] = sum;
       }
     } else {
-      const int tok = (int)fast_div((uint32_t)r, a.G_div), head = pl.h * a.G + r - tok * a.G;
+      const int head = pl.h * a.G + r - tok * a.G;  // (r is qr here)
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       char* at = a.out + 2 * ((int64_t)b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m);
 #pragma unroll
@@ -1215,40 +1216,38 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int32_t BM) {
   const int32_t h = (int32_t)(x / R), r = (int32_t)(x % R), tile = r / BM, rr = r % BM;
   // places run over the splits, the tiles from the last, the heads
   const int64_t slot = st.start + ((int64_t)h * st.tiles + (st.tiles - 1 - tile)) * st.splits;
+  // the row's elements of 16 parts at a time, the first ones on their way while the weights are made
+  constexpr int E = D >= 64 ? D / 64 : 1, ROUND = 16;
+  typedef float Part __attribute__((ext_vector_type(E)));
+  const float* p = a.part + (slot * BM + rr) * D + (lane * E) % D;
+  Part y[ROUND];
+  const auto load_round = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < ROUND; ++k)  // the last again past the last, with no weight
+      y[k] = *reinterpret_cast<const Part*>(p + (int64_t)min(s0 + k, st.splits - 1) * BM * D);
+  };
+  load_round(0);
   const float* ml = a.part_ml + (slot * BM + rr) * 2;
   float m = -INFINITY, l = 0.f;
   if (lane < st.splits) m = ml[(int64_t)lane * BM * 2], l = ml[(int64_t)lane * BM * 2 + 1];
-  float top = m;
+  const float top = wave_max(m), w = exp2_hw(m - shift_of(top)), sum = wave_sum(l * w);
+  Part v = 0.f;
+  for (int s0 = 0;;) {
 #pragma unroll
-  for (int k = 1; k < kWave; k *= 2) top = fmaxf(top, __shfl_xor(top, k, kWave));
-  const float w = exp2_hw(m - shift_of(top));
-  float sum = l * w;
-#pragma unroll
-  for (int k = 1; k < kWave; k *= 2) sum += __shfl_xor(sum, k, kWave);
-  constexpr int E = D >= 64 ? D / 64 : 1;
-  float v[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) v[e] = 0.f;
-  const float* p = a.part + (slot * BM + rr) * D + (lane * E) % D;
-  for (int s0 = 0; s0 < st.splits; s0 += 8) {
-    float y[8][E];
-#pragma unroll
-    for (int k = 0; k < 8; ++k)  // the last again past the last, with no weight
-#pragma unroll
-      for (int e = 0; e < E; ++e) y[k][e] = p[(int64_t)min(s0 + k, st.splits - 1) * BM * D + e];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float f = __shfl(w, min(s0 + k, st.splits - 1), kWave);
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = s0 + k < st.splits ? v[e] + f * y[k][e] : v[e];
+    for (int k = 0; k < ROUND; ++k) {
+      const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), min(s0 + k, kWave - 1)));
+      if (s0 + k < st.splits) v += y[k] * f;
     }
+    s0 += ROUND;
+    if (s0 >= st.splits) break;
+    load_round(s0);
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const int32_t tok = (int32_t)fast_div((uint32_t)r, a.G_div), head = h * a.G + r - tok * a.G;
   const int64_t b = a.b0 + blockIdx.y, at = b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m + lane * E;
   if (lane * E < D) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) reinterpret_cast<__bf16*>(a.out)[at + e] = (__bf16)(v[e] * inv);
+    for (int e = 0; e < E; ++e) reinterpret_cast<__bf16*>(a.out)[at + e] = (__bf16)(v[e] * inv);  // (one store)
   }
   if (lane == 0 && a.lse)
     a.lse[(b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (top + log2_hw(sum)) * kLn2;
