@@ -361,7 +361,8 @@ ipv_status ipv_ckv_stream(const ipv_shape* shape, void* K, void* V, int32_t* fra
  *                   and their negatives), element 2i in the low half of byte i
  * The quantised formats keep one scale for each 32 consecutive elements of a
  * row, K_scales and V_scales [pages, layers, kv_heads, page_rows, D / 32] bytes:
- * an element stands for its value times 2^(byte - 127); byte 255: the block is NaN.
+ * an element stands for its value times 2^(byte - 127); byte 255: the block is NaN
+ * (values below 2^-126 in magnitude may be taken for zero).
  * Row j of stream b (its position) is slot j % page_rows of page
  * page_table[b * table_cols + j / page_rows] (int32, device). Pages may be
  * shared between streams that only read them. page_table NULL: stream b's rows
@@ -438,7 +439,8 @@ ipv_status ipv_attend_workspace_bytes(const ipv_page_shape* pool, int32_t stream
  * are written: q_first[b] = n_tokens[b] - q_rows[b].
  * q and out are bf16 (fp32 for IPV_PAGES_F32); query i of head a of stream b is
  * at q + b * q_strides[0] + a * q_strides[1] + i * q_strides[2], out alike; lse (fp32,
- * may be NULL) is [streams, q_heads, max_rows], written for i < q_rows[b].
+ * may be NULL) is [streams, q_heads, max_rows], written for i < q_rows[b]. out may
+ * not overlap q or the pool.
  * Queries are expected rotated to their positions where the keys are. Products
  * accumulate in fp32 and the softmax is fp32; its weights are rounded to bf16 before
  * they multiply V (not with IPV_PAGES_F32). One call gives the same bits every time.

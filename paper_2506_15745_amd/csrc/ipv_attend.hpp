@@ -275,11 +275,21 @@ __device__ __forceinline__ void load_piece(const char* p, uint32_t* w) {
   }
 }
 
+// Sixteen bytes a lane from memory straight into LDS: lane i's to `at` + 16 i, `at` the
+// same in all lanes. No register waits for them: copies_done() does, for all of the wave's.
+__device__ __forceinline__ void copy_to_lds(const char* from, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const char* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+
 // ---------------------------------------------------------------- few rows
 // Up to 16 * NB rows a KV head (single tokens of grouped heads): bound by the
 // bytes of the cache. Each wave takes key tiles of its own (32 rows), K straight
 // into the matrix operand's layout, V through an LDS tile that only this wave
-// uses; the next tile's rows are in flight while one is computed. The four waves
+// uses (bf16: copied there, two tiles in turn); the next tile's rows are in flight while one is computed. The four waves
 // join through LDS, the splits of a key range through k_attend_join.
 constexpr int kFewWaves = 4;
 constexpr int kFewKeys = 32;
@@ -309,12 +319,14 @@ struct JoinLds {
   static constexpr size_t kWaveBytes = (size_t)NR * STRIDE * 4;
 };
 
-// Workgroups of a CU, by registers.
-constexpr int few_per_cu(int F, int D, int NB) { return NB * D > 256 ? 1 : fmt_scaled(F) && NB * D <= 128 ? 3 : 2; }
+// Workgroups of a CU, by registers and LDS.
+constexpr int few_per_cu(int F, int D, int NB) {
+  return NB * D > 256 || (F == kFmtBf16 && D > 128) ? 1 : fmt_scaled(F) && NB * D <= 128 ? 3 : 2;  // (D = 256: by its bf16 tiles)
+}
 
-template <int D, int NB>
+template <int F, int D, int NB>
 constexpr size_t few_wave_lds() {
-  constexpr size_t tile = (size_t)kFewKeys * D * 2, join = JoinLds<D, 16 * NB>::kWaveBytes;
+  constexpr size_t tile = (size_t)kFewKeys * D * 2 * (F == kFmtBf16 ? 2 : 1), join = JoinLds<D, 16 * NB>::kWaveBytes;
   return tile > join ? tile : join;
 }
 
@@ -385,10 +397,18 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendStre
   load_round(threadIdx.x, 0);
   // weights of the parts, by row: lane s has part s
   float(*weight)[kMaxSplits] = reinterpret_cast<float(*)[kMaxSplits]>(&lds[0][0]);
-  for (int r = wave; r < rows; r += kFewWaves) {
-    float pm = -INFINITY, ps = 0.f;
-    if (lane < st.splits) load_pair(a.part_ml + ((int64_t)(pl.first + lane) * NR + r) * 2, pm, ps);
-    const float top = wave_max(pm), f = exp2_hw(pm - shift_of(top)), sum = wave_sum(ps * f);
+  constexpr int RW = NR / kFewWaves;  // rows of a wave, all on their way at once
+  float pm[RW], ps[RW];
+#pragma unroll
+  for (int i = 0; i < RW; ++i) {
+    const int r = i * kFewWaves + wave;
+    pm[i] = -INFINITY, ps[i] = 0.f;
+    if (r < rows && lane < st.splits) load_pair(a.part_ml + ((int64_t)(pl.first + lane) * NR + r) * 2, pm[i], ps[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < RW; ++i) {
+    const int r = i * kFewWaves + wave;
+    const float top = wave_max(pm[i]), f = exp2_hw(pm[i] - shift_of(top)), sum = wave_sum(ps[i] * f);
     weight[r][lane] = f;
     if (lane == 0) lds_ml[0][r][0] = top, lds_ml[0][r][1] = sum;
   }
@@ -412,7 +432,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendStre
 template <int F, int D, int NB>
 __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend_few(AttendArgs a) {
   using C = FewCfg<F, D>;
-  __shared__ __attribute__((aligned(16))) char lds[kFewWaves][few_wave_lds<D, NB>()];
+  __shared__ __attribute__((aligned(16))) char lds[kFewWaves][few_wave_lds<F, D, NB>()];
   __shared__ float lds_ml[kFewWaves][16 * NB][2];
   __shared__ uint32_t lds_last;
   const Place pl = place_of(a);
@@ -458,9 +478,11 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
     bad |= x;
     return r;
   };
-  uint32_t kr[2][C::KQ / 4], vr[C::NV][4];
-  uint64_t ks[2], vs[C::NV];
-  auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+  constexpr bool COPY = F == kFmtBf16;
+  uint32_t kr[2][C::KQ / 4], vr[COPY ? 1 : C::NV][4];
+  uint64_t ks[2], vs[COPY ? 1 : C::NV];
+  char* tile = lds[wave];
+  auto fetch = [&](int64_t row, char* v_tile) __attribute__((always_inline)) {
     int64_t kw[2], vw[C::NV];  // the rows (of the pool) of this lane's pieces
     if (whole) {
 #pragma unroll
@@ -482,19 +504,23 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
     }
 #pragma unroll
     for (int i = 0; i < C::NV; ++i) {
-      load_piece<16>(a.pool.V + vw[i] * C::RB + lane % C::CPR * 16, vr[i]);
-      if (fmt_scaled(F)) vs[i] = load_scales<D>(a.pool.Vs, vw[i]);
+      if constexpr (COPY) {  // the source column makes up for the place
+        const int ch = lane % C::CPR ^ C::swz((i * kWave + lane) / C::CPR);
+        copy_to_lds(a.pool.V + vw[i] * C::RB + ch * 16, __builtin_amdgcn_readfirstlane(lds_address(v_tile) + i * 1024));
+      } else {
+        load_piece<16>(a.pool.V + vw[i] * C::RB + lane % C::CPR * 16, vr[i]);
+        if (fmt_scaled(F)) vs[i] = load_scales<D>(a.pool.Vs, vw[i]);
+      }
     }
   };
 
-  char* tile = lds[wave];
   int64_t next = 0;
   bool special = false;  // V held infinities or NaN in rows that only some queries see
   const int32_t t_begin = t;
   if (t < t_end) {
     const int64_t row = row_of(t);
     next = row_of(t + kFewWaves);
-    fetch(row);
+    fetch(row, tile);
     // (after the rows, whose addresses took a trip to the table)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -504,7 +530,10 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
         for (int s = 0; s < C::KE / 8; ++s)
           q[nb][c * (C::KE / 8) + s] = __builtin_bit_cast(Bf16x8, load16(q_at[nb] + 2 * ((c * 4 + g) * C::KE + 8 * s)));
   }
+  constexpr int VTILE = kFewKeys * D * 2;
+  int vbuf = 0;
   for (; t < t_end; t += kFewWaves) {
+    if constexpr (COPY) copies_done();
     const int32_t j0 = kt.tile(t) * kFewKeys;
     const bool full = all_see(j0, j0 + kFewKeys, p_lo, p_hi, n, a.window, a.sinks);
     // scores of this tile's keys (the operand is built from the loaded bytes)
@@ -532,20 +561,31 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
 #pragma unroll
       for (int i = 0; i < C::NV; ++i) {
         const int x = i * kWave + lane;
-        special |= clean<F>(vr[i], vs[i], x % C::CPR * C::VE / kScaleBlock, kt.some(jv + x / C::CPR));
+        const bool some = kt.some(jv + x / C::CPR);
+        if constexpr (COPY) {
+          Raw16* p = reinterpret_cast<Raw16*>(tile + vbuf * VTILE + x * 16);  // as this lane copied it
+          const Raw16 v = *p;
+          uint32_t e[4] = {v.w[0], v.w[1], v.w[2], v.w[3]};
+          uint64_t none = 0;
+          special |= clean<F>(e, none, 0, some);
+          *p = Raw16{e[0], e[1], e[2], e[3]};
+        } else {
+          special |= clean<F>(vr[i], vs[i], x % C::CPR * C::VE / kScaleBlock, some);
+        }
       }
     }
+    if constexpr (!COPY)
 #pragma unroll
-    for (int i = 0; i < C::NV; ++i) {
-      const int x = i * kWave + lane, key = x / C::CPR, col = x % C::CPR;
-      if (C::CPR == 1 && x >= kFewKeys) continue;
-      const float scale = fmt_scaled(F) ? scale_at(vs[i], col * C::VE / kScaleBlock) : 0.f;
+      for (int i = 0; i < C::NV; ++i) {
+        const int x = i * kWave + lane, key = x / C::CPR, col = x % C::CPR;
+        if (C::CPR == 1 && x >= kFewKeys) continue;
+        const float scale = scale_at(vs[i], col * C::VE / kScaleBlock);
 #pragma unroll
-      for (int e = 0; e < C::VE / 8; ++e)
-        *reinterpret_cast<Raw16*>(tile + key * (D * 2) + 16 * ((col * (C::VE / 8) + e) ^ C::swz(key))) = piece8<F>(vr[i], e, scale);
-    }
+        for (int e = 0; e < C::VE / 8; ++e)
+          *reinterpret_cast<Raw16*>(tile + key * (D * 2) + 16 * ((col * (C::VE / 8) + e) ^ C::swz(key))) = piece8<F>(vr[i], e, scale);
+      }
     if (t + kFewWaves < t_end) {
-      fetch(next);
+      fetch(next, tile + (vbuf ^ 1) * VTILE);
       next = row_of(t + 2 * kFewWaves);
     }
     // softmax: weights of 8 keys a lane, keys 4 g + i and 16 + 4 g + i
@@ -583,14 +623,16 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) {
       const int k0 = 4 * g + l16 / 4, ch = 2 * db + (l16 % 4) / 2, in = 8 * (l16 & 1);
-      const U32x2 x = lds_column4(tile + k0 * (D * 2) + 16 * (ch ^ C::swz(k0)) + in);
-      const U32x2 y = lds_column4(tile + (k0 + 16) * (D * 2) + 16 * (ch ^ C::swz(k0 + 16)) + in);
+      const char* at = tile + (COPY ? vbuf * VTILE : 0);
+      const U32x2 x = lds_column4(at + k0 * (D * 2) + 16 * (ch ^ C::swz(k0)) + in);
+      const U32x2 y = lds_column4(at + (k0 + 16) * (D * 2) + 16 * (ch ^ C::swz(k0 + 16)) + in);
       const Raw16 r = {x.x, x.y, y.x, y.y};
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
         o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf16x8, r), w[nb], o[nb][db], 0, 0, 0);
     }
     __builtin_amdgcn_wave_barrier();
+    vbuf ^= 1;
   }
   if (__ballot(special) != 0) {
 #pragma unroll 1
@@ -645,16 +687,6 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
 // for D = 256, whose sums and queries alone take 192 registers.
 constexpr int kTileKeys = 64;
 __host__ __device__ constexpr int tile_waves(int D) { return D <= 128 ? 8 : 4; }
-
-// Sixteen bytes a lane from memory straight into LDS: lane i's to `at` + 16 i, `at` the
-// same in all lanes. No register waits for them: copies_done() does, for all of the wave's.
-__device__ __forceinline__ void copy_to_lds(const char* from, uint32_t at) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory", "m0");
-}
-__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ uint32_t lds_address(const char* p) {
-  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
-}
 
 template <int F, int D, int W>
 struct TileCfg {

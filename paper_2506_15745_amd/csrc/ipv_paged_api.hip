@@ -291,10 +291,13 @@ ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const voi
   if (!(scale > 0) || !std::isfinite(scale) || !std::isnormal((float)(scale * 1.4426950408889634)) || window < 0 ||
       sinks < 0)
     return IPV_ERR_ARG;
+  int64_t queries = 0;  // of all streams and heads: their row tiles (16 rows at least) are counted in 31 bits
   for (int32_t b = 0; b < streams; ++b) {
     if (n_tokens[b] < 0 || n_tokens[b] > table_rows(pool, table_cols)) return IPV_ERR_SHAPE;
     if (q_rows[b] < 0 || q_rows[b] > max_rows || q_first[b] < 0 || q_first[b] > kMaxPosition - q_rows[b]) return IPV_ERR_SHAPE;
+    queries += (int64_t)q_rows[b] * q_heads;
   }
+  if (queries > (int64_t)kMaxPosition * 8) return IPV_ERR_SHAPE;
   size_t need = 0;
   IPV_TRY(ipv_attend_workspace_bytes(pool, streams, q_heads, max_rows, &need));
   IPV_TRY(check_word(ws, ws_bytes, need));

@@ -241,3 +241,51 @@ def test_many_streams_and_counts():
     inside = inside[:, None, None, :, None]
     assert torch.equal(k, torch.where(inside, K, torch.full_like(K, 5.0)))
     assert torch.equal(v, torch.where(inside, V, torch.full_like(V, 5.0)))
+
+
+def test_refused_calls_touch_nothing():
+    pool = R.filled_pool("fp8", 6, 2, 2, 16, 64, 3)
+    table, ws = R.shuffled_table(1, 3, 6, 1), ipv.alloc_page_workspace("cuda")
+    K, V = rows("bf16", 1, 2, 2, 8, 64, 3)
+    rotary = R.angles(10, 64, "cuda")
+    q = torch.ones(1, 4, 3, 64, dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.full_like(q, 3.0), torch.full((1, 4, 3), 4.0, device="cuda")
+    aws = ipv.alloc_attend_workspace(pool, 1, 4, 3)
+    held = (pool.K, pool.V, pool.K_scales, pool.V_scales, K, V, ws, aws, out, lse)
+    before = [t.clone() for t in held]
+    W, Rd, A = ipv.ipv_page_write, ipv.ipv_page_read, ipv.ipv_attend
+    for status, f, args, kw in (
+            (ipv.ERR_SHAPE, W, (pool, table, 41, K, V, ws), {}),               # past the table's 48 rows
+            (ipv.ERR_SHAPE, W, (pool, table, 0, K, V, ws), dict(rows=9)),
+            (ipv.ERR_SHAPE, W, (pool, table, 0, K, V, ws), dict(first_layer=1)),
+            (ipv.ERR_ARG, W, (pool, table, 5, K, V, ws), dict(rotary=rotary)),  # angles up to position 9
+            (ipv.ERR_SHAPE, W, (pool, table, 0, K, V, ws), dict(rotary=rotary[:, :16])),
+            (ipv.ERR_SHAPE, W, (pool, table, 0, K[:, :, :1], V[:, :, :1], ws), {}),
+            (ipv.ERR_DTYPE, W, (pool, table, 0, K, V.float(), ws), {}),
+            (ipv.ERR_DTYPE, W, (pool, table, 0, K.half(), V.half(), ws), {}),
+            (ipv.ERR_SHAPE, W, (pool, table.repeat(2, 1), 0, K, V, ws), {}),
+            (ipv.ERR_SHAPE, W, (pool, table.long(), 0, K, V, ws), {}),
+            (ipv.ERR_ARG, W, (pool, table.cpu(), 0, K, V, ws), {}),
+            (ipv.ERR_ARG, W, (pool, table, 0, K.cpu(), V, ws), {}),
+            (ipv.ERR_SHAPE, W, (pool, table, [0, 0], K, V, ws), {}),
+            (ipv.ERR_WORKSPACE, W, (pool, table, 0, K, V, None), {}),
+            (ipv.ERR_WORKSPACE, Rd, (pool, table, 0, K, V, ws[:128]), {}),
+            (ipv.ERR_SHAPE, Rd, (pool, table, 0, K.transpose(3, 4), V.transpose(3, 4), ws), {}),
+            (ipv.ERR_SHAPE, Rd, (pool, table, 0, K, V.transpose(2, 3).contiguous().transpose(2, 3), ws), {}),
+            (ipv.ERR_SHAPE, A, (pool, table, 49, 46, 0, q, out, aws), {}),
+            (ipv.ERR_SHAPE, A, (pool, table, 40, 37, 2, q, out, aws), {}),
+            (ipv.ERR_SHAPE, A, (pool, table, 40, 37, 0, q[:, :3], out[:, :3], aws), {}),
+            (ipv.ERR_SHAPE, A, (pool, table, 40, 37, 0, q, out, aws), dict(q_rows=4)),
+            (ipv.ERR_SHAPE, A, (pool, table, 40, 37, 0, q, out[:, :, :2], aws), {}),
+            (ipv.ERR_DTYPE, A, (pool, table, 40, 37, 0, q.float(), out.float(), aws), {}),
+            (ipv.ERR_DTYPE, A, (pool, table, 40, 37, 0, q, out, aws), dict(lse=lse.double())),
+            (ipv.ERR_SHAPE, A, (pool, table, 40, 37, 0, q, out, aws), dict(lse=lse[:, :, :2])),
+            (ipv.ERR_ARG, A, (pool, table, 40, 37, 0, q, out, aws), dict(scale=0.0)),
+            (ipv.ERR_ARG, A, (pool, table, 40, 37, 0, q, out, aws), dict(window=-1)),
+            (ipv.ERR_WORKSPACE, A, (pool, table, 40, 37, 0, q, out, ws), {}),
+            (ipv.ERR_ARG, A, (pool, table, 40, 37, 0, q.cpu(), out, aws), {})):
+        with pytest.raises(ipv.IpvError) as e:
+            f(*args, **kw)
+        assert e.value.status == status, (status, f.__name__, args[1:3], kw)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(held, before))
