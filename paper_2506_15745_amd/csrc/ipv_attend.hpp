@@ -23,13 +23,14 @@
 
 namespace ipv {
 
-constexpr int kAttendStreams = 96;  // streams of one launch (their counts travel in its arguments)
+constexpr int kAttendStreams = 64;  // streams of one launch (their counts travel in its arguments)
 constexpr int kMaxSplits = 64;      // parts of a key range that are joined: a lane each
 
 struct AttendStream {
   int32_t n, first, rows;  // rows of the cache; position of the first query; queries
   int32_t start;           // its first workgroup
   int32_t tiles, splits;   // row tiles of a KV head; parts of a tile's keys
+  FastDiv by_tiles, by_splits;
 };
 
 struct AttendArgs {
@@ -158,6 +159,9 @@ struct Place {
   int32_t first;  // slot of the row tile's first part
 };
 __device__ __forceinline__ Place place_of(const AttendArgs& a) {
+  // the arguments that the first loads wait for, all on their way at once
+  asm volatile("" ::"s"(a.blocks), "s"(a.streams), "s"(a.pool.K), "s"(a.pool.V), "s"(a.pool.table), "s"(a.pool.T.m), "s"(a.q),
+               "s"(a.G_div.m), "s"(a.window), "s"(a.s[0].n), "s"(a.s[0].by_splits.m), "s"(a.layer_row), "s"(a.pool.page_rows_all));
   const uint32_t per = (uint32_t)(a.blocks + 7) / 8u;
   Place p;
   p.slot = (int32_t)((blockIdx.x % 8u) * per + blockIdx.x / 8u);
@@ -174,13 +178,12 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a) {
   }
   p.b = lo;
   const AttendStream& s = a.s[lo];
-  uint32_t x = (uint32_t)(p.slot - s.start);
-  p.split = (int32_t)(x % (uint32_t)s.splits);
+  const uint32_t x = (uint32_t)(p.slot - s.start), y = fast_div(x, s.by_splits);
+  p.split = (int32_t)(x - y * (uint32_t)s.splits);
   p.first = p.slot - p.split;
-  x /= (uint32_t)s.splits;
+  p.h = (int32_t)fast_div(y, s.by_tiles);
   // the last row tile first: under a causal mask it has the most keys
-  p.tile = s.tiles - 1 - (int32_t)(x % (uint32_t)s.tiles);
-  p.h = (int32_t)(x / (uint32_t)s.tiles);
+  p.tile = s.tiles - 1 - (int32_t)(y - (uint32_t)p.h * (uint32_t)s.tiles);
   return p;
 }
 

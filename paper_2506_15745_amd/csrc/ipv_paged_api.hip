@@ -222,6 +222,8 @@ void plan(AttendArgs* a, AttendKind kind, int D, int format) {
   int64_t at = 0;
   for (int32_t i = 0; i < a->streams; ++i) {
     a->s[i].start = (int32_t)at;
+    a->s[i].by_tiles = make_fastdiv((uint32_t)std::max(a->s[i].tiles, 1));
+    a->s[i].by_splits = make_fastdiv((uint32_t)a->s[i].splits);
     at += (int64_t)a->H * a->s[i].tiles * a->s[i].splits;
   }
   a->blocks = (int32_t)at;
