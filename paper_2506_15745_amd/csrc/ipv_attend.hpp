@@ -473,11 +473,14 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
   bool bad = false;
   // pages that hold whole tiles: a tile's rows follow each other
   const bool whole = a.pool.T.d % kFewKeys == 0;
-  // row (in the pool) of the tile's key lane % 32, or of its first; a key past the last is the last
-  auto row_of = [&](int32_t tt) __attribute__((always_inline)) {
-    const int32_t j = kt.tile(min(tt, kt.count - 1)) * kFewKeys + (whole ? 0 : lane % 32);
+  // the tile's key lane % 32, or its first; a key past the last is the last; its page, and its row in the pool
+  const auto key_of = [&](int32_t tt) __attribute__((always_inline)) {
+    return min(kt.tile(min(tt, kt.count - 1)) * kFewKeys + (whole ? 0 : lane % 32), n - 1);
+  };
+  const auto page_of = [&](int32_t tt) __attribute__((always_inline)) { return pool_page(a.pool, b, (uint32_t)key_of(tt)); };
+  const auto row_of = [&](int32_t page, int32_t tt) __attribute__((always_inline)) {
     bool x;
-    const int64_t r = pool_row(a.pool, b, (uint32_t)min(j, n - 1), &x) + head_row;
+    const int64_t r = pool_row(a.pool, page, (uint32_t)key_of(tt), &x) + head_row;
     bad |= x;
     return r;
   };
@@ -517,13 +520,13 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
     }
   };
 
-  int64_t next = 0;
+  int32_t next = 0;      // the next tile's page
   bool special = false;  // V held infinities or NaN in rows that only some queries see
   const int32_t t_begin = t;
   if (t < t_end) {
-    const int64_t row = row_of(t);
-    next = row_of(t + kFewWaves);
-    fetch(row, tile);
+    const int32_t page = page_of(t);
+    next = page_of(t + kFewWaves);
+    fetch(row_of(page, t), tile);
     // (after the rows, whose addresses took a trip to the table)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -588,8 +591,9 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
           *reinterpret_cast<Raw16*>(tile + key * (D * 2) + 16 * ((col * (C::VE / 8) + e) ^ C::swz(key))) = piece8<F>(vr[i], e, scale);
       }
     if (t + kFewWaves < t_end) {
-      fetch(next, tile + (vbuf ^ 1) * VTILE);
-      next = row_of(t + 2 * kFewWaves);
+      const int64_t row = row_of(next, t + kFewWaves);
+      next = page_of(t + 2 * kFewWaves);  // before the rows: what waits for it need not wait for them
+      fetch(row, tile + (vbuf ^ 1) * VTILE);
     }
     // softmax: weights of 8 keys a lane, keys 4 g + i and 16 + 4 g + i
     Bf16x8 w[NB];
@@ -642,7 +646,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
     for (int32_t tt = t_begin; tt < t_end; tt += kFewWaves) {
       const int32_t j0 = kt.tile(tt) * kFewKeys;
       if (all_see(j0, j0 + kFewKeys, p_lo, p_hi, n, a.window, a.sinks)) continue;
-      const int64_t row = row_of(tt);
+      const int64_t row = row_of(page_of(tt), tt);
 #pragma unroll 1
       for (int key = 0; key < kFewKeys; ++key) {
         if (!kt.some(j0 + key)) continue;
@@ -749,10 +753,14 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
   bool bad = false;
   // pages that hold whole tiles: a tile's rows follow each other
   const bool whole = a.pool.T.d % BN == 0;
-  auto row_of = [&](int32_t tt) {  // the pool's row of the tile's key `lane` (whole: of its first key)
-    const int32_t j = kt.tile(min(tt, kt.count - 1)) * BN + (whole ? 0 : lane);
+  // the tile's key `lane` (whole: its first); its page, and its row in the pool
+  const auto key_of = [&](int32_t tt) __attribute__((always_inline)) {
+    return min(kt.tile(min(tt, kt.count - 1)) * BN + (whole ? 0 : lane), n - 1);
+  };
+  const auto page_of = [&](int32_t tt) __attribute__((always_inline)) { return pool_page(a.pool, b, (uint32_t)key_of(tt)); };
+  const auto row_of = [&](int32_t page, int32_t tt) __attribute__((always_inline)) {
     bool x;
-    const int64_t r = pool_row(a.pool, b, (uint32_t)min(j, n - 1), &x) + head_row;
+    const int64_t r = pool_row(a.pool, page, (uint32_t)key_of(tt), &x) + head_row;
     bad |= x;
     return r;
   };
@@ -891,7 +899,8 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
   // t + 1 are computed beside its softmax. A product takes the matrix unit 32 cycles
   // in which the vector unit is free: the source has between two products what
   // fits there, and their operands' reads two or three products ahead.
-  int64_t rows[KAHEAD + 1];  // of the tiles t + 1, ...
+  int64_t rows[KAHEAD];  // of the tiles t + 1, ...
+  int32_t page = 0;      // of the tile after those
   const int32_t t_begin = t;
   constexpr int NS = D / 8, NP = D / 8, HALF = NP / 2;  // products for the scores, and with the weights
   // operands in flight: KA products ahead of the first kind's, VA of the second's
@@ -925,9 +934,10 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
       operand(i + KA);
       score(i);
     }
-    fetch_k(rows[KAHEAD], (KB + KAHEAD + 1) % KBUF);
+    const int64_t later = row_of(page, t + KAHEAD + 1);
+    page = page_of(t + KAHEAD + 2);  // a step before it is needed, and before the copies: nothing waits for it, or for them with it
+    fetch_k(later, (KB + KAHEAD + 1) % KBUF);
     if constexpr (BOTH) fetch_v(rows[0], VB ^ 1);
-    const int64_t later = row_of(t + KAHEAD + 2);
     const int32_t j0 = kt.tile(t) * BN;
     if (!all_see(j0, j0 + BN, pw_lo, pw_hi, n, a.window, a.sinks)) {
       const Limits in(j0 + 4 * h, pos, n, a.window, a.sinks);
@@ -998,15 +1008,19 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
     s[0] = ahead[0], s[1] = ahead[1];
     most = biggest;
 #pragma unroll
-    for (int i = 0; i < KAHEAD; ++i) rows[i] = rows[i + 1];
-    rows[KAHEAD] = later;
+    for (int i = 0; i + 1 < KAHEAD; ++i) rows[i] = rows[i + 1];
+    rows[KAHEAD - 1] = later;
     ++t;
   };
   if (t < t_end) {
     // tiles past the last are read as the last again, and not used
-    const int64_t here = row_of(t);
+    int32_t pages[KAHEAD + 1];
 #pragma unroll
-    for (int i = 0; i <= KAHEAD; ++i) rows[i] = row_of(t + 1 + i);
+    for (int i = 0; i <= KAHEAD; ++i) pages[i] = page_of(t + i);
+    page = page_of(t + KAHEAD + 1);
+    const int64_t here = row_of(pages[0], t);
+#pragma unroll
+    for (int i = 0; i < KAHEAD; ++i) rows[i] = row_of(pages[i + 1], t + 1 + i);
     __syncthreads();  // lds_special is set
 #pragma unroll
     for (int i = 0; i <= KAHEAD; ++i) {
@@ -1046,7 +1060,7 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
       for (int32_t tt = t_begin; tt < t_end; ++tt) {
         const int32_t j0 = kt.tile(tt) * BN;
         if (all_see(j0, j0 + BN, p_lo, p_hi, n, a.window, a.sinks)) continue;
-        const int64_t tile_row = row_of(tt);
+        const int64_t tile_row = row_of(page_of(tt), tt);
 #pragma unroll 1
         for (int key = 0; key < BN; ++key) {
           if (!kt.some(j0 + key)) continue;
@@ -1137,7 +1151,8 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(
   bool bad = false, special = false;
   auto row_of = [&](int32_t t) __attribute__((always_inline)) {  // the pool's row of the tile's key l32
     bool x;
-    const int64_t at = pool_row(a.pool, b, (uint32_t)min(kt.tile(t) * BN + l32, n - 1), &x) + head_row;
+    const uint32_t j = (uint32_t)min(kt.tile(t) * BN + l32, n - 1);
+    const int64_t at = pool_row(a.pool, pool_page(a.pool, b, j), j, &x) + head_row;
     bad |= x;
     return at;
   };

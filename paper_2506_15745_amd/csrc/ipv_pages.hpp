@@ -34,15 +34,18 @@ struct Pool {
   FastDiv T;              // rows of a page's (layer, head)
 };
 
-// Row of position j of stream b within its page's first (layer, head); add
-// (layer * H + head) * T. *bad: the table's entry names no page (page 0 is
-// taken in its place).
-__device__ __forceinline__ int64_t pool_row(const Pool& p, int b, uint32_t j, bool* bad) {
-  const uint32_t col = fast_div(j, p.T);
-  int32_t page = p.table ? p.table[(int64_t)b * p.cols + col] : b;
+// The page of position j of stream b, as the table has it. Where a loop looks rows up
+// ahead, this load is apart from what is made of it, so that nothing waits for it meanwhile.
+__device__ __forceinline__ int32_t pool_page(const Pool& p, int b, uint32_t j) {
+  return p.table ? p.table[(int64_t)b * p.cols + fast_div(j, p.T)] : b;
+}
+
+// Row of position j, which lies in that page, counted from the pool's first within
+// the first (layer, head); add (layer * H + head) * T. *bad: there is no such page
+// (page 0 is taken in its place).
+__device__ __forceinline__ int64_t pool_row(const Pool& p, int32_t page, uint32_t j, bool* bad) {
   *bad = (uint32_t)page >= (uint32_t)p.pages;
-  if (*bad) page = 0;
-  return (int64_t)page * p.page_rows_all + (j - col * p.T.d);
+  return (int64_t)(*bad ? 0 : page) * p.page_rows_all + (j - fast_div(j, p.T) * p.T.d);
 }
 
 // A scale byte as the power of two that the conversions take (255: NaN).
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(kPageThreads) void k_page_write(PageCall c) {
   const int d = (int)(threadIdx.x % S::kThreads) * 8;
   const int64_t pos = (int64_t)c.first[b] + i;
   bool bad;
-  const int64_t row0 = pool_row(c.pool, c.b0 + b, (uint32_t)pos, &bad) + c.first_slice;
+  const int64_t row0 = pool_row(c.pool, pool_page(c.pool, c.b0 + b, (uint32_t)pos), (uint32_t)pos, &bad) + c.first_slice;
   if (bad) {
     if (d == 0) atomicOr(c.err, kDevBadPage);
     return;
@@ -318,7 +321,7 @@ __global__ __launch_bounds__(kPageThreads) void k_page_read(PageCall c) {
   const int d = (int)(threadIdx.x % S::kThreads) * 8;
   const int64_t pos = (int64_t)c.first[b] + i;
   bool bad;
-  const int64_t row0 = pool_row(c.pool, c.b0 + b, (uint32_t)pos, &bad) + c.first_slice;
+  const int64_t row0 = pool_row(c.pool, pool_page(c.pool, c.b0 + b, (uint32_t)pos), (uint32_t)pos, &bad) + c.first_slice;
   if (bad && d == 0) atomicOr(c.err, kDevBadPage);
   const char* src = isv ? c.pool.V : c.pool.K;
   char* dst = isv ? c.V : c.K;
