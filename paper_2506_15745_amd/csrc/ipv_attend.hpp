@@ -283,6 +283,10 @@ __device__ __forceinline__ void load_piece(const char* p, uint32_t* w) {
 __device__ __forceinline__ void copy_to_lds(const char* from, uint32_t at) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory", "m0");
 }
+// From `base`, the same in all lanes, + offset.
+__device__ __forceinline__ void copy_to_lds(const char* base, uint32_t offset, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(offset), "s"(base) : "memory", "m0");
+}
 __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const char* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
@@ -432,7 +436,12 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendStre
   }
 }
 
-template <int F, int D, int NB>
+// WHOLE: pages hold whole tiles (their rows are a multiple of a tile's), so a tile's rows follow
+// each other: one page to look up, by a scalar load, and one scalar base with 32-bit offsets that
+// stay the same, where otherwise each lane has a 64-bit address a row. For D = 256 that is also
+// what makes its registers suffice: one token of fp8 over 16384 positions of 8 heads takes 22.1 us
+// with it and 28.5 without, four tokens of bf16 49.4 and 64.5.
+template <int F, int D, int NB, bool WHOLE>
 __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend_few(AttendArgs a) {
   using C = FewCfg<F, D>;
   __shared__ __attribute__((aligned(16))) char lds[kFewWaves][few_wave_lds<F, D, NB>()];
@@ -471,13 +480,13 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
   }
 
   bool bad = false;
-  // pages that hold whole tiles: a tile's rows follow each other
-  const bool whole = a.pool.T.d % kFewKeys == 0;
   // the tile's key lane % 32, or its first; a key past the last is the last; its page, and its row in the pool
   const auto key_of = [&](int32_t tt) __attribute__((always_inline)) {
-    return min(kt.tile(min(tt, kt.count - 1)) * kFewKeys + (whole ? 0 : lane % 32), n - 1);
+    return min(kt.tile(min(tt, kt.count - 1)) * kFewKeys + (WHOLE ? 0 : lane % 32), n - 1);
   };
-  const auto page_of = [&](int32_t tt) __attribute__((always_inline)) { return pool_page(a.pool, b, (uint32_t)key_of(tt)); };
+  const auto page_of = [&](int32_t tt) __attribute__((always_inline)) {
+    return WHOLE ? pool_page_uniform(a.pool, b, (uint32_t)key_of(tt)) : pool_page(a.pool, b, (uint32_t)key_of(tt));
+  };
   const auto row_of = [&](int32_t page, int32_t tt) __attribute__((always_inline)) {
     bool x;
     const int64_t r = pool_row(a.pool, page, (uint32_t)key_of(tt), &x) + head_row;
@@ -489,33 +498,35 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
   uint64_t ks[2], vs[COPY ? 1 : C::NV];
   char* tile = lds[wave];
   auto fetch = [&](int64_t row, char* v_tile) __attribute__((always_inline)) {
-    int64_t kw[2], vw[C::NV];  // the rows (of the pool) of this lane's pieces
-    if (whole) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) kw[kb] = row + (kb * 16 + l16);
-#pragma unroll
-      for (int i = 0; i < C::NV; ++i) vw[i] = row + (i * kWave + lane) / C::CPR % kFewKeys;
-    } else {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) kw[kb] = shfl64(row, kb * 16 + l16);
-#pragma unroll
-      for (int i = 0; i < C::NV; ++i) vw[i] = shfl64(row, (i * kWave + lane) / C::CPR % kFewKeys);
-    }
+    // rows from the tile's first one on (WHOLE: base and 32-bit offset), or each in the pool
+    using At = std::conditional_t<WHOLE, uint32_t, int64_t>;
+    const int64_t base = WHOLE ? row : 0;
+    const char* kp = a.pool.K + base * C::RB;
+    const char* vp = a.pool.V + base * C::RB;
+    const uint8_t* ksp = a.pool.Ks + base * (D / kScaleBlock);
+    const uint8_t* vsp = a.pool.Vs + base * (D / kScaleBlock);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      const char* p = a.pool.K + kw[kb] * C::RB + g * C::KB;
+      const At r = WHOLE ? l16 : shfl64(row, kb * 16 + l16);
+      constexpr int up = WHOLE ? 16 : 0;
 #pragma unroll
-      for (int c = 0; c < C::KN; ++c) load_piece<C::KB>(p + c * 4 * C::KB, kr[kb] + c * (C::KB / 4));
-      if (fmt_scaled(F)) ks[kb] = load_scales<D>(a.pool.Ks, kw[kb]);
+      for (int c = 0; c < C::KN; ++c)
+        load_piece<C::KB>(kp + (kb * up * C::RB + c * 4 * C::KB) + (At)(r * C::RB + g * C::KB), kr[kb] + c * (C::KB / 4));
+      if (fmt_scaled(F)) ks[kb] = load_scales<D>(ksp + kb * up * (D / kScaleBlock), r);
     }
 #pragma unroll
     for (int i = 0; i < C::NV; ++i) {
+      const int key = (i * kWave + lane) / C::CPR % kFewKeys;  // (a piece too many is the first ones' again)
+      constexpr int step = WHOLE ? kWave / C::CPR : 0;
+      const At r = WHOLE ? (lane / C::CPR) % kFewKeys : shfl64(row, key);
       if constexpr (COPY) {  // the source column makes up for the place
         const int ch = lane % C::CPR ^ C::swz((i * kWave + lane) / C::CPR);
-        copy_to_lds(a.pool.V + vw[i] * C::RB + ch * 16, __builtin_amdgcn_readfirstlane(lds_address(v_tile) + i * 1024));
+        const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(v_tile) + i * 1024);
+        if constexpr (WHOLE) copy_to_lds(vp + i * step * C::RB, r * C::RB + ch * 16, at);
+        else copy_to_lds(vp + (r * C::RB + ch * 16), at);
       } else {
-        load_piece<16>(a.pool.V + vw[i] * C::RB + lane % C::CPR * 16, vr[i]);
-        if (fmt_scaled(F)) vs[i] = load_scales<D>(a.pool.Vs, vw[i]);
+        load_piece<16>(vp + i * step * C::RB + (At)(r * C::RB + lane % C::CPR * 16), vr[i]);
+        if (fmt_scaled(F)) vs[i] = load_scales<D>(vsp + i * step * (D / kScaleBlock), r);
       }
     }
   };
@@ -650,7 +661,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
 #pragma unroll 1
       for (int key = 0; key < kFewKeys; ++key) {
         if (!kt.some(j0 + key)) continue;
-        const int64_t r = whole ? row + key : shfl64(row, key);
+        const int64_t r = WHOLE ? row + key : shfl64(row, key);
 #pragma unroll
         for (int db = 0; db < D / 16; ++db)
 #pragma unroll
@@ -712,15 +723,15 @@ struct TileCfg {
 // below 2^8, which costs no bit of their bf16 or of the fp32 sums.
 constexpr float kLazy = 8.f;
 
-template <int F, int D>
+// WHOLE: as for the kernel of few rows; 2048 tokens of 64 heads over 32768 positions of 8, D = 128,
+// take 1820 us with it and 1901 without.
+template <int F, int D, bool WHOLE>
 __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_attend_tile(AttendArgs a) {
   constexpr int W = tile_waves(D), BM = 32 * W, BN = kTileKeys;
   using C = TileCfg<F, D, W>;
   // bf16 rows are copied straight into LDS; the others pass through registers, as bf16
   constexpr bool COPY = F == kFmtBf16;
-  // K is staged two tiles ahead of its use where there is room, V one
-  constexpr int KAHEAD = COPY && D <= 128 ? 1 : 1, KBUF = 2 * KAHEAD;
-  __shared__ __attribute__((aligned(16))) char ldsK[KBUF][BN * D * 2];
+  __shared__ __attribute__((aligned(16))) char ldsK[2][BN * D * 2];
   __shared__ __attribute__((aligned(16))) char ldsV[2][BN * D * 2];
   __shared__ int32_t lds_special;
   const Place pl = place_of(a);
@@ -751,13 +762,13 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
   if (threadIdx.x == 0) lds_special = 0;
 
   bool bad = false;
-  // pages that hold whole tiles: a tile's rows follow each other
-  const bool whole = a.pool.T.d % BN == 0;
-  // the tile's key `lane` (whole: its first); its page, and its row in the pool
+  // the tile's key `lane` (WHOLE: its first); its page, and its row in the pool
   const auto key_of = [&](int32_t tt) __attribute__((always_inline)) {
-    return min(kt.tile(min(tt, kt.count - 1)) * BN + (whole ? 0 : lane), n - 1);
+    return min(kt.tile(min(tt, kt.count - 1)) * BN + (WHOLE ? 0 : lane), n - 1);
   };
-  const auto page_of = [&](int32_t tt) __attribute__((always_inline)) { return pool_page(a.pool, b, (uint32_t)key_of(tt)); };
+  const auto page_of = [&](int32_t tt) __attribute__((always_inline)) {
+    return WHOLE ? pool_page_uniform(a.pool, b, (uint32_t)key_of(tt)) : pool_page(a.pool, b, (uint32_t)key_of(tt));
+  };
   const auto row_of = [&](int32_t page, int32_t tt) __attribute__((always_inline)) {
     bool x;
     const int64_t r = pool_row(a.pool, page, (uint32_t)key_of(tt), &x) + head_row;
@@ -776,48 +787,34 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
   constexpr int STEP = 64 * W / C::CPR;
   const int col = threadIdx.x % C::CPR, block = col * C::E / kScaleBlock;
   const bool mine = C::CHUNKS >= 64 * W || (int)threadIdx.x < C::CHUNKS;  // (whole waves)
-  const auto tile_rows = [&](int64_t row, int64_t (&r)[C::NL]) __attribute__((always_inline)) {
-    if (whole) {
-#pragma unroll
-      for (int i = 0; i < C::NL; ++i) r[i] = row + (key0 + i * STEP);
-    } else {
-#pragma unroll
-      for (int i = 0; i < C::NL; ++i) r[i] = shfl64(row, key0 + i * STEP);
-    }
-  };
   // fetch: rows of a tile set out; stage: they are in LDS buffer `buf` when it is done
   // (copied rows set out with their buffer known; the source column makes up for the place)
-  const auto fetch_k = [&](int64_t row, int buf) __attribute__((always_inline)) {
-    int64_t r[C::NL];
-    tile_rows(row, r);
-    if constexpr (COPY) {
-      const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(ldsK[buf]) + wave * 1024);
+  const auto fetch = [&](const char* pages, const uint8_t* scales, int64_t row, const char* buf, auto swz, auto& x, auto& xs)
+      __attribute__((always_inline)) {
+    using At = std::conditional_t<WHOLE, uint32_t, int64_t>;
+    const int64_t base = WHOLE ? row : 0;
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(buf) + wave * 1024);
 #pragma unroll
-      for (int i = 0; i < C::NL; ++i)
-        if (mine) copy_to_lds(a.pool.K + r[i] * C::RB + 16 * (col ^ C::kswz(key0 + i * STEP)), at + i * 1024 * W);
-    } else {
-#pragma unroll
-      for (int i = 0; i < C::NL; ++i) {
-        load_piece<16>(a.pool.K + r[i] * C::RB + col * 16, kr[i]);
-        if (fmt_scaled(F)) ks[i] = load_scales<D>(a.pool.Ks, r[i]);
+    for (int i = 0; i < C::NL; ++i) {
+      const int key = key0 + i * STEP;
+      const char* p = pages + (base + (WHOLE ? i * STEP : 0)) * C::RB;
+      const At r = WHOLE ? key0 : shfl64(row, key);
+      if constexpr (COPY) {
+        const int ch = col ^ swz(key);
+        if (!mine) continue;
+        if constexpr (WHOLE) copy_to_lds(p, r * C::RB + 16 * ch, at + i * 1024 * W);
+        else copy_to_lds(p + (r * C::RB + 16 * ch), at + i * 1024 * W);
+      } else {
+        load_piece<16>(p + (At)(r * C::RB + col * 16), x[i]);
+        if (fmt_scaled(F)) xs[i] = load_scales<D>(scales + (base + (WHOLE ? i * STEP : 0)) * (D / kScaleBlock), r);
       }
     }
   };
+  const auto fetch_k = [&](int64_t row, int buf) __attribute__((always_inline)) {
+    fetch(a.pool.K, a.pool.Ks, row, ldsK[buf], [](int key) { return C::kswz(key); }, kr, ks);
+  };
   const auto fetch_v = [&](int64_t row, int buf) __attribute__((always_inline)) {
-    int64_t r[C::NL];
-    tile_rows(row, r);
-    if constexpr (COPY) {
-      const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(ldsV[buf]) + wave * 1024);
-#pragma unroll
-      for (int i = 0; i < C::NL; ++i)
-        if (mine) copy_to_lds(a.pool.V + r[i] * C::RB + 16 * (col ^ C::vswz(key0 + i * STEP)), at + i * 1024 * W);
-    } else {
-#pragma unroll
-      for (int i = 0; i < C::NL; ++i) {
-        load_piece<16>(a.pool.V + r[i] * C::RB + col * 16, vr[i]);
-        if (fmt_scaled(F)) vs[i] = load_scales<D>(a.pool.Vs, r[i]);
-      }
-    }
+    fetch(a.pool.V, a.pool.Vs, row, ldsV[buf], [](int key) { return C::vswz(key); }, vr, vs);
   };
   const auto stage_k = [&](int buf) __attribute__((always_inline)) {
     if constexpr (!COPY) {
@@ -899,21 +896,19 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
   // t + 1 are computed beside its softmax. A product takes the matrix unit 32 cycles
   // in which the vector unit is free: the source has between two products what
   // fits there, and their operands' reads two or three products ahead.
-  int64_t rows[KAHEAD];  // of the tiles t + 1, ...
-  int32_t page = 0;      // of the tile after those
+  int64_t rows;      // of tile t + 1
+  int32_t page = 0;  // of the tile after it
   const int32_t t_begin = t;
   constexpr int NS = D / 8, NP = D / 8, HALF = NP / 2;  // products for the scores, and with the weights
   // operands in flight: KA products ahead of the first kind's, VA of the second's
   constexpr int KA = D > 128 ? 3 : NS < 5 ? NS : 5, VA = D > 128 ? 2 : NP < 4 ? NP : 4;
   Bf16x8 kf[KA + 1];
   auto step = [&](auto bufc) __attribute__((always_inline)) {
-    constexpr int BUF = decltype(bufc)::value, KB = BUF % KBUF, VB = BUF % 2;  // tile t's buffers
-    // Tile t + 1's K (for KAHEAD = 2: t + 2's) and t's V are in LDS, and no wave reads
-    // what is written below.
+    constexpr int BUF = decltype(bufc)::value, NEXT = BUF ^ 1;  // tile t's buffers, and t + 1's
+    // Tile t + 1's K and t's V are in LDS, and no wave reads what is written below.
     __syncthreads();
-    if constexpr (KAHEAD == 1)
 #pragma unroll
-      for (int i = 0; i < KA; ++i) kf[i] = k_operand((KB + 1) % KBUF, i);
+    for (int i = 0; i < KA; ++i) kf[i] = k_operand(NEXT, i);
     F32x16 ahead[2];
     const auto score = [&](int i) __attribute__((always_inline)) {  // the i-th product of tile t + 1's scores
       const int kb = i / (D / 16), kk = i % (D / 16);
@@ -921,8 +916,8 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
     };
     Bf16x8 vf[VA + 1];
     const auto operand = [&](int i) __attribute__((always_inline)) {  // of the scores' i-th product, then of the weights' first ones
-      if (i < NS) kf[i % (KA + 1)] = k_operand((KB + 1) % KBUF, i);
-      else if (i - NS < VA) vf[i - NS] = v_operand(VB, i - NS);
+      if (i < NS) kf[i % (KA + 1)] = k_operand(NEXT, i);
+      else if (i - NS < VA) vf[i - NS] = v_operand(BUF, i - NS);
     };
     // The first products need nothing of tile t: its mask, its maximum and the next
     // tiles' loads go beside them.
@@ -934,10 +929,10 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
       operand(i + KA);
       score(i);
     }
-    const int64_t later = row_of(page, t + KAHEAD + 1);
-    page = page_of(t + KAHEAD + 2);  // a step before it is needed, and before the copies: nothing waits for it, or for them with it
-    fetch_k(later, (KB + KAHEAD + 1) % KBUF);
-    if constexpr (BOTH) fetch_v(rows[0], VB ^ 1);
+    const int64_t later = row_of(page, t + 2);
+    page = page_of(t + 3);  // a step before it is needed, and before the copies: nothing waits for it, or for them with it
+    fetch_k(later, BUF);
+    if constexpr (BOTH) fetch_v(rows, NEXT);
     const int32_t j0 = kt.tile(t) * BN;
     if (!all_see(j0, j0 + BN, pw_lo, pw_hi, n, a.window, a.sinks)) {
       const Limits in(j0 + 4 * h, pos, n, a.window, a.sinks);
@@ -981,14 +976,13 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
       __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (!BOTH) {
-      stage_k((KB + KAHEAD + 1) % KBUF);
-      fetch_v(rows[0], VB ^ 1);
+      stage_k(BUF);
+      fetch_v(rows, NEXT);
     }
     float biggest = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      if (i + VA < NP) vf[(i + VA) % (VA + 1)] = v_operand(VB, i + VA);
-      else if (KAHEAD == 2 && i + VA - NP < KA) kf[i + VA - NP] = k_operand((KB + 2) % KBUF, i + VA - NP);
+      if (i + VA < NP) vf[(i + VA) % (VA + 1)] = v_operand(BUF, i + VA);
       const int ks4 = i / (D / 32), db = i % (D / 32);
       o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % (VA + 1)], w[ks4], o[db], 0, 0, 0);
       if (i < HALF) {
@@ -999,34 +993,25 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (KAHEAD == 2)
-#pragma unroll
-      for (int i = VA < KA ? VA : KA; i < KA; ++i) kf[i] = k_operand((KB + 2) % KBUF, i);
     __builtin_amdgcn_s_setprio(0);
-    if constexpr (BOTH) stage_k((KB + KAHEAD + 1) % KBUF);
-    stage_v(t + 1, VB ^ 1);
+    if constexpr (BOTH) stage_k(BUF);
+    stage_v(t + 1, NEXT);
     s[0] = ahead[0], s[1] = ahead[1];
     most = biggest;
-#pragma unroll
-    for (int i = 0; i + 1 < KAHEAD; ++i) rows[i] = rows[i + 1];
-    rows[KAHEAD - 1] = later;
+    rows = later;
     ++t;
   };
   if (t < t_end) {
     // tiles past the last are read as the last again, and not used
-    int32_t pages[KAHEAD + 1];
-#pragma unroll
-    for (int i = 0; i <= KAHEAD; ++i) pages[i] = page_of(t + i);
-    page = page_of(t + KAHEAD + 1);
-    const int64_t here = row_of(pages[0], t);
-#pragma unroll
-    for (int i = 0; i < KAHEAD; ++i) rows[i] = row_of(pages[i + 1], t + 1 + i);
+    const int32_t first = page_of(t), second = page_of(t + 1);
+    page = page_of(t + 2);
+    const int64_t here = row_of(first, t);
+    rows = row_of(second, t + 1);
     __syncthreads();  // lds_special is set
-#pragma unroll
-    for (int i = 0; i <= KAHEAD; ++i) {
-      fetch_k(i == 0 ? here : rows[i - 1], i);
-      stage_k(i);
-    }
+    fetch_k(here, 0);
+    stage_k(0);
+    fetch_k(rows, 1);
+    stage_k(1);
     fetch_v(here, 0);
     const char* q_at = a.q + 2 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + qr - tok * a.G) * a.q_h + (int64_t)tok * a.q_m);
 #pragma unroll
@@ -1039,20 +1024,11 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
       s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(0, i), q[kk], kk == 0 ? F32x16{} : s[kb], 0, 0, 0);
     }
     most = largest(s, 0, 16, -INFINITY);
-    if constexpr (KAHEAD == 2)
-#pragma unroll
-      for (int i = 0; i < KA; ++i) kf[i] = k_operand(1, i);
     for (;;) {
       step(std::integral_constant<int, 0>());
       if (t >= t_end) break;
       step(std::integral_constant<int, 1>());
       if (t >= t_end) break;
-      if constexpr (KBUF == 4) {
-        step(std::integral_constant<int, 2>());
-        if (t >= t_end) break;
-        step(std::integral_constant<int, 3>());
-        if (t >= t_end) break;
-      }
     }
     __syncthreads();
     if (lds_special) {
@@ -1064,7 +1040,7 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
 #pragma unroll 1
         for (int key = 0; key < BN; ++key) {
           if (!kt.some(j0 + key)) continue;
-          const int64_t r = whole ? tile_row + key : shfl64(tile_row, key);
+          const int64_t r = WHOLE ? tile_row + key : shfl64(tile_row, key);
 #pragma unroll
           for (int db = 0; db < D / 32; ++db)
 #pragma unroll

@@ -40,6 +40,13 @@ __device__ __forceinline__ int32_t pool_page(const Pool& p, int b, uint32_t j) {
   return p.table ? p.table[(int64_t)b * p.cols + fast_div(j, p.T)] : b;
 }
 
+// The same where j is the same in all lanes: a scalar load (the table is not written meanwhile).
+__device__ __forceinline__ int32_t pool_page_uniform(const Pool& p, int b, uint32_t j) {
+  if (!p.table) return b;
+  typedef const int32_t __attribute__((address_space(4))) * Constant;
+  return *(Constant)(uintptr_t)(p.table + ((int64_t)b * p.cols + fast_div(j, p.T)));
+}
+
 // Row of position j, which lies in that page, counted from the pool's first within
 // the first (layer, head); add (layer * H + head) * T. *bad: there is no such page
 // (page 0 is taken in its place).
