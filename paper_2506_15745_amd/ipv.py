@@ -564,11 +564,12 @@ def _table(pool, table, streams):
     """(pointer, columns) of a page table [B, cols], or of none (stream b's rows are page b)."""
     if table is None:
         return None, 1
-    if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != streams:
+    shape = table.shape
+    if table.dtype is not torch.int32 or len(shape) != 2 or shape[0] != streams:
         raise IpvError(ERR_SHAPE, "page_table must be int32 [%d, columns]" % streams)
-    if table.get_device() != pool.K.get_device():
+    if table.get_device() != pool._dev:
         raise IpvError(ERR_ARG, "page_table is on %s, the pool on %s" % (table.device, pool.device))
-    return _ptr(table), table.shape[1]
+    return _ptr(table), shape[1]
 
 
 @functools.lru_cache(maxsize=256)
@@ -614,8 +615,8 @@ def _page_rows(name, pool, page_table, first_row, K, V, ws, rows, first_layer, r
     if V.dtype is not K.dtype:
         raise IpvError(ERR_DTYPE, "K and V must have one dtype")
     B, L, _, N, D = shape
-    strides = _stride_array(K.stride(), shape)
-    if V.stride() != K.stride() and list(_stride_array(V.stride(), shape)) != list(strides):
+    strides = _stride_array(k_strides := K.stride(), shape)
+    if V.stride() != k_strides and list(_stride_array(V.stride(), shape)) != list(strides):
         raise IpvError(ERR_SHAPE, "K and V must have the same strides")
     if rows is None:
         rows = N
@@ -633,7 +634,7 @@ def _page_rows(name, pool, page_table, first_row, K, V, ws, rows, first_layer, r
     first, counts_ = _host_counts(first_row, B, "first_row"), _host_counts(rows, B, "rows")
     rc = getattr(_paged(), name)(*pool._args, table, cols, B, first.buffer_info()[0], counts_.buffer_info()[0], first_layer, L,
                                  K.data_ptr(), V.data_ptr(), _dtype_code(K), strides,
-                                 None if rotary is None else _ptr(rotary), angles, _ptr(ws), _ws_bytes(ws), _stream(stream))
+                                 None if rotary is None else _ptr(rotary), angles, _ptr(ws), ws.nbytes, _stream(stream))
     if rc != OK:
         _check(rc, name)
 
@@ -676,11 +677,12 @@ def ipv_attend(pool, page_table, n_tokens, q_first, layer, q, out, ws, q_rows=No
         _same_gpu(pool, ws, q=q, out=out)
     n, first = _host_counts(n_tokens, B, "n_tokens"), _host_counts(q_first, B, "q_first")
     rows = _host_counts(M if q_rows is None else q_rows, B, "q_rows")
+    q_strides, out_strides = q.stride(), out.stride()
+    q_at = _stride_array(q_strides, shape)
     rc = _paged().ipv_attend(*pool._args, table, cols, B, n.buffer_info()[0], first.buffer_info()[0], rows.buffer_info()[0],
-                             layer, q.data_ptr(), _stride_array(q.stride(), shape), A, M,
-                             D ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(),
-                             _stride_array(out.stride(), shape), None if lse is None else _ptr(lse), _ptr(ws), _ws_bytes(ws),
-                             _stream(stream))
+                             layer, q.data_ptr(), q_at, A, M, D ** -0.5 if scale is None else scale, window, sinks,
+                             out.data_ptr(), q_at if out_strides == q_strides else _stride_array(out_strides, shape),
+                             None if lse is None else _ptr(lse), _ptr(ws), ws.nbytes, _stream(stream))
     if rc != OK:
         _check(rc, "ipv_attend")
 
