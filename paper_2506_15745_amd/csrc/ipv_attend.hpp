@@ -1093,7 +1093,10 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
 // straight from the caches into its operands, without LDS. Its operands take one
 // element a lane: half h of the wave holds the elements h * D / 2 + k of a key, and
 // S^T leaves the weights as the second product's operand as they stand.
-template <int D>
+// Chunks are bound by that instruction, single tokens by the cache's bytes: 512 tokens of 64 heads over
+// 4096 positions of 8, D = 128, 604 us, 107 TFLOP/s (the library's product of such sizes: 154);
+// one token of 8 streams over 32768 positions 400 us, 5.4 TB/s.
+template <int D, bool WHOLE>
 __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(AttendArgs a) {
   constexpr int BN = 32;
   __shared__ __attribute__((aligned(16))) char lds[kFewWaves][JoinLds<D, 32>::kWaveBytes];
@@ -1125,37 +1128,67 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = F32x16{};
   bool bad = false, special = false;
-  auto row_of = [&](int32_t t) __attribute__((always_inline)) {  // the pool's row of the tile's key l32
+  auto row_of = [&](int32_t t) __attribute__((always_inline)) {  // the pool's row of the tile's key l32 (WHOLE: its first)
     bool x;
-    const uint32_t j = (uint32_t)min(kt.tile(t) * BN + l32, n - 1);
-    const int64_t at = pool_row(a.pool, pool_page(a.pool, b, j), j, &x) + head_row;
+    const uint32_t j = (uint32_t)min(kt.tile(min(t, kt.count - 1)) * BN + (WHOLE ? 0 : l32), n - 1);
+    const int32_t page = WHOLE ? pool_page_uniform(a.pool, b, j) : pool_page(a.pool, b, j);
+    const int64_t at = pool_row(a.pool, page, j, &x) + head_row;
     bad |= x;
     return at;
   };
+  // K in pieces of four elements, KA of them in registers: all of a row's up to D = 128. With one
+  // wave a SIMD (D > 64) the next tile's are on their way while V is used: 512 tokens of 64 heads
+  // over 4096 positions of 8, D = 128, take 604 us with that and 825 without. Where two share it
+  // they cover for each other, and loads ahead only hold them up: 357 us with it and 321 without, D = 64.
+  constexpr bool AHEAD = D > 64;
+  using At = std::conditional_t<WHOLE, uint32_t, int64_t>;
+  constexpr int KA = D <= 128 ? D / 8 : 8;
+  F32x4 kx[KA];
+  const auto load_k = [&](int64_t row, int k) __attribute__((always_inline)) {
+    const char* base = a.pool.K + (WHOLE ? row * D * 4 : 0);
+    kx[k % KA] = *reinterpret_cast<const F32x4*>(base + 16 * k + (At)((WHOLE ? (At)l32 : (At)row) * D * 4 + h * D * 2));
+  };
+  // V's rows (all of them up to D = 128, else four keys ahead) are on their way while the
+  // scores are computed
+  constexpr int VA = D <= 128 ? 16 : 4;
+  float vx[VA][D / 32];
+  int64_t row = 0;
+  if (t_begin < t_end) {
+    row = row_of(t_begin);
+    if constexpr (AHEAD)
+#pragma unroll
+      for (int k = 0; k < KA; ++k) load_k(row, k);
+  }
   for (int32_t t = t_begin; t < t_end; t += kFewWaves) {
     const int32_t j0 = kt.tile(t) * BN;
-    const int64_t row = row_of(t);
+    const int64_t next = row_of(t + kFewWaves);
+    if constexpr (!AHEAD)
+#pragma unroll
+      for (int k = 0; k < KA; ++k) load_k(row, k);
     const bool full = all_see(j0, j0 + BN, p_lo, p_hi, n, a.window, a.sinks);
-    const F32x4* ka = reinterpret_cast<const F32x4*>(a.pool.K + 4 * (row * D + h * (D / 2)));
-    F32x4 kx[D / 8];
+    const auto load_v = [&](int i) __attribute__((always_inline)) {
+      const int key = 8 * (i / 4) + i % 4;  // (+ 4 h)
+      const char* base = a.pool.V + (WHOLE ? (row + key) * D * 4 : 0);
+      const At at = WHOLE ? (At)(4 * h * D * 4) : (At)(shfl64(row, key + 4 * h) * D * 4);
 #pragma unroll
-    for (int k = 0; k < D / 8; ++k) kx[k] = ka[k];
-    // V's rows are on their way while the scores are computed (up to D = 128)
-    constexpr bool EARLY = D <= 128;
-    float vx[EARLY ? 16 : 1][D / 32];
-    const auto load_v = [&](int i, float (&v)[D / 32]) __attribute__((always_inline)) {
-      const float* va = reinterpret_cast<const float*>(a.pool.V) + shfl64(row, 8 * (i / 4) + 4 * h + i % 4) * D + l32;
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) v[db] = va[32 * db];
+      for (int db = 0; db < D / 32; ++db) vx[i % VA][db] = *reinterpret_cast<const float*>(base + 128 * db + (At)(at + 4 * l32));
     };
-    if constexpr (EARLY)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) load_v(i, vx[i]);
+    for (int i = 0; i < VA; ++i) load_v(i);
+    if constexpr (AHEAD) __builtin_amdgcn_sched_barrier(0);
     F32x16 s = {};
 #pragma unroll
-    for (int k = 0; k < D / 8; ++k)
+    for (int k = 0; k < D / 8; ++k) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kx[k][i], q[4 * k + i], s, 0, 0, 0);
+      for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kx[k % KA][i], q[4 * k + i], s, 0, 0, 0);
+      if (k + KA < D / 8) load_k(row, k + KA);
+    }
+    if constexpr (AHEAD) __builtin_amdgcn_sched_barrier(0);
+    if (AHEAD && t + kFewWaves < t_end) {
+#pragma unroll
+      for (int k = 0; k < KA; ++k) load_k(next, k);
+    }
+    if constexpr (AHEAD) __builtin_amdgcn_sched_barrier(0);
     if (!full) {
       const Limits in(j0 + 4 * h, pos, n, a.window, a.sinks);
 #pragma unroll
@@ -1175,8 +1208,7 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(
     for (int i = 0; i < 16; ++i) {
       const float e = exp2_hw(__builtin_fmaf(s[i], a.c, -shift));
       l += e;
-      if constexpr (!EARLY) load_v(i, vx[0]);
-      float(&v)[D / 32] = vx[EARLY ? i : 0];
+      float(&v)[D / 32] = vx[i % VA];
       if (!full) {  // as in the other kernels: nothing of rows that nobody sees, infinities and NaN at the end
         const bool some = kt.some(j0 + 8 * (i / 4) + 4 * h + i % 4);
 #pragma unroll
@@ -1187,7 +1219,9 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(
       }
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[db], e, o[db], 0, 0, 0);
+      if (i + VA < 16) load_v(i + VA);
     }
+    row = next;
   }
   if (__ballot(special) != 0) {
 #pragma unroll 1
@@ -1197,7 +1231,7 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(
       const int64_t row = row_of(t);
 #pragma unroll 1
       for (int key = 0; key < BN; ++key) {
-        const int64_t rv = shfl64(row, key);
+        const int64_t rv = WHOLE ? row + key : shfl64(row, key);
         if (!kt.some(j0 + key)) continue;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
