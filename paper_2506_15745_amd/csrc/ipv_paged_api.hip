@@ -186,9 +186,27 @@ ipv_status check_heads(const ipv_page_shape* s, int32_t streams, int32_t q_heads
 // the first workgroup of each. A key range is split when the row tiles alone
 // leave the card unfilled, into parts of about equal length that give about as many
 // workgroups as it holds (few: at least a tile for each wave).
+// What `blocks` workgroups of `per` key tiles take, `fill` of them at once, where row tiles are in `splits`
+// parts: us, as measured. A workgroup costs its tiles and, around them, its start, the wait for its
+// first rows and the store of its part; the joining costs a launch and the parts' bytes; of fp32 parts,
+// trips of the last workgroup, 16 parts at a time. A last round that does not fill the card costs a
+// whole one, but for bf16 heads of 128: a full card lowers its clock for their products.
+// Against parts only where they fit in one round: 300 tokens of 64 heads of 256 over 8192 positions
+// 319 -> 240 us, 600 of 64 heads of 64 145 -> 122, 1100 of 64 heads of 128 372 -> 329; fp32, 300 tokens of 28 heads of
+// 128 over 6272, 460 -> 336.
+double attend_us(AttendKind kind, int D, int64_t per, int64_t blocks, int32_t fill, int64_t splits) {
+  const int size = D == 32 ? 0 : D == 64 ? 1 : D == 128 ? 2 : 3;
+  static constexpr double kTileUs[4] = {0.8, 1.06, 1.8, 2.4}, kF32Us[4] = {0.67, 1.35, 1.2, 2.7};
+  const int64_t whole = blocks / fill, rounds = (blocks + fill - 1) / fill;
+  if (kind == kF32)
+    return rounds * (per * kF32Us[size] + 5 + D / 32.0) + (splits > 1 ? 2 + D / 32.0 * (double)((splits + 15) / 16) : 0);
+  const double rest = (double)(blocks % fill) / fill, last = D != 128 ? 1 : whole == 0 ? 0.6 + 0.3 * rest : 0.5 + 0.45 * rest * rest;
+  const double part = attend_rows(kind, D) * D / 32768.0 * blocks;  // bytes of all parts, of 256 rows of 128
+  return (whole + (rest > 0 ? last : 0)) * per * kTileUs[size] + 13 + 8 * (rounds - 1) + (splits > 1 ? 3.5 + 0.015 * part : 0);
+}
+
 void plan(AttendArgs* a, AttendKind kind, int D, int format) {
   const int32_t BM = attend_rows(kind, D), BN = attend_keys(kind);
-  const bool few = kind != kTile;  // waves share a workgroup's keys
   int64_t base = 0, work = 0;
   int32_t count[kAttendStreams];
   for (int32_t i = 0; i < a->streams; ++i) {
@@ -202,20 +220,36 @@ void plan(AttendArgs* a, AttendKind kind, int D, int format) {
     work += (int64_t)a->H * s.tiles * count[i];
   }
   const int32_t fill = attend_fill(kind, D, format);
-  if (base < fill) {
-    // parts of `per` tiles: the shortest that make no more workgroups than fit at once
-    // (waves that share a workgroup's keys: and no shorter than a square root of the range, where a
-    // step of four tiles, 0.65 us, costs what the parts it saves cost the last workgroup, 0.1 us each)
-    const int64_t unit = few ? kFewWaves : 1;
-    const int64_t least = few ? std::max<int64_t>(kFewWaves, (int64_t)std::sqrt(0.6 * *std::max_element(count, count + a->streams))) : 2;
-    int64_t per = std::max<int64_t>((work + fill - 1) / fill, least);
+  const int32_t longest = *std::max_element(count, count + a->streams);
+  const int64_t unit = kind == kTile ? 1 : kFewWaves;  // waves that share a workgroup's keys
+  // splits for parts of `per` tiles; the workgroups
+  const auto split = [&](int64_t per) {
+    int64_t blocks = 0;
+    for (int32_t i = 0; i < a->streams; ++i) {
+      a->s[i].splits = (int32_t)std::min<int64_t>(std::max<int64_t>((count[i] + per - 1) / per, 1), kMaxSplits);
+      blocks += (int64_t)a->H * a->s[i].tiles * a->s[i].splits;
+    }
+    return blocks;
+  };
+  if (kind == kTile || kind == kF32) {
+    // Bound by computing: as many parts as the model below finds fastest.
+    int64_t best = std::max(longest, 1);
+    double least = 0;
+    for (int64_t parts = 1; parts <= kMaxSplits && (parts == 1 || base * parts <= std::min<int64_t>(4 * fill, kMaxParts)); ++parts) {
+      const int64_t per = ((std::max<int64_t>(longest, 1) + parts - 1) / parts + unit - 1) / unit * unit, blocks = split(per);
+      if (parts > 1 && (per < 2 || blocks > kMaxParts)) break;
+      const double us = attend_us(kind, D, per, blocks, fill, blocks > base ? parts : 1);
+      if (parts == 1 || us < least) least = parts == 1 ? 0.96 * us : us, best = per;  // (no parts for the model's error's sake)
+    }
+    split(best);
+  } else if (base < fill) {
+    // Bound by loading: parts of `per` tiles, the shortest that make no more workgroups than fit at once, and
+    // no shorter than a square root of the range, where a step of four tiles, 0.65 us, costs what the
+    // parts it saves cost the last workgroup, 0.1 us each.
+    int64_t per = std::max<int64_t>({(work + fill - 1) / fill, kFewWaves, (int64_t)std::sqrt(0.6 * longest)});
     per = (per + unit - 1) / unit * unit;
     for (;; per += std::max(unit, per / 16 / unit * unit)) {
-      int64_t blocks = 0;
-      for (int32_t i = 0; i < a->streams; ++i) {
-        a->s[i].splits = (int32_t)std::min<int64_t>(std::max<int64_t>((count[i] + per - 1) / per, 1), kMaxSplits);
-        blocks += (int64_t)a->H * a->s[i].tiles * a->s[i].splits;
-      }
+      const int64_t blocks = split(per);
       if (blocks <= fill || blocks == base) break;
     }
   }

@@ -255,3 +255,36 @@ def test_a_table_entry_outside_the_pool_is_reported():
             ipv.ipv_clear_device_errors(ws)
             ipv.ipv_attend(pool, table, 90, 90 - m, 0, q, out, ws)
             assert ipv.ipv_read_device_errors(ws) == 0
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D", [32, 64, 128, 256])
+@pytest.mark.parametrize("T", [64, 192])
+@pytest.mark.parametrize("G,m,window,sinks", [(1, 1, 0, 0), (5, 1, 90, 3), (2, 9, 0, 0), (3, 11, 70, 33), (8, 40, 0, 0), (1, 133, 100, 1)])
+def test_pages_of_whole_tiles(fmt, D, T, G, m, window, sinks):
+    """A tile's rows follow each other in a page, whose rows past the last are not zeros."""
+    B, L, H, n = 2, 2, 2, [413, 192]
+    pool = R.filled_pool(fmt, 20, L, H, T, D, D + G)
+    table = R.shuffled_table(B, 7, 20, m)
+    check(fmt, pool, table, n, [x - m for x in n], 1, queries(fmt, B, H * G, m, D, 3, token_major=G == 3), window, sinks)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T", [100, 128])
+@pytest.mark.parametrize("G,m", [(1, 1), (2, 13), (1, 40), (2, 300)])
+def test_key_range_in_many_parts(fmt, T, G, m):
+    """One KV head: more parts than are joined in one go."""
+    n = 9000
+    pool = R.filled_pool(fmt, 95, 1, 1, T, 128, 2)
+    table = R.shuffled_table(1, 92, 95, m)
+    check(fmt, pool, table, [n], [n - m], 0, queries(fmt, 1, G, m, 128, 3))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "f32"])
+@pytest.mark.parametrize("B,m", [(1, 300), (5, 140), (12, 40)])
+def test_parts_beyond_one_round(fmt, B, m):
+    """Row tiles that fill a part of the card: key ranges in parts that take it more than once."""
+    H, G, D, n = 8, 8, 128, [700 + 100 * b for b in range(B)]
+    pool = R.filled_pool(fmt, 30 * B, 1, H, 64, D, 2)
+    table = R.shuffled_table(B, 30, 30 * B, m)
+    check(fmt, pool, table, n, [x - m for x in n], 0, queries(fmt, B, H * G, m, D, 3))
