@@ -288,3 +288,29 @@ def test_parts_beyond_one_round(fmt, B, m):
     pool = R.filled_pool(fmt, 30 * B, 1, H, 64, D, 2)
     table = R.shuffled_table(B, 30, 30 * B, m)
     check(fmt, pool, table, n, [x - m for x in n], 0, queries(fmt, B, H * G, m, D, 3))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D", [32, 64, 128, 256])
+@pytest.mark.parametrize("m", [1, 6, 40])
+def test_what_is_not_seen_stays_out_of_whole_tiles(fmt, D, m):
+    """The same in pages that hold whole tiles, which are read to their last row; and an entry outside the pool."""
+    n, T, G, window, sinks = 300, 64, 4, 50, 3
+    pool = R.filled_pool(fmt, 8, 1, 1, T, D, 8)
+    table = R.shuffled_table(1, 6, 8, 9)
+    dirty = [(r, 0) for r in range(n, 6 * T)] + [(r, r) for r in range(sinks, n - m - window)]
+    dirty += [(n - 1, 1)] * (m > 1)  # the last query alone sees this one
+    for row, kind in dirty:
+        at = (int(table[0, row // T]), 0, 0, row % T)
+        if fmt in ("bf16", "f32"):
+            pool.K[at], pool.V[at] = (0.5 if row == n - 1 else math.nan), (math.nan, math.inf, -math.inf)[kind % 3]
+        else:
+            pool.K_scales[at] = pool.V_scales[at] = 255
+    q = queries(fmt, 1, G, m, D, 10)
+    check(fmt, pool, table, [n], [n - m], 0, q, window, sinks)
+    ws = ipv.alloc_attend_workspace(pool, 1, G, m)
+    for entry in (8, -1, 1 << 30):
+        table[0, 4] = entry
+        ipv.ipv_attend(pool, table, n, n - m, 0, q, torch.empty_like(q), ws)
+        assert ipv.ipv_read_device_errors(ws) == ipv.DEV_BAD_PAGE
+        ipv.ipv_clear_device_errors(ws)
