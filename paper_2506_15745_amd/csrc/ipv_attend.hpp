@@ -25,6 +25,10 @@ namespace ipv {
 
 constexpr int kAttendStreams = 64;  // streams of one launch (their counts travel in its arguments)
 constexpr int kMaxSplits = 64;      // parts of a key range that are joined: a lane each
+// The last workgroup of a row tile takes a trip for 1024 elements of up to 16 parts; beyond kJoinTrips
+// of them a launch joins the parts.
+constexpr int kJoinTrips = 2;
+constexpr int64_t join_rounds(int64_t rows, int D) { return (rows * D + 1023) / 1024; }
 
 struct AttendStream {
   int32_t n, first, rows;  // rows of the cache; position of the first query; queries
@@ -49,6 +53,7 @@ struct AttendArgs {
   uint32_t* err;
   uint32_t* arrived;  // workgroups of a row tile that have left their part: zero before and after a call
   int32_t streams, blocks;
+  int32_t join_apart;  // parts are joined by a launch of its own, not by the last workgroup
   AttendStream s[kAttendStreams];
 };
 
@@ -296,8 +301,12 @@ __device__ __forceinline__ uint32_t lds_address(const char* p) {
 // Up to 16 * NB rows a KV head (single tokens of grouped heads): bound by the
 // bytes of the cache. Each wave takes key tiles of its own (32 rows), K straight
 // into the matrix operand's layout, V through an LDS tile that only this wave
-// uses (bf16: copied there, two tiles in turn); the next tile's rows are in flight while one is computed. The four waves
-// join through LDS, the splits of a key range through k_attend_join.
+// uses (bf16: copied there, two tiles in turn); the next tile's rows are in flight
+// while one is computed. The four waves join through LDS; parts of a key range through
+// memory, by the last workgroup to come or, where that takes it long, by k_attend_join.
+// One token of 8 streams over 32768 positions of 8 heads of 128: 184 us in bf16 (5.8 TB/s),
+// 106 in fp8 (5.2), 53 in fp4 (5.4); of one stream, where the start, the first rows' way and
+// the join weigh, 28 us (4.8 TB/s) in bf16 and 16 in fp4.
 constexpr int kFewWaves = 4;
 constexpr int kFewKeys = 32;
 
@@ -379,7 +388,8 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendStre
       row_out<D, F32OUT>(a, b, pl.h, r0 + r, d, v, top, sum);
     }
   }
-  if (st.splits <= 1) return;
+  if (st.splits <= 1 || a.join_apart) return;
+  if (!F32OUT && NR > 16 && join_rounds(17, D) > kJoinTrips) return;  // (as many rows always are)
 
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's parts are written
   __syncthreads();
@@ -702,7 +712,14 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
 // ---------------------------------------------------------------- many rows
 // Row tiles of 32 rows a wave, keys in tiles of 64 through LDS, where all waves
 // read them; the next tiles' rows are in flight meanwhile. Two waves a SIMD, or one
-// for D = 256, whose sums and queries alone take 192 registers.
+// for D = 256, whose sums and queries alone take 192 registers. Bound by the matrix
+// unit, at a clock that its load lowers: 2048 tokens of 64 heads over 32768 positions of 8,
+// D = 128, take 1820 us, 1170 TFLOP/s at 60% of the unit's cycles and 1.86 GHz (the library's
+// product of random bf16 matrices reaches 1490); fp8 1890, fp4 1805; D = 64 in half the
+// operations 850 TFLOP/s, where the softmax's instructions weigh twice, D = 256 880.
+// 128 rows a workgroup, two of them a CU: 2045 us. Short calls are bound by the way to
+// their first rows and back: a frame of 196 tokens of 28 heads over 6272 positions 33.5 us and
+// 7.5 for the join, of 12 at the library product's rate.
 constexpr int kTileKeys = 64;
 __host__ __device__ constexpr int tile_waves(int D) { return D <= 128 ? 8 : 4; }
 
@@ -1263,10 +1280,11 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(
   join_parts<D, 32, true>(a, st, pl, b, r0, min(R - r0, 32), lds, lds_ml, &lds_last);
 }
 
-// ---------------------------------------------------------------- joining splits of many rows
+// ---------------------------------------------------------------- joining parts by a launch
 // One wave a row: lane s has split s's maximum and sum, then every lane a part
-// of the row's elements over the splits in order.
-template <int D>
+// of the row's elements over the splits in order. Bound by the parts' bytes, which come from
+// other XCDs: 28 heads of 196 rows of 128 in 10 parts (28 MB) 7.5 us, 3.8 TB/s.
+template <int D, bool F32OUT>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int32_t BM) {
   const AttendStream st = a.s[blockIdx.y];
   if (st.splits <= 1) return;
@@ -1307,7 +1325,10 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int32_t BM) {
   const int64_t b = a.b0 + blockIdx.y, at = b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m + lane * E;
   if (lane * E < D) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) reinterpret_cast<__bf16*>(a.out)[at + e] = (__bf16)(v[e] * inv);  // (one store)
+    for (int e = 0; e < E; ++e) {  // (one store)
+      if constexpr (F32OUT) reinterpret_cast<float*>(a.out)[at + e] = v[e] * inv;
+      else reinterpret_cast<__bf16*>(a.out)[at + e] = (__bf16)(v[e] * inv);
+    }
   }
   if (lane == 0 && a.lse)
     a.lse[(b * (a.H * a.G) + head) * a.max_rows + tok] = sum == 0.f ? -INFINITY : (top + log2_hw(sum)) * kLn2;
@@ -1318,7 +1339,6 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int32_t BM) {
 enum AttendKind { kFew1, kFew2, kTile, kF32 };
 template <int F>
 hipError_t launch_attend(int D, AttendKind kind, uint32_t grid, const AttendArgs& a, hipStream_t st);
-hipError_t launch_join(int D, uint32_t rows, int32_t BM, const AttendArgs& a, hipStream_t st);
 inline int attend_rows(AttendKind k, int D) { return k == kFew1 ? 16 : k == kFew2 || k == kF32 ? 32 : 32 * tile_waves(D); }
 inline int attend_keys(AttendKind k) { return k == kTile ? kTileKeys : 32; }
 

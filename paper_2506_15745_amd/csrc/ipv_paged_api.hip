@@ -182,29 +182,25 @@ ipv_status check_heads(const ipv_page_shape* s, int32_t streams, int32_t q_heads
   return IPV_OK;
 }
 
-// The split of one launch's streams: row tiles, parts of the key ranges, and
-// the first workgroup of each. A key range is split when the row tiles alone
-// leave the card unfilled, into parts of about equal length that give about as many
-// workgroups as it holds (few: at least a tile for each wave).
-// What `blocks` workgroups of `per` key tiles take, `fill` of them at once, where row tiles are in `splits`
-// parts: us, as measured. A workgroup costs its tiles and, around them, its start, the wait for its
-// first rows and the store of its part; the joining costs a launch and the parts' bytes; of fp32 parts,
-// trips of the last workgroup, 16 parts at a time. A last round that does not fill the card costs a
-// whole one, but for bf16 heads of 128: a full card lowers its clock for their products.
+// What `blocks` workgroups of `per` key tiles take, `fill` of them at once, us, as measured. A workgroup
+// costs its tiles and, around them, its start, the wait for its first rows and the store of its
+// result or part; joining parts costs a launch and their bytes. A last round that does not fill the
+// card costs a whole one, but for bf16 heads of 128: a full card lowers its clock for their products.
 // Against parts only where they fit in one round: 300 tokens of 64 heads of 256 over 8192 positions
-// 319 -> 240 us, 600 of 64 heads of 64 145 -> 122, 1100 of 64 heads of 128 372 -> 329; fp32, 300 tokens of 28 heads of
-// 128 over 6272, 460 -> 336.
-double attend_us(AttendKind kind, int D, int64_t per, int64_t blocks, int32_t fill, int64_t splits) {
+// 319 -> 240 us, 600 of 64 heads of 64 145 -> 122, 1100 of 64 heads of 128 372 -> 329; fp32, 300 tokens
+// of 28 heads of 128 over 6272, 460 -> 331.
+double attend_us(AttendKind kind, int D, int64_t per, int64_t blocks, int32_t fill, bool parts) {
   const int size = D == 32 ? 0 : D == 64 ? 1 : D == 128 ? 2 : 3;
   static constexpr double kTileUs[4] = {0.8, 1.06, 1.8, 2.4}, kF32Us[4] = {0.67, 1.35, 1.2, 2.7};
   const int64_t whole = blocks / fill, rounds = (blocks + fill - 1) / fill;
-  if (kind == kF32)
-    return rounds * (per * kF32Us[size] + 5 + D / 32.0) + (splits > 1 ? 2 + D / 32.0 * (double)((splits + 15) / 16) : 0);
   const double rest = (double)(blocks % fill) / fill, last = D != 128 ? 1 : whole == 0 ? 0.6 + 0.3 * rest : 0.5 + 0.45 * rest * rest;
-  const double part = attend_rows(kind, D) * D / 32768.0 * blocks;  // bytes of all parts, of 256 rows of 128
-  return (whole + (rest > 0 ? last : 0)) * per * kTileUs[size] + 13 + 8 * (rounds - 1) + (splits > 1 ? 3.5 + 0.015 * part : 0);
+  const double joins = parts ? 3.5 + 0.015 * attend_rows(kind, D) * D / 32768 * blocks : 0;
+  if (kind == kF32) return rounds * (per * kF32Us[size] + 5 + D / 32.0) + joins;
+  return (whole + (rest > 0 ? last : 0)) * per * kTileUs[size] + 13 + 8 * (rounds - 1) + joins;
 }
 
+// The split of one launch's streams: row tiles, parts of the key ranges, and the first workgroup of
+// each. A key range is split when the row tiles alone leave the card, or its last round, unfilled.
 void plan(AttendArgs* a, AttendKind kind, int D, int format) {
   const int32_t BM = attend_rows(kind, D), BN = attend_keys(kind);
   int64_t base = 0, work = 0;
@@ -238,15 +234,15 @@ void plan(AttendArgs* a, AttendKind kind, int D, int format) {
     for (int64_t parts = 1; parts <= kMaxSplits && (parts == 1 || base * parts <= std::min<int64_t>(4 * fill, kMaxParts)); ++parts) {
       const int64_t per = ((std::max<int64_t>(longest, 1) + parts - 1) / parts + unit - 1) / unit * unit, blocks = split(per);
       if (parts > 1 && (per < 2 || blocks > kMaxParts)) break;
-      const double us = attend_us(kind, D, per, blocks, fill, blocks > base ? parts : 1);
+      const double us = attend_us(kind, D, per, blocks, fill, blocks > base);
       if (parts == 1 || us < least) least = parts == 1 ? 0.96 * us : us, best = per;  // (no parts for the model's error's sake)
     }
     split(best);
   } else if (base < fill) {
-    // Bound by loading: parts of `per` tiles, the shortest that make no more workgroups than fit at once, and
-    // no shorter than a square root of the range, where a step of four tiles, 0.65 us, costs what the
-    // parts it saves cost the last workgroup, 0.1 us each.
-    int64_t per = std::max<int64_t>({(work + fill - 1) / fill, kFewWaves, (int64_t)std::sqrt(0.6 * longest)});
+    // Bound by loading: parts of `per` tiles, the shortest that make no more workgroups than fit at once
+    // and, where the last workgroup joins them, no shorter than a square root of the range: there a
+    // step of four tiles, 0.65 us, costs what the parts it saves cost that workgroup, 0.1 us each.
+    int64_t per = std::max<int64_t>({(work + fill - 1) / fill, kFewWaves, a->join_apart ? 0 : (int64_t)std::sqrt(0.6 * longest)});
     per = (per + unit - 1) / unit * unit;
     for (;; per += std::max(unit, per / 16 / unit * unit)) {
       const int64_t blocks = split(per);
@@ -263,16 +259,41 @@ void plan(AttendArgs* a, AttendKind kind, int D, int format) {
   a->blocks = (int32_t)at;
 }
 
+int32_t most_splits(const AttendArgs& a) {
+  int32_t most = 1;
+  for (int32_t i = 0; i < a.streams; ++i) most = std::max(most, a.s[i].splits);
+  return most;
+}
+
+// Trips to other workgroups' parts, over a microsecond each, that the last workgroup of a row tile would
+// make to join them: four elements a thread, 16 parts at a time. A launch that joins them a wave a row
+// costs as much as two to three: one token of 28 heads of 128 over 1000 positions (one trip) 7.5 us
+// joined by the last workgroup and 10.1 by a launch, four tokens over 6272 (eight trips) 20.4 and 14.1,
+// of heads of 256 34.7 and 20.5.
+int64_t join_trips(const AttendArgs& a, AttendKind kind, int D, int32_t most_rows) {
+  const int32_t splits = most_splits(a);
+  if (splits == 1) return 0;
+  const int64_t rows = std::min<int64_t>((int64_t)most_rows * a.G, attend_rows(kind, D));
+  return join_rounds(rows, D) * ((splits + 15) / 16);
+}
+
 }  // namespace
 
-hipError_t ipv::launch_join(int D, uint32_t rows, int32_t BM, const AttendArgs& a, hipStream_t st) {
-  const dim3 grid((rows + 3) / 4, (uint32_t)a.streams), block(256);
+template <bool F32OUT>
+static void launch_join_t(int D, dim3 grid, int32_t BM, const AttendArgs& a, hipStream_t st) {
+  const dim3 block(256);
   switch (D) {
-    case 32: k_attend_join<32><<<grid, block, 0, st>>>(a, BM); break;
-    case 64: k_attend_join<64><<<grid, block, 0, st>>>(a, BM); break;
-    case 128: k_attend_join<128><<<grid, block, 0, st>>>(a, BM); break;
-    default: k_attend_join<256><<<grid, block, 0, st>>>(a, BM); break;
+    case 32: k_attend_join<32, F32OUT><<<grid, block, 0, st>>>(a, BM); break;
+    case 64: k_attend_join<64, F32OUT><<<grid, block, 0, st>>>(a, BM); break;
+    case 128: k_attend_join<128, F32OUT><<<grid, block, 0, st>>>(a, BM); break;
+    default: k_attend_join<256, F32OUT><<<grid, block, 0, st>>>(a, BM); break;
   }
+}
+
+static hipError_t launch_join(int D, bool f32, uint32_t rows, int32_t BM, const AttendArgs& a, hipStream_t st) {
+  const dim3 grid((rows + 3) / 4, (uint32_t)a.streams);
+  if (f32) launch_join_t<true>(D, grid, BM, a, st);
+  else launch_join_t<false>(D, grid, BM, a, st);
   return hipGetLastError();
 }
 
@@ -363,7 +384,12 @@ ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const voi
     }
     if (most == 0) continue;
     const AttendKind kind = attend_kind(pool->format, (int64_t)most * a.G);
+    a.join_apart = kind == kTile;
     plan(&a, kind, pool->head_dim, pool->format);
+    if (!a.join_apart && join_trips(a, kind, pool->head_dim, most) > kJoinTrips) {
+      a.join_apart = 1;
+      if (kind != kF32) plan(&a, kind, pool->head_dim, pool->format);  // (parts may be shorter then)
+    }
     a.arrived = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + kWsHeader);
     a.part_ml = reinterpret_cast<float*>(a.arrived + kMaxParts);
     a.part = a.part_ml + (size_t)kMaxParts * attend_rows(kind, pool->head_dim) * 2;
@@ -376,10 +402,9 @@ ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const voi
       default: e = launch_attend<kFmtFp4>(pool->head_dim, kind, grid, a, st); break;
     }
     IPV_TRY(launched(e));
-    if (kind != kTile) continue;  // the others join their parts themselves
-    bool split = false;
-    for (int32_t i = 0; i < a.streams; ++i) split |= a.s[i].splits > 1;
-    if (split) IPV_TRY(launched(launch_join(pool->head_dim, (uint32_t)most * (uint32_t)q_heads, attend_rows(kind, pool->head_dim), a, st)));
+    if (a.join_apart && most_splits(a) > 1)
+      IPV_TRY(launched(launch_join(pool->head_dim, kind == kF32, (uint32_t)most * (uint32_t)q_heads,
+                                   attend_rows(kind, pool->head_dim), a, st)));
   }
   return IPV_OK;
 }
