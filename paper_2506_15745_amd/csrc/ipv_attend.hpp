@@ -1035,17 +1035,32 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
     for (int kk = 0; kk < D / 16; ++kk) q[kk] = __builtin_bit_cast(Bf16x8, load16(q_at + 2 * (16 * kk + 8 * h)));
     stage_v(t, 0);
     __syncthreads();
+    if (r0 + wave * 32 < R) {
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const int kb = i / (D / 16), kk = i % (D / 16);
-      s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(0, i), q[kk], kk == 0 ? F32x16{} : s[kb], 0, 0, 0);
-    }
-    most = largest(s, 0, 16, -INFINITY);
-    for (;;) {
-      step(std::integral_constant<int, 0>());
-      if (t >= t_end) break;
-      step(std::integral_constant<int, 1>());
-      if (t >= t_end) break;
+      for (int i = 0; i < NS; ++i) {
+        const int kb = i / (D / 16), kk = i % (D / 16);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(0, i), q[kk], kk == 0 ? F32x16{} : s[kb], 0, 0, 0);
+      }
+      most = largest(s, 0, 16, -INFINITY);
+      for (;;) {
+        step(std::integral_constant<int, 0>());
+        if (t >= t_end) break;
+        step(std::integral_constant<int, 1>());
+        if (t >= t_end) break;
+      }
+    } else {  // no rows: only the other waves' keys, in the same steps (6 tokens of 32 heads, 16 streams over
+              // 12000 positions: 80 us against 112 with products of the last row over again)
+      for (int buf = 0; t < t_end; ++t, buf ^= 1) {
+        __syncthreads();
+        const int64_t later = row_of(page, t + 2);
+        page = page_of(t + 3);
+        fetch_k(later, buf);
+        if constexpr (!BOTH) stage_k(buf);
+        fetch_v(rows, buf ^ 1);
+        if constexpr (BOTH) stage_k(buf);
+        stage_v(t + 1, buf ^ 1);
+        rows = later;
+      }
     }
     __syncthreads();
     if (lds_special) {
