@@ -100,6 +100,23 @@ struct Limits {
   __device__ __forceinline__ bool operator()(int32_t x) const { return (x <= hi) & ((x > lo) | (x < first)); }
 };
 
+// The same for 64 places as bits: a score is kept or made -inf by two instructions (its bit spread over a
+// word, a choice by bits) instead of three comparisons and what joins them.
+struct SeenBits {
+  uint32_t w[2];
+  __device__ __forceinline__ explicit SeenBits(const Limits& in) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      w[i] = below(in.hi + 1 - 32 * i) & (~below(in.lo + 1 - 32 * i) | below(in.first - 32 * i));
+  }
+  // bits x < k of a word
+  static __device__ __forceinline__ uint32_t below(int32_t k) { return k >= 32 ? ~0u : (1u << max(k, 0)) - 1u; }
+  __device__ __forceinline__ float operator()(int32_t x, float score) const {
+    const uint32_t all = (uint32_t)__builtin_amdgcn_sbfe((int32_t)w[x / 32], x % 32, 1);
+    return __uint_as_float((__float_as_uint(score) & all) | (__float_as_uint(-INFINITY) & ~all));
+  }
+};
+
 // Keeps a rare branch a branch: its body is not computed ahead and selected.
 __device__ __forceinline__ void rare() { asm volatile("" ::: "memory"); }
 
@@ -952,12 +969,11 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
     if constexpr (BOTH) fetch_v(rows, NEXT);
     const int32_t j0 = kt.tile(t) * BN;
     if (!all_see(j0, j0 + BN, pw_lo, pw_hi, n, a.window, a.sinks)) {
-      const Limits in(j0 + 4 * h, pos, n, a.window, a.sinks);
+      const SeenBits in(Limits(j0 + 4 * h, pos, n, a.window, a.sinks));
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (!in(kb * 32 + 8 * (i / 4) + i % 4)) s[kb][i] = -INFINITY;
+        for (int i = 0; i < 16; ++i) s[kb][i] = in(kb * 32 + 8 * (i / 4) + i % 4, s[kb][i]);
       most = largest(s, 0, 16, -INFINITY);
     }
     float top = lanes_max<2>(most) * a.c;
