@@ -120,6 +120,16 @@ struct SeenBits {
 // Keeps a rare branch a branch: its body is not computed ahead and selected.
 __device__ __forceinline__ void rare() { asm volatile("" ::: "memory"); }
 
+// Keeps a value in accumulation registers, which only the matrix unit reads, where the others do not
+// suffice: left to itself the compiler moves such values there and back in every step (900 tokens of 64
+// heads of 256 over 8192 positions 612 us, 546 without that).
+__device__ __forceinline__ void in_acc(F32x16& x) { asm volatile("" : "+a"(x)); }
+__device__ __forceinline__ void in_acc(Bf16x8& x) {
+  U32x4 w = __builtin_bit_cast(U32x4, x);
+  asm volatile("" : "+a"(w));
+  x = __builtin_bit_cast(Bf16x8, w);
+}
+
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_hw(float x) { return __builtin_amdgcn_logf(x); }
 constexpr float kLn2 = 0.693147180559945309f;
@@ -729,11 +739,11 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
 // ---------------------------------------------------------------- many rows
 // Row tiles of 32 rows a wave, keys in tiles of 64 through LDS, where all waves
 // read them; the next tiles' rows are in flight meanwhile. Two waves a SIMD, or one
-// for D = 256, whose sums and queries alone take 192 registers. Bound by the matrix
+// for D = 256, whose sums and queries take 192 accumulation registers. Bound by the matrix
 // unit, at a clock that its load lowers: 2048 tokens of 64 heads over 32768 positions of 8,
 // D = 128, take 1820 us, 1170 TFLOP/s at 60% of the unit's cycles and 1.86 GHz (the library's
 // product of random bf16 matrices reaches 1490); fp8 1890, fp4 1805; D = 64 in half the
-// operations 850 TFLOP/s, where the softmax's instructions weigh twice, D = 256 880.
+// operations 900 TFLOP/s, where the softmax's instructions weigh twice, D = 256 960.
 // 128 rows a workgroup, two of them a CU: 2045 us. Short calls are bound by the way to
 // their first rows and back: a frame of 196 tokens of 28 heads over 6272 positions 33.5 us and
 // 7.5 for the join, of 12 at the library product's rate.
@@ -809,13 +819,10 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
     bad |= x;
     return r;
   };
-  // rows on their way through registers (D = 256 has none for both: V's are fetched when K's are there)
-  constexpr bool BOTH = COPY || D <= 128;
-  constexpr int NK = COPY ? 1 : C::NL, NV = COPY || !BOTH ? 1 : C::NL;
-  uint32_t kr[NK][4], vx[NV][4];
-  uint64_t ks[NK], vsx[NV];
-  auto& vr = [&]() -> auto& { if constexpr (BOTH) return vx; else return kr; }();
-  auto& vs = [&]() -> auto& { if constexpr (BOTH) return vsx; else return ks; }();
+  // rows on their way through registers
+  constexpr int NX = COPY ? 1 : C::NL;
+  uint32_t kr[NX][4], vr[NX][4];
+  uint64_t ks[NX], vs[NX];
   // this thread's chunks: column threadIdx.x % CPR of rows key0 + i * 64 W / CPR
   const int key0 = threadIdx.x / C::CPR % BN;
   constexpr int STEP = 64 * W / C::CPR;
@@ -935,7 +942,7 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
   const int32_t t_begin = t;
   constexpr int NS = D / 8, NP = D / 8, HALF = NP / 2;  // products for the scores, and with the weights
   // operands in flight: KA products ahead of the first kind's, VA of the second's
-  constexpr int KA = D > 128 ? 3 : NS < 5 ? NS : 5, VA = D > 128 ? 2 : NP < 4 ? NP : 4;
+  constexpr int KA = NS < 5 ? NS : 5, VA = NP < 4 ? NP : 4;
   Bf16x8 kf[KA + 1];
   auto step = [&](auto bufc) __attribute__((always_inline)) {
     constexpr int BUF = decltype(bufc)::value, NEXT = BUF ^ 1;  // tile t's buffers, and t + 1's
@@ -966,7 +973,7 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
     const int64_t later = row_of(page, t + 2);
     page = page_of(t + 3);  // a step before it is needed, and before the copies: nothing waits for it, or for them with it
     fetch_k(later, BUF);
-    if constexpr (BOTH) fetch_v(rows, NEXT);
+    fetch_v(rows, NEXT);
     const int32_t j0 = kt.tile(t) * BN;
     if (!all_see(j0, j0 + BN, pw_lo, pw_hi, n, a.window, a.sinks)) {
       const SeenBits in(Limits(j0 + 4 * h, pos, n, a.window, a.sinks));
@@ -984,7 +991,11 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
       m = top;
       l *= old;
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) o[i] *= old;
+      for (int i = 0; i < D / 32; ++i) {
+        if constexpr (D > 128) in_acc(o[i]);
+        o[i] *= old;
+        if constexpr (D > 128) in_acc(o[i]);
+      }
     }
     const float shift = shift_of(m);
     Bf16x8 w[4];
@@ -1008,10 +1019,6 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
       weights(0, 8 * (i - FIRST) / (NS - FIRST), 8 * (i - FIRST + 1) / (NS - FIRST));
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (!BOTH) {
-      stage_k(BUF);
-      fetch_v(rows, NEXT);
-    }
     float biggest = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
@@ -1027,7 +1034,7 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
-    if constexpr (BOTH) stage_k(BUF);
+    stage_k(BUF);
     stage_v(t + 1, NEXT);
     s[0] = ahead[0], s[1] = ahead[1];
     most = biggest;
@@ -1048,7 +1055,10 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
     fetch_v(here, 0);
     const char* q_at = a.q + 2 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + qr - tok * a.G) * a.q_h + (int64_t)tok * a.q_m);
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) q[kk] = __builtin_bit_cast(Bf16x8, load16(q_at + 2 * (16 * kk + 8 * h)));
+    for (int kk = 0; kk < D / 16; ++kk) {
+      q[kk] = __builtin_bit_cast(Bf16x8, load16(q_at + 2 * (16 * kk + 8 * h)));
+      if constexpr (D > 128) in_acc(q[kk]);
+    }
     stage_v(t, 0);
     __syncthreads();
     if (r0 + wave * 32 < R) {
@@ -1071,9 +1081,8 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
         const int64_t later = row_of(page, t + 2);
         page = page_of(t + 3);
         fetch_k(later, buf);
-        if constexpr (!BOTH) stage_k(buf);
         fetch_v(rows, buf ^ 1);
-        if constexpr (BOTH) stage_k(buf);
+        stage_k(buf);
         stage_v(t + 1, buf ^ 1);
         rows = later;
       }

@@ -186,12 +186,13 @@ ipv_status check_heads(const ipv_page_shape* s, int32_t streams, int32_t q_heads
 // costs its tiles and, around them, its start, the wait for its first rows and the store of its
 // result or part; joining parts costs a launch and their bytes. A last round that does not fill the
 // card costs a whole one, but for bf16 heads of 128: a full card lowers its clock for their products.
-// Against parts only where they fit in one round: 300 tokens of 64 heads of 256 over 8192 positions
-// 319 -> 240 us, 600 of 64 heads of 64 145 -> 122, 1100 of 64 heads of 128 372 -> 329; fp32, 300 tokens
-// of 28 heads of 128 over 6272, 460 -> 331.
+// Against no parts, where the row tiles do not fill the card's rounds: 300 tokens of 64 heads of 256 over
+// 8192 positions 293 -> 255 us, 600 of 64 heads of 64 145 -> 125, 1100 of 64 heads of 128 383 -> 343; fp32,
+// 300 tokens of 28 heads of 128 over 6272, 452 -> 332; where they leave most of it empty, 196 of those
+// in bf16, 144 -> 38. Against parts that always fill a round: 400 tokens of 64 heads over 400 38 -> 21.
 double attend_us(AttendKind kind, int D, int64_t per, int64_t blocks, int32_t fill, bool parts) {
   const int size = D == 32 ? 0 : D == 64 ? 1 : D == 128 ? 2 : 3;
-  static constexpr double kTileUs[4] = {0.8, 1.06, 1.8, 2.4}, kF32Us[4] = {0.67, 1.35, 1.2, 2.7};
+  static constexpr double kTileUs[4] = {0.8, 1.06, 1.8, 2.0}, kF32Us[4] = {0.67, 1.35, 1.2, 2.7};
   const int64_t whole = blocks / fill, rounds = (blocks + fill - 1) / fill;
   const double rest = (double)(blocks % fill) / fill, last = D != 128 ? 1 : whole == 0 ? 0.6 + 0.3 * rest : 0.5 + 0.45 * rest * rest;
   const double joins = parts ? 3.5 + 0.015 * attend_rows(kind, D) * D / 32768 * blocks : 0;
