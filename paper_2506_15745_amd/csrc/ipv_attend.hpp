@@ -744,9 +744,9 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
 // D = 128, take 1820 us, 1170 TFLOP/s at 60% of the unit's cycles and 1.86 GHz (the library's
 // product of random bf16 matrices reaches 1490); fp8 1890, fp4 1805; D = 64 in half the
 // operations 900 TFLOP/s, where the softmax's instructions weigh twice, D = 256 960.
-// 128 rows a workgroup, two of them a CU: 2045 us; 64 rows a wave, one wave a SIMD: 3135. Short calls are bound by the way to
-// their first rows and back: a frame of 196 tokens of 28 heads over 6272 positions 33.5 us and
-// 7.5 for the join, of 12 at the library product's rate.
+// 128 rows a workgroup, two of them a CU: 2045 us; 64 rows a wave, one wave a SIMD: 3135.
+// Short calls are bound by the way to their first rows and back: a frame of 196 tokens of 28 heads
+// over 6272 positions 33 us and 7.6 for the join, of 12 at the library product's rate.
 constexpr int kTileKeys = 64;
 __host__ __device__ constexpr int tile_waves(int D) { return D <= 128 ? 8 : 4; }
 
