@@ -1148,11 +1148,13 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
 // Row tiles of 32 rows; the four waves share the keys, 32 at a time, with the fp32
 // matrix instruction. It has a sixteenth of the bf16 one's rate, so rows are read
 // straight from the caches into its operands, without LDS. Its operands take one
-// element a lane: half h of the wave holds the elements h * D / 2 + k of a key, and
-// S^T leaves the weights as the second product's operand as they stand.
+// element a lane: half h of the wave holds the elements 8 k + 4 h + i of a key, so that a
+// load reads 32 bytes of each row, and a row's lines stay in the first cache until they
+// are used up (halves of a row instead: 819 -> 860 us for 1600 tokens of 64 heads of 64 over
+// 4096 positions). S^T leaves the weights as the second product's operand as they stand.
 // Chunks are bound by that instruction, single tokens by the cache's bytes: 512 tokens of 64 heads over
-// 4096 positions of 8, D = 128, 604 us, 107 TFLOP/s (the library's product of such sizes: 154);
-// one token of 8 streams over 32768 positions 400 us, 5.4 TB/s.
+// 4096 positions of 8, D = 128, 548 us, 117 TFLOP/s (the library's product of such sizes: 154), 106
+// for D = 64, 112 for 256; one token of 8 streams over 32768 positions 370 us, 5.8 TB/s.
 template <int D, bool WHOLE>
 __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(AttendArgs a) {
   constexpr int BN = 32;
@@ -1174,10 +1176,10 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(
   const int32_t t_begin = (int32_t)((int64_t)kt.count * pl.split / st.splits) + wave;
   const int32_t r = min(r0 + l32, R - 1), tok = (int32_t)fast_div((uint32_t)r, a.G_div), pos = st.first + tok;
   float q[D / 2];
-  const char* qa = a.q + 4 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + r - tok * a.G) * a.q_h + (int64_t)tok * a.q_m + h * (D / 2));
+  const char* qa = a.q + 4 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + r - tok * a.G) * a.q_h + (int64_t)tok * a.q_m + 4 * h);
 #pragma unroll
   for (int k = 0; k < D / 2; k += 4) {
-    const F32x4 v = *reinterpret_cast<const F32x4*>(qa + 4 * k);
+    const F32x4 v = *reinterpret_cast<const F32x4*>(qa + 8 * k);
     q[k] = v.x, q[k + 1] = v.y, q[k + 2] = v.z, q[k + 3] = v.w;
   }
   F32x16 o[D / 32];
@@ -1195,15 +1197,15 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(
   };
   // K in pieces of four elements, KA of them in registers: all of a row's up to D = 128. With one
   // wave a SIMD (D > 64) the next tile's are on their way while V is used: 512 tokens of 64 heads
-  // over 4096 positions of 8, D = 128, take 604 us with that and 825 without. Where two share it
-  // they cover for each other, and loads ahead only hold them up: 357 us with it and 321 without, D = 64.
+  // over 4096 positions of 8, D = 128, take 549 us with that and 648 without. Where two share it
+  // they cover for each other, and loads ahead only hold them up: 320 us with it and 297 without, D = 64.
   constexpr bool AHEAD = D > 64;
   using At = std::conditional_t<WHOLE, uint32_t, int64_t>;
   constexpr int KA = D <= 128 ? D / 8 : 8;
   F32x4 kx[KA];
   const auto load_k = [&](int64_t row, int k) __attribute__((always_inline)) {
     const char* base = a.pool.K + (WHOLE ? row * D * 4 : 0);
-    kx[k % KA] = *reinterpret_cast<const F32x4*>(base + 16 * k + (At)((WHOLE ? (At)l32 : (At)row) * D * 4 + h * D * 2));
+    kx[k % KA] = *reinterpret_cast<const F32x4*>(base + 32 * k + (At)((WHOLE ? (At)l32 : (At)row) * D * 4 + 16 * h));
   };
   // V's rows (all of them up to D = 128, else four keys ahead) are on their way while the
   // scores are computed
@@ -1255,12 +1257,21 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
-    top = fmaxf(m, lanes_max<2>(top) * a.c);
-    const float shift = shift_of(top), old = exp2_hw(m - shift);
-    m = top;
-    l *= old;
+    top = lanes_max<2>(top) * a.c;
+    if (__ballot(top > m + kLazy) != 0) {
+      rare();
+      top = fmaxf(top, m);
+      const float old = exp2_hw(m - shift_of(top));
+      m = top;
+      l *= old;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] *= old;
+      for (int i = 0; i < D / 32; ++i) {
+        if constexpr (D > 64) in_acc(o[i]);
+        o[i] *= old;
+        if constexpr (D > 64) in_acc(o[i]);
+      }
+    }
+    const float shift = shift_of(m);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float e = exp2_hw(__builtin_fmaf(s[i], a.c, -shift));

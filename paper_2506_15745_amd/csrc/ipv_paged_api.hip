@@ -192,7 +192,7 @@ ipv_status check_heads(const ipv_page_shape* s, int32_t streams, int32_t q_heads
 // in bf16, 144 -> 38. Against parts that always fill a round: 400 tokens of 64 heads over 400 38 -> 21.
 double attend_us(AttendKind kind, int D, int64_t per, int64_t blocks, int32_t fill, bool parts) {
   const int size = D == 32 ? 0 : D == 64 ? 1 : D == 128 ? 2 : 3;
-  static constexpr double kTileUs[4] = {0.8, 1.06, 1.8, 2.0}, kF32Us[4] = {0.67, 1.35, 1.2, 2.7};
+  static constexpr double kTileUs[4] = {0.8, 1.06, 1.8, 2.0}, kF32Us[4] = {0.67, 1.27, 1.1, 2.2};
   const int64_t whole = blocks / fill, rounds = (blocks + fill - 1) / fill;
   const double rest = (double)(blocks % fill) / fill, last = D != 128 ? 1 : whole == 0 ? 0.6 + 0.3 * rest : 0.5 + 0.45 * rest * rest;
   const double joins = parts ? 3.5 + 0.015 * attend_rows(kind, D) * D / 32768 * blocks : 0;
