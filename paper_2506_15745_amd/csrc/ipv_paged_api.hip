@@ -371,8 +371,8 @@ ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const voi
   a.max_rows = max_rows;
   a.G_div = make_fastdiv((uint32_t)a.G);
   a.c = (float)(scale * 1.4426950408889634);
-  a.window = window;
-  a.sinks = sinks;
+  a.window = window > kMaxPosition ? 0 : window;  // (wider than any range: none, and sums with it stay in 32 bits)
+  a.sinks = std::min(sinks, kMaxPosition);
   a.err = static_cast<uint32_t*>(ws);
   hipStream_t st = static_cast<hipStream_t>(stream);
   for (int32_t b0 = 0; b0 < streams; b0 += kAttendStreams) {

@@ -314,3 +314,18 @@ def test_what_is_not_seen_stays_out_of_whole_tiles(fmt, D, m):
         ipv.ipv_attend(pool, table, n, n - m, 0, q, torch.empty_like(q), ws)
         assert ipv.ipv_read_device_errors(ws) == ipv.DEV_BAD_PAGE
         ipv.ipv_clear_device_errors(ws)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("m", [1, 70])
+@pytest.mark.parametrize("window,sinks", [(2**31 - 1, 0), (2**31 - 1, 2**31 - 1), (20, 2**31 - 1), (2**30, 5)])
+def test_windows_beyond_any_position(fmt, m, window, sinks):
+    """The widest window is none, and all rows may be first rows."""
+    n = 200
+    pool = R.filled_pool(fmt, 5, 1, 2, 64, 64, 3)
+    table = R.shuffled_table(1, 4, 5, 4)
+    q = queries(fmt, 1, 4, m, 64, 5)
+    out, lse = check(fmt, pool, table, [n], [n - m], 0, q, window, sinks)
+    full, flse = check(fmt, pool, table, [n], [n - m], 0, q)
+    if window > n:
+        assert torch.equal(out, full) and torch.equal(lse, flse)
