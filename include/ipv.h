@@ -124,7 +124,8 @@ enum {
                                   not zero (a workspace shared by overlapping calls); its rows were not
                                   moved */
   IPV_DEV_BAD_PAGE = 64u       /* paged cache: a page_table entry outside [0, pages): ipv_page_write left the
-                                  row out, ipv_page_read and ipv_attend read page 0 in its place */
+                                  row out, ipv_page_read and ipv_attend read page 0 in its place (ipv_attend:
+                                  the entry of a row that some query sees; the others may hold anything) */
 };
 
 /*

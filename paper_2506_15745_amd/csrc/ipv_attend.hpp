@@ -521,6 +521,8 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
     for (int i = 0; i < D / 16; ++i) o[nb][i] = F32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  // Whether a row that some query sees has no page: a tile of other rows than a whole page's may
+  // also hold rows that none sees, whose entries say nothing (every tile has one that is seen).
   bool bad = false;
   // the tile's key lane % 32, or its first; a key past the last is the last; its page, and its row in the pool
   const auto key_of = [&](int32_t tt) __attribute__((always_inline)) {
@@ -531,8 +533,9 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
   };
   const auto row_of = [&](int32_t page, int32_t tt) __attribute__((always_inline)) {
     bool x;
-    const int64_t r = pool_row(a.pool, page, (uint32_t)key_of(tt), &x) + head_row;
-    bad |= x;
+    const int32_t j = key_of(tt);
+    const int64_t r = pool_row(a.pool, page, (uint32_t)j, &x) + head_row;
+    bad |= x & (WHOLE | kt.some(j));
     return r;
   };
   constexpr bool COPY = F == kFmtBf16;
@@ -827,8 +830,9 @@ __global__ __launch_bounds__(64 * tile_waves(D), tile_waves(D) / 4) void k_atten
   };
   const auto row_of = [&](int32_t page, int32_t tt) __attribute__((always_inline)) {
     bool x;
-    const int64_t r = pool_row(a.pool, page, (uint32_t)key_of(tt), &x) + head_row;
-    bad |= x;
+    const int32_t j = key_of(tt);
+    const int64_t r = pool_row(a.pool, page, (uint32_t)j, &x) + head_row;
+    bad |= x & (WHOLE | kt.some(j));
     return r;
   };
   // rows on their way through registers
@@ -1201,10 +1205,10 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_f32(
   bool bad = false, special = false;
   auto row_of = [&](int32_t t) __attribute__((always_inline)) {  // the pool's row of the tile's key l32 (WHOLE: its first)
     bool x;
-    const uint32_t j = (uint32_t)min(kt.tile(min(t, kt.count - 1)) * BN + (WHOLE ? 0 : l32), n - 1);
-    const int32_t page = WHOLE ? pool_page_uniform(a.pool, b, j) : pool_page(a.pool, b, j);
-    const int64_t at = pool_row(a.pool, page, j, &x) + head_row;
-    bad |= x;
+    const int32_t j = min(kt.tile(min(t, kt.count - 1)) * BN + (WHOLE ? 0 : l32), n - 1);
+    const int32_t page = WHOLE ? pool_page_uniform(a.pool, b, (uint32_t)j) : pool_page(a.pool, b, (uint32_t)j);
+    const int64_t at = pool_row(a.pool, page, (uint32_t)j, &x) + head_row;
+    bad |= x & (WHOLE | kt.some(j));
     return at;
   };
   // K in pieces of four elements, KA of them in registers: all of a row's up to D = 128. With one
