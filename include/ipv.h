@@ -363,7 +363,7 @@ ipv_status ipv_ckv_stream(const ipv_shape* shape, void* K, void* V, int32_t* fra
  * The quantised formats keep one scale for each 32 consecutive elements of a
  * row, K_scales and V_scales [pages, layers, kv_heads, page_rows, D / 32] bytes:
  * an element stands for its value times 2^(byte - 127); byte 255: the block is NaN
- * (values below 2^-126 in magnitude may be taken for zero).
+ * (values below 2^-126 in magnitude may be taken for zero, those of 2^128 and more are infinite).
  * Row j of stream b (its position) is slot j % page_rows of page
  * page_table[b * table_cols + j / page_rows] (int32, device). Pages may be
  * shared between streams that only read them. page_table NULL: stream b's rows
@@ -401,8 +401,9 @@ typedef struct {
  * rotary_rows. Quantised formats: a block's scale is the smallest power of two 2^e,
  * -126 <= e, that keeps its largest magnitude within the type's largest value (so
  * nothing is cut off), and the elements round to nearest, ties to even, after the
- * division, which is exact. A block that holds an infinity or NaN becomes NaN
- * and raises IPV_DEV_NAN.
+ * division, which is exact (magnitudes next to the largest of bf16 and fp32, from
+ * 1.9375 * 2^127 in e4m3 and 1.75 * 2^127 in e2m1 on, thus round to 2^128, an infinity).
+ * A block that holds an infinity or NaN becomes NaN and raises IPV_DEV_NAN.
  * Positions of one call that lie in the same page and slot (pages shared by two
  * streams that both write) are written in no fixed order.
  */

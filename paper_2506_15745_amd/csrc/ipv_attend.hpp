@@ -225,16 +225,29 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a) {
 }
 
 // Stored elements of a row that some query does not see: nothing of them if none
-// does, else without infinities and NaN (a product with a weight of zero would
+// does, else without infinities (in bf16) and NaN (a product with a weight of zero would
 // be NaN). Whether any were taken out of a row that some see.
 template <int F>
 __device__ __forceinline__ bool clean(uint32_t (&x)[4], uint64_t& scales, int block, bool some) {
   bool special = false, nan = false;
   asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));  // nothing of this outside the branch that needs it
   if constexpr (fmt_scaled(F)) {
-    nan = ((scales >> (8 * block)) & 255u) == 255u;
+    // values of 2^128 and more, infinite in bf16, need a scale of 2^120 (e4m3) or 2^126 (e2m1) at least
+    constexpr uint32_t large = F == kFmtFp8 ? 247u : 253u;
+    const uint32_t byte = (uint32_t)(scales >> (8 * block)) & 255u;
+    nan = byte == 255u;
     special = nan && some;
     if (nan) scales = 0;
+    if (byte >= large && !nan) {  // all elements of a word at once, by their exponents
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t over;
+        if constexpr (F == kFmtFp8) over = (((x[e] >> 3) & 0x0f0f0f0fu) + (byte - 246u) * 0x01010101u) >> 4 & 0x01010101u;
+        else over = x[e] >> 2 & (byte == large ? x[e] >> 1 : ~0u) & 0x11111111u;
+        x[e] &= ~(over * (F == kFmtFp8 ? 255u : 15u));
+        special |= some & (over != 0);
+      }
+    }
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
