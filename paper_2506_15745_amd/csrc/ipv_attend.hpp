@@ -1420,6 +1420,7 @@ enum AttendKind { kFew1, kFew2, kTile, kF32 };
 template <int F>
 hipError_t launch_attend(int D, AttendKind kind, uint32_t grid, const AttendArgs& a, hipStream_t st);
 inline int attend_rows(AttendKind k, int D) { return k == kFew1 ? 16 : k == kFew2 || k == kF32 ? 32 : 32 * tile_waves(D); }
+inline int attend_threads(AttendKind k, int D) { return 64 * (k == kTile ? tile_waves(D) : kFewWaves); }
 inline int attend_keys(AttendKind k) { return k == kTile ? kTileKeys : 32; }
 
 }  // namespace ipv

@@ -24,6 +24,7 @@ static_assert((int)kFmtBf16 == IPV_BF16 && (int)kFmtF32 == IPV_F32, "rows in the
 static_assert(kDevNan == IPV_DEV_NAN && kDevBadPage == IPV_DEV_BAD_PAGE, "the error bits of the header");
 
 constexpr int32_t kMaxPosition = 1 << 30;  // positions and their tiles' ends stay in 31 bits
+constexpr int64_t kGridThreads = 0xffffffffll;  // threads of a grid along one dimension, at most
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
@@ -88,10 +89,15 @@ hipError_t page_launch(const PageCall& c, dim3 grid, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Workgroups along the rows of a launch whose widest stream has `rows`.
+int64_t page_blocks(int D, int64_t rows) {
+  const int per = kPageThreads / (D / 16);
+  return (rows + per - 1) / per;
+}
+
 template <bool WRITE, int F, int X>
 hipError_t page_launch_d(int D, const PageCall& c, int32_t rows, hipStream_t st, int32_t streams) {
-  const int per = kPageThreads / (D / 16);
-  const dim3 grid((uint32_t)((rows + per - 1) / per), (uint32_t)(2 * ((c.LH + kPageSlices - 1) / kPageSlices)), (uint32_t)streams);
+  const dim3 grid((uint32_t)page_blocks(D, rows), (uint32_t)(2 * ((c.LH + kPageSlices - 1) / kPageSlices)), (uint32_t)streams);
   switch (D) {
     case 32: return page_launch<WRITE, F, X, 32>(c, grid, st);
     case 64: return page_launch<WRITE, F, X, 64>(c, grid, st);
@@ -126,6 +132,7 @@ ipv_status page_rows(const ipv_page_shape* s, const void* K_pages, const void* V
     if (rows[b] < 0 || first[b] < 0) return IPV_ERR_SHAPE;
     const int64_t end = (int64_t)first[b] + rows[b];
     if (rows[b] > 0 && end > table_rows(s, cols)) return IPV_ERR_SHAPE;
+    if (page_blocks(s->head_dim, rows[b]) * kPageThreads > kGridThreads) return IPV_ERR_SHAPE;
     if (rows[b] > 0 && rotary && end > rotary_rows) return IPV_ERR_ARG;
   }
   IPV_TRY(check_word(ws, ws_bytes, kWsHeader));
@@ -179,6 +186,21 @@ size_t part_bytes(AttendKind k, int D) { return (size_t)kMaxParts * attend_rows(
 ipv_status check_heads(const ipv_page_shape* s, int32_t streams, int32_t q_heads, int32_t max_rows) {
   if (streams < 1 || q_heads < 1 || max_rows < 1 || q_heads % s->kv_heads != 0) return IPV_ERR_SHAPE;
   if ((int64_t)q_heads * max_rows > kMaxPosition) return IPV_ERR_SHAPE;
+  return IPV_OK;
+}
+
+// Every launch's row tiles as a grid (parts only add to it where it stays within kMaxParts).
+ipv_status check_grids(const ipv_page_shape* s, int32_t streams, const int32_t* q_rows, int32_t q_heads) {
+  const int64_t G = q_heads / s->kv_heads;
+  for (int32_t b0 = 0; b0 < streams; b0 += kAttendStreams) {
+    const int32_t* rows = q_rows + b0;
+    const int32_t nb = std::min(kAttendStreams, streams - b0);
+    const AttendKind kind = attend_kind(s->format, *std::max_element(rows, rows + nb) * G);
+    const int32_t BM = attend_rows(kind, s->head_dim);
+    int64_t tiles = 0;
+    for (int32_t i = 0; i < nb; ++i) tiles += (rows[i] * G + BM - 1) / BM;
+    if ((tiles * s->kv_heads + 7) / 8 * 8 * attend_threads(kind, s->head_dim) > kGridThreads) return IPV_ERR_SHAPE;
+  }
   return IPV_OK;
 }
 
@@ -349,13 +371,11 @@ ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const voi
   if (!(scale > 0) || !std::isfinite(scale) || !std::isnormal((float)(scale * 1.4426950408889634)) || window < 0 ||
       sinks < 0)
     return IPV_ERR_ARG;
-  int64_t queries = 0;  // of all streams and heads: their row tiles (16 rows at least) are counted in 31 bits
   for (int32_t b = 0; b < streams; ++b) {
     if (n_tokens[b] < 0 || n_tokens[b] > table_rows(pool, table_cols)) return IPV_ERR_SHAPE;
     if (q_rows[b] < 0 || q_rows[b] > max_rows || q_first[b] < 0 || q_first[b] > kMaxPosition - q_rows[b]) return IPV_ERR_SHAPE;
-    queries += (int64_t)q_rows[b] * q_heads;
   }
-  if (queries > (int64_t)kMaxPosition * 8) return IPV_ERR_SHAPE;
+  IPV_TRY(check_grids(pool, streams, q_rows, q_heads));
   size_t need = 0;
   IPV_TRY(ipv_attend_workspace_bytes(pool, streams, q_heads, max_rows, &need));
   IPV_TRY(check_word(ws, ws_bytes, need));
