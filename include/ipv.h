@@ -445,7 +445,9 @@ ipv_status ipv_attend_workspace_bytes(const ipv_page_shape* pool, int32_t stream
  * not overlap q or the pool.
  * Queries are expected rotated to their positions where the keys are. Products
  * accumulate in fp32 and the softmax is fp32; its weights are rounded to bf16 before
- * they multiply V (not with IPV_PAGES_F32). One call gives the same bits every time.
+ * they multiply V (not with IPV_PAGES_F32). In calls of up to 32 rows a KV head (queries
+ * times its query heads) the largest weight so far is 1 and not rounded.
+ * One call gives the same bits every time.
  */
 ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const void* V_pages, const uint8_t* K_scales,
                       const uint8_t* V_scales, const int32_t* page_table, int32_t table_cols, int32_t streams,
