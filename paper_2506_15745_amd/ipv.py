@@ -553,11 +553,24 @@ class PagePool:
 # pool's own arguments are made with it.
 def _host_counts(values, streams, what):
     """A host array with one count per stream, from an int or a sequence."""
-    if isinstance(values, int):
-        return array("i", (values,) * streams)
-    if len(values) != streams:
-        raise IpvError(ERR_SHAPE, "%s needs one count per stream (%d)" % (what, streams))
-    return array("i", values)
+    try:
+        if isinstance(values, int):
+            return array("i", (values,) * streams)
+        if len(values) != streams:
+            raise IpvError(ERR_SHAPE, "%s needs one count per stream (%d)" % (what, streams))
+        return array("i", values)
+    except OverflowError:
+        raise IpvError(ERR_SHAPE, "%s holds a count of more than 32 bits" % what) from None
+
+
+_I32 = 2**31
+
+
+def _whole32(what, *values):
+    """Refuse what ctypes would cut to its low 32 bits."""
+    for v in values:
+        if not -_I32 <= v < _I32:
+            raise IpvError(ERR_ARG, "%s: %d has more than 32 bits" % (what, v))
 
 
 def _table(pool, table, streams):
@@ -597,6 +610,7 @@ def alloc_page_workspace(device) -> torch.Tensor:
 
 
 def attend_workspace_bytes(pool: PagePool, streams: int, q_heads: int, max_rows: int) -> int:
+    _whole32("ipv_attend_workspace_bytes", streams, q_heads, max_rows)
     out = ctypes.c_size_t(0)
     _check(_paged().ipv_attend_workspace_bytes(pool._args[0], streams, q_heads, max_rows, ctypes.byref(out)),
            "ipv_attend_workspace_bytes")
@@ -632,6 +646,8 @@ def _page_rows(name, pool, page_table, first_row, K, V, ws, rows, first_layer, r
             (rotary is not None and rotary.get_device() != dev):
         _same_gpu(pool, ws, K=K, V=V, rotary=rotary)
     first, counts_ = _host_counts(first_row, B, "first_row"), _host_counts(rows, B, "rows")
+    if not -_I32 <= first_layer < _I32:
+        _whole32("first_layer", first_layer)
     rc = getattr(_paged(), name)(*pool._args, table, cols, B, first.buffer_info()[0], counts_.buffer_info()[0], first_layer, L,
                                  K.data_ptr(), V.data_ptr(), _dtype_code(K), strides,
                                  None if rotary is None else _ptr(rotary), angles, _ptr(ws), ws.nbytes, _stream(stream))
@@ -679,6 +695,8 @@ def ipv_attend(pool, page_table, n_tokens, q_first, layer, q, out, ws, q_rows=No
     rows = _host_counts(M if q_rows is None else q_rows, B, "q_rows")
     q_strides, out_strides = q.stride(), out.stride()
     q_at = _stride_array(q_strides, shape)
+    if not (-_I32 <= layer < _I32 and -_I32 <= window < _I32 and -_I32 <= sinks < _I32):
+        _whole32("layer, window, sinks", layer, window, sinks)
     rc = _paged().ipv_attend(*pool._args, table, cols, B, n.buffer_info()[0], first.buffer_info()[0], rows.buffer_info()[0],
                              layer, q.data_ptr(), q_at, A, M, D ** -0.5 if scale is None else scale, window, sinks,
                              out.data_ptr(), q_at if out_strides == q_strides else _stride_array(out_strides, shape),
