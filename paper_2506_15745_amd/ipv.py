@@ -648,9 +648,10 @@ def _page_rows(name, pool, page_table, first_row, K, V, ws, rows, first_layer, r
     first, counts_ = _host_counts(first_row, B, "first_row"), _host_counts(rows, B, "rows")
     if not -_I32 <= first_layer < _I32:
         _whole32("first_layer", first_layer)
+    at = _ptr(ws)  # also stands for tensors without elements, whose own addresses are null
     rc = getattr(_paged(), name)(*pool._args, table, cols, B, first.buffer_info()[0], counts_.buffer_info()[0], first_layer, L,
-                                 K.data_ptr(), V.data_ptr(), _dtype_code(K), strides,
-                                 None if rotary is None else _ptr(rotary), angles, _ptr(ws), ws.nbytes, _stream(stream))
+                                 K.data_ptr() or at, V.data_ptr() or at, _dtype_code(K), strides,
+                                 None if rotary is None else _ptr(rotary), angles, at, ws.nbytes, _stream(stream))
     if rc != OK:
         _check(rc, name)
 
@@ -697,10 +698,11 @@ def ipv_attend(pool, page_table, n_tokens, q_first, layer, q, out, ws, q_rows=No
     q_at = _stride_array(q_strides, shape)
     if not (-_I32 <= layer < _I32 and -_I32 <= window < _I32 and -_I32 <= sinks < _I32):
         _whole32("layer, window, sinks", layer, window, sinks)
+    at = _ptr(ws)  # also stands for tensors without elements, whose own addresses are null
     rc = _paged().ipv_attend(*pool._args, table, cols, B, n.buffer_info()[0], first.buffer_info()[0], rows.buffer_info()[0],
-                             layer, q.data_ptr(), q_at, A, M, D ** -0.5 if scale is None else scale, window, sinks,
-                             out.data_ptr(), q_at if out_strides == q_strides else _stride_array(out_strides, shape),
-                             None if lse is None else _ptr(lse), _ptr(ws), ws.nbytes, _stream(stream))
+                             layer, q.data_ptr() or at, q_at, A, M or 1, D ** -0.5 if scale is None else scale, window, sinks,
+                             out.data_ptr() or at, q_at if out_strides == q_strides else _stride_array(out_strides, shape),
+                             None if lse is None else _ptr(lse), at, ws.nbytes, _stream(stream))
     if rc != OK:
         _check(rc, "ipv_attend")
 

@@ -42,3 +42,30 @@ def test_whole_numbers_beyond_32_bits(value):
         assert e.value.status in (ipv.ERR_SHAPE, ipv.ERR_ARG), (f.__name__, args[1:], kw)
     torch.cuda.synchronize()
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(held, before))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "f32", "fp8", "fp4"])
+def test_tensors_without_rows(fmt):
+    """Nothing to write, to read or to ask: calls that do nothing, with the checks of the others."""
+    pool, table, q, out, aws, ws = setup(fmt)
+    before = [t.clone() for t in (pool.K, pool.V)]
+    K, V = (torch.ones(1, 2, 2, 0, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for f in (ipv.ipv_page_write, ipv.ipv_page_read):
+        f(pool, table, 5, K, V, ws)
+        f(pool, table, 5, K, V, ws, rows=[0], rotary=R.angles(1, 64, "cuda"))
+        f(pool, table, 5, *(torch.ones(1, 2, 2, 8, 64, device="cuda")[:, :, :, 8:] for _ in range(2)), ws)
+        for args, kw in (((pool, table, 5, K, V, ws), dict(rows=1)), ((pool, table, 5, K, V, ws), dict(first_layer=1)),
+                         ((pool, table, [5, 5], K, V, ws), {}), ((pool, table, -1, K, V, ws), {})):
+            with pytest.raises(ipv.IpvError) as e:
+                f(*args, **kw)
+            assert e.value.status == ipv.ERR_SHAPE
+    lse = torch.empty(1, 4, 0, device="cuda")
+    for lse in (None, lse):
+        ipv.ipv_attend(pool, table, 40, 40, 1, q[:, :, :0], out[:, :, :0], aws, lse=lse)
+    for args in ((pool, table, 40, 40, 2), (pool, table, 49, 40, 0)):
+        with pytest.raises(ipv.IpvError) as e:
+            ipv.ipv_attend(*args, q[:, :, :0], out[:, :, :0], aws)
+        assert e.value.status == ipv.ERR_SHAPE
+    torch.cuda.synchronize()
+    assert ipv.ipv_read_device_errors(ws) == 0 and ipv.ipv_read_device_errors(aws) == 0
+    assert all(torch.equal(a, b) for a, b in zip((pool.K, pool.V), before)) and bool((out == 3.0).all())
