@@ -651,7 +651,7 @@ def _page_rows(name, pool, page_table, first_row, K, V, ws, rows, first_layer, r
     at = _ptr(ws)  # also stands for tensors without elements, whose own addresses are null
     rc = getattr(_paged(), name)(*pool._args, table, cols, B, first.buffer_info()[0], counts_.buffer_info()[0], first_layer, L,
                                  K.data_ptr() or at, V.data_ptr() or at, _dtype_code(K), strides,
-                                 None if rotary is None else _ptr(rotary), angles, at, ws.nbytes, _stream(stream))
+                                 None if rotary is None else _ptr(rotary) or at, angles, at, ws.nbytes, _stream(stream))
     if rc != OK:
         _check(rc, name)
 

@@ -69,3 +69,16 @@ def test_tensors_without_rows(fmt):
     torch.cuda.synchronize()
     assert ipv.ipv_read_device_errors(ws) == 0 and ipv.ipv_read_device_errors(aws) == 0
     assert all(torch.equal(a, b) for a, b in zip((pool.K, pool.V), before)) and bool((out == 3.0).all())
+
+
+def test_a_table_of_no_angles():
+    """Rows cannot be turned by a table without positions (and are not left as they are)."""
+    pool, table, q, out, aws, ws = setup("bf16")
+    K, V = (torch.ones(1, 2, 2, 8, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    before = pool.K.clone()
+    for f in (ipv.ipv_page_write, ipv.ipv_page_read):
+        with pytest.raises(ipv.IpvError) as e:
+            f(pool, table, 0, K, V, ws, rotary=R.angles(10, 64, "cuda")[:0])
+        assert e.value.status == ipv.ERR_ARG
+    torch.cuda.synchronize()
+    assert torch.equal(pool.K, before) and bool((K == 1).all())
