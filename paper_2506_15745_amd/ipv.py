@@ -593,6 +593,12 @@ def _stride_array(strides, sizes):
     return (ctypes.c_int64 * (len(sizes) - 1))(*[st if n > 1 else 0 for st, n in zip(strides[:-1], sizes)])
 
 
+def _not_expanded(what, strides, sizes):
+    """Refuse a result's place whose elements are the same memory."""
+    if any(st == 0 and n > 1 for st, n in zip(strides, sizes)):
+        raise IpvError(ERR_SHAPE, "%s is written and must not be an expanded tensor" % what)
+
+
 def _same_gpu(pool, ws, **tensors):
     dev = pool.K.get_device()
     for what, t in tensors.items():
@@ -632,6 +638,8 @@ def _page_rows(name, pool, page_table, first_row, K, V, ws, rows, first_layer, r
     strides = _stride_array(k_strides := K.stride(), shape)
     if V.stride() != k_strides and list(_stride_array(V.stride(), shape)) != list(strides):
         raise IpvError(ERR_SHAPE, "K and V must have the same strides")
+    if 0 in k_strides and name == "ipv_page_read":
+        _not_expanded("K, V", k_strides, shape)
     if rows is None:
         rows = N
     elif (rows if isinstance(rows, int) else max(rows, default=0)) > N:
@@ -696,6 +704,8 @@ def ipv_attend(pool, page_table, n_tokens, q_first, layer, q, out, ws, q_rows=No
     rows = _host_counts(M if q_rows is None else q_rows, B, "q_rows")
     q_strides, out_strides = q.stride(), out.stride()
     q_at = _stride_array(q_strides, shape)
+    if 0 in out_strides:
+        _not_expanded("out", out_strides, shape)
     if not (-_I32 <= layer < _I32 and -_I32 <= window < _I32 and -_I32 <= sinks < _I32):
         _whole32("layer, window, sinks", layer, window, sinks)
     at = _ptr(ws)  # also stands for tensors without elements, whose own addresses are null

@@ -82,3 +82,24 @@ def test_a_table_of_no_angles():
         assert e.value.status == ipv.ERR_ARG
     torch.cuda.synchronize()
     assert torch.equal(pool.K, before) and bool((K == 1).all())
+
+
+def test_results_into_expanded_tensors():
+    """Rows and queries may be expanded, results may not: their elements would be the same memory."""
+    pool, table, q, out, aws, ws = setup("bf16")
+    one = torch.ones(1, 2, 2, 1, 64, dtype=torch.bfloat16, device="cuda")
+    ipv.ipv_page_write(pool, table, 0, *(one.expand(1, 2, 2, 8, 64),) * 2, ws)
+    got = [torch.zeros(1, 2, 2, 8, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    ipv.ipv_page_read(pool, table, 0, *got, ws)
+    assert all(bool((x == 1).all()) for x in got)
+    ipv.ipv_attend(pool, table, 40, 37, 0, q[:, :, :1].expand(q.shape), out, aws)
+    for f, args in ((ipv.ipv_page_read, (pool, table, 0, *(one.expand(1, 2, 2, 8, 64),) * 2, ws)),
+                    (ipv.ipv_attend, (pool, table, 40, 37, 0, q, q[:, :, :1].expand(q.shape), aws)),
+                    (ipv.ipv_attend, (pool, table, 40, 37, 0, q[:, :1].expand(q.shape), q[:, :1].expand(q.shape), aws))):
+        with pytest.raises(ipv.IpvError) as e:
+            f(*args)
+        assert e.value.status == ipv.ERR_SHAPE
+    torch.cuda.synchronize()
+    assert bool((one == 1).all()) and bool((q == 1).all())
+    # a dimension of one may have any stride
+    ipv.ipv_attend(pool, table, 40, 39, 0, q[:, :, :1], out[:, :, :1].as_strided((1, 4, 1, 64), (0, 192, 0, 1)), aws)
