@@ -372,8 +372,9 @@ ipv_status ipv_ckv_stream(const ipv_shape* shape, void* K, void* V, int32_t* fra
  * Pools and K/V rows are 16-byte aligned; scales, tables and lse 4-byte.
  * Every count is a HOST array with one entry per stream. The workspace of
  * ipv_page_write and ipv_page_read is the 256 bytes of the error word; that of
- * ipv_attend is sized by ipv_attend_workspace_bytes and must have been zeroed
- * when it was allocated. Calls that share a workspace must not overlap in time.
+ * ipv_attend is sized by ipv_attend_workspace_bytes, and its first 4352 bytes
+ * must have been zeroed when it was allocated (the rest may hold anything).
+ * Calls that share a workspace must not overlap in time.
  * Strides are HOST arrays, in elements, each a multiple of 8; the elements of a
  * row are contiguous.
  */
@@ -424,8 +425,10 @@ ipv_status ipv_page_read(const ipv_page_shape* pool, const void* K_pages, const 
                          void* V, int32_t dtype, const int64_t* strides, const float* rotary, int32_t rotary_rows,
                          void* ws, size_t ws_bytes, void* stream);
 
-/* Bytes of device workspace (zeroed when allocated) that every ipv_attend call with this pool, at most `streams`
-   streams, q_heads query heads and at most max_rows queries a stream needs. */
+/* Bytes of device workspace that every ipv_attend call with this pool, at most `streams` streams, q_heads query heads
+   and at most max_rows queries a stream needs: fp32 sums for the parts of split key ranges, at most 1024 parts.
+   With 28 query and 4 KV heads of 128: 2 MiB for one token of one stream, 8 of sixteen, 33 for 35 tokens of one, 130
+   at most (heads of 64: 66, fp32 pools 16). */
 ipv_status ipv_attend_workspace_bytes(const ipv_page_shape* pool, int32_t streams, int32_t q_heads, int32_t max_rows,
                                       size_t* bytes);
 

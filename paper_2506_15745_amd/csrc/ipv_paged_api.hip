@@ -181,7 +181,17 @@ AttendKind attend_kind(int format, int64_t rows) {
   return rows <= 16 ? kFew1 : rows <= 32 ? kFew2 : kTile;
 }
 
-size_t part_bytes(AttendKind k, int D) { return (size_t)kMaxParts * attend_rows(k, D) * (size_t)(D + 2) * sizeof(float); }
+// Parts that launches of at most so many streams, and rows a KV head, can make.
+int64_t max_parts(AttendKind k, int D, int32_t streams, int32_t kv_heads, int64_t rows) {
+  const int64_t tiles = k == kFew1 || k == kFew2 ? 1 : (rows + attend_rows(k, D) - 1) / attend_rows(k, D);
+  return std::min<int64_t>(std::min(streams, kAttendStreams) * (kv_heads * tiles) * kMaxSplits, kMaxParts);
+}
+
+size_t part_bytes(AttendKind k, int D, int64_t parts) { return (size_t)parts * attend_rows(k, D) * (size_t)(D + 2) * sizeof(float); }
+
+// The workspace: error word, counters (zero before and after a call), parts' maxima and sums, parts.
+constexpr size_t kZeroed = kWsHeader + kMaxParts * sizeof(uint32_t);
+static_assert(kZeroed == 4352, "the bytes to be zeroed that the header names");
 
 ipv_status check_heads(const ipv_page_shape* s, int32_t streams, int32_t q_heads, int32_t max_rows) {
   if (streams < 1 || q_heads < 1 || max_rows < 1 || q_heads % s->kv_heads != 0) return IPV_ERR_SHAPE;
@@ -346,11 +356,14 @@ ipv_status ipv_attend_workspace_bytes(const ipv_page_shape* pool, int32_t stream
   IPV_TRY(check_pool_shape(pool));
   IPV_TRY(check_heads(pool, streams, q_heads, max_rows));
   // a call of fewer rows may take a kernel of narrower tiles
-  const AttendKind widest = attend_kind(pool->format, (int64_t)max_rows * (q_heads / pool->kv_heads));
+  const int64_t rows = (int64_t)max_rows * (q_heads / pool->kv_heads);
+  const AttendKind widest = attend_kind(pool->format, rows);
+  const int D = pool->head_dim;
   size_t parts = 0;
   for (AttendKind k : {kFew1, kFew2, kTile, kF32})
-    if (k <= widest && (k == kF32) == (widest == kF32)) parts = std::max(parts, part_bytes(k, pool->head_dim));
-  *bytes = kWsHeader + kMaxParts * sizeof(uint32_t) + parts;
+    if (k <= widest && (k == kF32) == (widest == kF32))
+      parts = std::max(parts, part_bytes(k, D, max_parts(k, D, streams, pool->kv_heads, rows)));
+  *bytes = kZeroed + parts;
   return IPV_OK;
 }
 
@@ -412,8 +425,8 @@ ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const voi
       if (kind != kF32) plan(&a, kind, pool->head_dim, pool->format);  // (parts may be shorter then)
     }
     a.arrived = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + kWsHeader);
-    a.part_ml = reinterpret_cast<float*>(a.arrived + kMaxParts);
-    a.part = a.part_ml + (size_t)kMaxParts * attend_rows(kind, pool->head_dim) * 2;
+    a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + kZeroed);
+    a.part = a.part_ml + (size_t)a.blocks * attend_rows(kind, pool->head_dim) * 2;  // (a launch that splits has at most max_parts)
     const uint32_t grid = (uint32_t)(a.blocks + 7) / 8u * 8u;
     hipError_t e;
     switch (pool->format) {
