@@ -527,12 +527,18 @@ class PagePool:
             if K_scales is not None or V_scales is not None:
                 raise IpvError(ERR_ARG, "bf16 and fp32 pages have no scales")
             fmt, D = _dtype_code(K), X
-        self.K, self.V, self.K_scales, self.V_scales = K, V, K_scales, V_scales
+        self._tensors = K, V, K_scales, V_scales
         self.format, self.head_dim, self.device = fmt, D, K.device
         self.dtype = torch.float32 if fmt == PAGES_F32 else torch.bfloat16  # of queries and outputs
         self.shape = PageShape(P, L, H, T, D, fmt)
         self._dev = K.get_device()
         self._args = (ctypes.byref(self.shape), _ptr(K), _ptr(V), _ptr(K_scales), _ptr(V_scales))
+
+    # not to be replaced: their addresses are made into arguments once
+    K = property(lambda self: self._tensors[0])
+    V = property(lambda self: self._tensors[1])
+    K_scales = property(lambda self: self._tensors[2])
+    V_scales = property(lambda self: self._tensors[3])
 
     @classmethod
     def empty(cls, pages, layers, kv_heads, page_rows, head_dim, format, device="cuda"):  # noqa: A002

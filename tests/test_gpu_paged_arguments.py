@@ -103,3 +103,13 @@ def test_results_into_expanded_tensors():
     assert bool((one == 1).all()) and bool((q == 1).all())
     # a dimension of one may have any stride
     ipv.ipv_attend(pool, table, 40, 39, 0, q[:, :, :1], out[:, :, :1].as_strided((1, 4, 1, 64), (0, 192, 0, 1)), aws)
+
+
+def test_a_pools_tensors_stay():
+    """A pool's addresses are taken when it is made, so its tensors cannot be exchanged under it."""
+    pool, *_ = setup()
+    held = [pool.K, pool.V, pool.K_scales, pool.V_scales]
+    for name in ("K", "V", "K_scales", "V_scales"):
+        with pytest.raises(AttributeError):
+            setattr(pool, name, torch.zeros_like(pool.K))
+    assert all(a is b for a, b in zip(held, (pool.K, pool.V, pool.K_scales, pool.V_scales)))
