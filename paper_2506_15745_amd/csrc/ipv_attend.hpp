@@ -122,7 +122,7 @@ __device__ __forceinline__ void rare() { asm volatile("" ::: "memory"); }
 
 // How far a maximum may grow before the sums are rescaled to it, in the kernel of many rows and that of
 // fp32 pools: weights stay below 2^8, which costs the fp32 sums nothing. Weights in bf16 it costs the largest
-// one's exactness: rescaled at once that is 1, lazily it is rounded like the others (by up to 2^-9 of it), and
+// one's exactness: rescaled at once that is 1, lazily it is rounded like the others (by up to 2^-8 of it), and
 // since it often has the largest part in a result, the error against 64 bits grows, of a frame of 196 tokens of 28
 // heads over 6272 positions from 0.0018 to 0.0022 of the result's norm (0.0017 of it the result's own rounding).
 // At once costs time: that frame 39.0 -> 40.7 us, its windowed prompt 130 -> 136, 2048 tokens of 64 heads over 32768
@@ -687,8 +687,8 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
       top = lanes_max<4>(top) * a.c;
       // The sums are rescaled as soon as a maximum grows, so that the largest weight is 1 and not rounded; only
       // where a maximum has grown (four tokens of 8 streams of 64 heads of 256 in e2m1 over 32768 positions 183 us,
-      // in every tile 214). Lazily, as the kernel of many rows does it, they take 162 (in e4m3 200
-      // and 219, bf16 353 and 356; single tokens of heads of 128 2% less), and their error against 64 bits grows from 0.0019 to 0.0023.
+      // in every tile 214). Rescaled lazily, as by the kernel of many rows, those would take 162 us, in e4m3 200 in
+      // place of 219, in bf16 353 in place of 356, and be off by 0.0023 of the result's norm in place of 0.0019.
       if (__ballot(top > m[nb]) != 0) {
         rare();
         top = fmaxf(top, m[nb]);
@@ -779,9 +779,9 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
 // read them; the next tiles' rows are in flight meanwhile. Two waves a SIMD, or one
 // for D = 256, whose sums and queries take 192 accumulation registers. Bound by the matrix
 // unit, at a clock that its load lowers: 2048 tokens of 64 heads over 32768 positions of 8,
-// D = 128, take 1820 us, 1170 TFLOP/s at 60% of the unit's cycles and 1.86 GHz (the library's
-// product of random bf16 matrices reaches 1490); fp8 1890, fp4 1805; D = 64 in half the
-// operations 900 TFLOP/s, where the softmax's instructions weigh twice, D = 256 960.
+// D = 128, take 1790 to 1890 us, 1130 to 1190 TFLOP/s at 60% of the unit's cycles and 1.86 GHz (the library's
+// product of random bf16 matrices reaches 1490); fp8 1860 to 1930. D = 64: half the products with the
+// same softmax instructions, 38% of the unit's cycles, 900 TFLOP/s; D = 256, one wave a SIMD: 40%, 950.
 // 128 rows a workgroup, two of them a CU: 2045 us; 64 rows a wave, one wave a SIMD: 3135.
 // Short calls are bound by the way to their first rows and back: a frame of 196 tokens of 28 heads
 // over 6272 positions 33 us and 7.6 for the join, of 12 at the library product's rate.

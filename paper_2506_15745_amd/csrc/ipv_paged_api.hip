@@ -214,14 +214,17 @@ ipv_status check_grids(const ipv_page_shape* s, int32_t streams, const int32_t* 
   return IPV_OK;
 }
 
-// What `blocks` workgroups of `per` key tiles take, `fill` of them at once, us, as measured. A workgroup
-// costs its tiles and, around them, its start, the wait for its first rows and the store of its
+// What `blocks` workgroups of `per` key tiles take, `fill` of them at once, us, as measured on bf16 and fp32
+// pools. A workgroup costs its tiles and, around them, its start, the wait for its first rows and the store of its
 // result or part; joining parts costs a launch and their bytes. A last round that does not fill the
-// card costs a whole one, but for bf16 heads of 128: a full card lowers its clock for their products.
+// card costs a whole one, but for heads of 128: a full card lowers its clock for their products.
 // Against no parts, where the row tiles do not fill the card's rounds: 300 tokens of 64 heads of 256 over
-// 8192 positions 293 -> 255 us, 600 of 64 heads of 64 145 -> 125, 1100 of 64 heads of 128 383 -> 343; fp32,
+// 8192 positions 276 -> 220 us, 600 of 64 heads of 64 147 -> 124, 1100 of 64 heads of 128 385 -> 343; fp32,
 // 300 tokens of 28 heads of 128 over 6272, 452 -> 332; where they leave most of it empty, 196 of those
-// in bf16, 144 -> 38. Against parts that always fill a round: 400 tokens of 64 heads over 400 38 -> 21.
+// in bf16, 146 -> 41. Against parts that always fill a round: 400 tokens of 64 heads over 400 38 -> 21.
+// Tiles of e4m3 and e2m1 take up to a seventh longer, which chooses no worse: those calls 353 -> 260 and 345 -> 252,
+// 159 -> 130 and 165 -> 134, 410 -> 354 and 397 -> 348, 165 -> 43 and 158 -> 41; of heads of 128 with whole last
+// rounds instead, 600 tokens of 64 heads over 8192 189 -> 193 and 185 -> 189, 1500 415 -> 408 and 403 -> 399.
 double attend_us(AttendKind kind, int D, int64_t per, int64_t blocks, int32_t fill, bool parts) {
   const int size = D == 32 ? 0 : D == 64 ? 1 : D == 128 ? 2 : 3;
   static constexpr double kTileUs[4] = {0.8, 1.06, 1.8, 2.0}, kF32Us[4] = {0.67, 1.27, 1.1, 2.2};
