@@ -28,6 +28,13 @@
  *   ipv_attend       attention of new tokens (one or many) over the pages or
  *                    over the cache itself, causal, with a sliding window and
  *                    first rows that stay visible
+ *   ipv_qkv_write    new tokens of a layer: queries and keys normed for each head
+ *                    and rotated, keys and values into the pages
+ *   ipv_block_bounds, ipv_block_select, ipv_attend_blocks
+ *                    attention over the few blocks of rows that can score highest
+ *                    for a query, by bounds of each block's keys
+ *   ipv_page_compact, ipv_page_copy
+ *                    kept rows into new pages, pages onto other pages
  *
  * A `mode` argument (IPV_MODE_* bits, 0 = the method as published) selects the
  * variants of the paper's ablation (Tab. 5: TaR Reverse, VaN Reverse, TaR
@@ -117,15 +124,19 @@ enum {
   IPV_DEV_RECENT_OVER = 4u,    /* recent window |R| larger than the budget: keep_idx set to 0..C-1 (the
                                   compaction then moves nothing) */
   IPV_DEV_BAD_KEEP = 8u,       /* keep_idx[j] outside [j, n) or not above keep_idx[j-1]: the compaction
-                                  chunk (512 rows) holding row j was not moved */
-  IPV_DEV_NAN = 16u,           /* a candidate score is NaN: its rank is unspecified; ipv_page_write: an infinite
-                                  or NaN element in a block of a quantised row */
+                                  chunk (512 rows) holding row j was not moved; ipv_page_compact: keep_idx[j]
+                                  outside [0, n): row j was left out */
+  IPV_DEV_NAN = 16u,           /* a candidate score is NaN: its rank is unspecified; ipv_page_write, ipv_qkv_write and
+                                  ipv_page_compact: an infinite or NaN element in a block of a quantised row */
   IPV_DEV_WAIT_TIMEOUT = 32u,  /* compaction: a chunk's bounded wait expired or its walk's counters were
                                   not zero (a workspace shared by overlapping calls); its rows were not
                                   moved */
   IPV_DEV_BAD_PAGE = 64u       /* paged cache: a page_table entry outside [0, pages): ipv_page_write left the
                                   row out, ipv_page_read and ipv_attend read page 0 in its place (ipv_attend:
-                                  the entry of a row that some query sees; the others may hold anything) */
+                                  the entry of a row that some query sees; the others may hold anything);
+                                  ipv_qkv_write, ipv_block_bounds, ipv_page_compact and ipv_page_copy left the
+                                  row, the block or the page out, ipv_block_select and ipv_attend_blocks read
+                                  page 0 in its place (for blocks that some query of the call can pick, or picked) */
 };
 
 /*
@@ -458,6 +469,124 @@ ipv_status ipv_attend(const ipv_page_shape* pool, const void* K_pages, const voi
                       const void* q, const int64_t* q_strides, int32_t q_heads, int32_t max_rows, double scale,
                       int32_t window, int32_t sinks, void* out, const int64_t* out_strides, float* lse, void* ws,
                       size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------ new tokens, blocks, pages
+ * A block is block_rows consecutive rows of a page's (layer, head): a multiple of 16
+ * that divides page_rows. Its bounds are the lowest and the highest element of each
+ * channel over the keys of its rows as they are stored (of the values that they stand
+ * for): bounds is [pages, layers, kv_heads, page_rows / block_rows, 2, D], bf16 (fp32 for
+ * IPV_PAGES_F32; both exact), device, 16-byte aligned. Where a key element is NaN one
+ * of its channel's bounds is NaN. Where a call takes bounds, NULL (then block_rows is not
+ * looked at) means that none are kept. Positions [0, n) of a stream fill its blocks in
+ * order: block j holds rows [j * block_rows, (j + 1) * block_rows).
+ */
+
+/*
+ * New tokens of one layer. Token i < rows[b] of stream b stands at position
+ * first_row[b] + i; its queries are at q + b * q_strides[0] + a * q_strides[1] +
+ * i * q_strides[2] (query head a), its keys and values at k and v + b * kv_strides[0] +
+ * h * kv_strides[1] + i * kv_strides[2], in `dtype`. For each head of the queries (q_norm)
+ * and of the keys (k_norm; fp32 [D], device, 4-byte aligned; NULL: not normed)
+ *   y[d] = (x[d] * s) * norm[d],   s = 1 / sqrt(mean of x[d]^2 + eps),
+ * the mean and s in 64 bits, s then rounded to fp32, each product rounded once; then
+ * the pairs turn by rotary as in ipv_page_write. Queries go to q_out (out_strides, as q's;
+ * bf16, fp32 for IPV_PAGES_F32), keys and values into the pages, as ipv_page_write does;
+ * bounds of every block that received a row are made anew from its rows before
+ * first_row[b] + rows[b]. q_out may be q itself where type and strides are the same;
+ * otherwise it may not overlap the inputs. eps > 0 (a normal fp32 number). The mean of
+ * squares needs |x| below 1e150. The workspace is the 256 bytes of the error word.
+ * Streams that write must not share the pages they write to.
+ */
+ipv_status ipv_qkv_write(const ipv_page_shape* pool, void* K_pages, void* V_pages, uint8_t* K_scales, uint8_t* V_scales,
+                         void* bounds, int32_t block_rows, const int32_t* page_table, int32_t table_cols, int32_t streams,
+                         const int32_t* first_row, const int32_t* rows, int32_t layer, const void* q,
+                         const int64_t* q_strides, int32_t q_heads, const void* k, const void* v, const int64_t* kv_strides,
+                         int32_t dtype, const float* q_norm, const float* k_norm, double eps, const float* rotary,
+                         int32_t rotary_rows, void* q_out, const int64_t* out_strides, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/*
+ * Bounds of every block of layers [first_layer, first_layer + layers) that holds one of the
+ * positions first_row[b], ..., first_row[b] + rows[b] - 1, from its rows before first_row[b] +
+ * rows[b] (after ipv_page_write, say). The workspace is the 256 bytes of the error word.
+ */
+ipv_status ipv_block_bounds(const ipv_page_shape* pool, const void* K_pages, const uint8_t* K_scales, void* bounds,
+                            int32_t block_rows, const int32_t* page_table, int32_t table_cols, int32_t streams,
+                            const int32_t* first_row, const int32_t* rows, int32_t first_layer, int32_t layers, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/* Bytes of device workspace that every ipv_block_select and ipv_attend_blocks call with this pool, at most `streams`
+   streams, q_heads query heads, max_rows queries a stream, `top` blocks a query and max_tokens rows a stream needs: a
+   query's scores (8 bytes a block, at most about 128 MiB of them at a time) or the parts of split lists. Its first 4352
+   bytes must have been zeroed when it was allocated. */
+ipv_status ipv_blocks_workspace_bytes(const ipv_page_shape* pool, int32_t block_rows, int32_t streams, int32_t q_heads,
+                                      int32_t max_rows, int32_t top, int32_t max_tokens, size_t* bytes);
+
+/*
+ * The blocks that can score highest. Query i of stream b stands at p = q_first[b] + i and can
+ * pick among the blocks that hold a row j < n_tokens[b], j <= p: the first c of the stream. For KV
+ * head h, with the queries q_a of its q_heads / kv_heads heads and a block's bounds lo, hi,
+ *   score = sum over a and d of max(q_a[d] lo[d], q_a[d] hi[d]),
+ * which is no less than the sum over a of q_a . K_j for any row j of the block. Picked are the
+ * first first_blocks and the last last_blocks of the c blocks and, of the others, those with
+ * the highest scores (NaN above all others), ties to the lower block, min(top, c) in all:
+ * blocks (int32 [streams, kv_heads, max_rows, top], device, 4-byte aligned) receives them in
+ * ascending order, then -1. Sums are in 64 bits. Rows i >= q_rows[b] are left alone.
+ * Needs first_blocks + last_blocks <= top <= 4096.
+ */
+ipv_status ipv_block_select(const ipv_page_shape* pool, const void* bounds, int32_t block_rows, const int32_t* page_table,
+                            int32_t table_cols, int32_t streams, const int32_t* n_tokens, const int32_t* q_first,
+                            const int32_t* q_rows, int32_t layer, const void* q, const int64_t* q_strides, int32_t q_heads,
+                            int32_t max_rows, int32_t first_blocks, int32_t last_blocks, int32_t top, int32_t* blocks,
+                            void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Attention over lists of blocks: query i of head a of stream b, at position p = q_first[b] + i,
+ * sees the rows j < n_tokens[b], j <= p of the blocks that blocks[b][h][i] lists for its KV
+ * head h; out and lse as in ipv_attend. Lists may be in any order; an entry that is
+ * negative or holds no such row adds nothing, and rows of a block that is listed twice count
+ * twice. With bounds, the lists are made first, as ipv_block_select does, and are left in
+ * `blocks`; with bounds NULL they are read (first_blocks and last_blocks are not looked at).
+ * Queries, outputs, scale and results are those of ipv_attend; the largest weight is
+ * not rounded. One call gives the same bits every time.
+ */
+ipv_status ipv_attend_blocks(const ipv_page_shape* pool, const void* K_pages, const void* V_pages, const uint8_t* K_scales,
+                             const uint8_t* V_scales, const void* bounds, int32_t block_rows, const int32_t* page_table,
+                             int32_t table_cols, int32_t streams, const int32_t* n_tokens, const int32_t* q_first,
+                             const int32_t* q_rows, int32_t layer, const void* q, const int64_t* q_strides, int32_t q_heads,
+                             int32_t max_rows, double scale, int32_t first_blocks, int32_t last_blocks, int32_t top,
+                             int32_t* blocks, void* out, const int64_t* out_strides, float* lse, void* ws, size_t ws_bytes,
+                             void* stream);
+
+/*
+ * Compaction of a paged cache into other pages: for j < rows[b] <= C, row j of every
+ * (layer, head) slice of stream b, in the pages of new_table[b] (new_cols entries), becomes
+ * row keep_idx[b][l][h][j] (int32 [streams, layers, kv_heads, C], device, of all the pool's
+ * layers, in any order) of its n_tokens[b] rows in the pages of page_table[b]. Values are
+ * copied bit for bit, and so are keys without rotary and those of rows that keep their
+ * position. With rotary the others are turned back from position keep_idx and on to position j, as
+ * by ipv_page_read into fp32 and ipv_page_write, but that a block keeps its scale up to a largest
+ * magnitude of (1 + 2^-16) times the type's largest (it is rounded to that), so that stored values
+ * turned by next to nothing stay what they are. Both positions must be below rotary_rows. bounds:
+ * those of the new blocks are made. The pages written must not be among those read: the old ones, which
+ * other streams may share, are as they were. The workspace is the 256 bytes of the error word.
+ */
+ipv_status ipv_page_compact(const ipv_page_shape* pool, void* K_pages, void* V_pages, uint8_t* K_scales, uint8_t* V_scales,
+                            void* bounds, int32_t block_rows, const int32_t* page_table, int32_t table_cols,
+                            const int32_t* new_table, int32_t new_cols, int32_t streams, const int32_t* n_tokens,
+                            const int32_t* keep_idx, int32_t C, const int32_t* rows, const float* rotary,
+                            int32_t rotary_rows, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Pages onto other pages of the pool: the first `rows` rows of every (layer, head) of page
+ * from[i] become those of page to[i], i < count (both int32, device), with their scales and the
+ * bounds of the blocks that they reach into (of a block copied in part its bounds are still those of
+ * all the rows that it has there). No page may be written twice, or written and read, but that a
+ * page copied onto itself is left alone. The workspace is the 256 bytes of the error word.
+ */
+ipv_status ipv_page_copy(const ipv_page_shape* pool, void* K_pages, void* V_pages, uint8_t* K_scales, uint8_t* V_scales,
+                         void* bounds, int32_t block_rows, const int32_t* from, const int32_t* to, int32_t count,
+                         int32_t rows, void* ws, size_t ws_bytes, void* stream);
 
 /* Reset the workspace's device error word (a small kernel on `stream`). */
 ipv_status ipv_clear_device_errors(void* ws, size_t ws_bytes, void* stream);

@@ -14,9 +14,11 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libipv.so")
 SOURCES = [os.path.join(CSRC, "ipv_api.hip")]  # the compression pass
-# the paged cache: its entry points, and the attention kernels of each page format
+# the paged cache: its entry points, and the attention kernels of each page format (over rows in order, over lists of blocks)
 PAGED_SOURCES = [os.path.join(CSRC, f) for f in ("ipv_paged_api.hip", "ipv_attend_bf16.hip", "ipv_attend_f32.hip",
-                                                 "ipv_attend_fp8.hip", "ipv_attend_fp4.hip")]
+                                                 "ipv_attend_fp8.hip", "ipv_attend_fp4.hip", "ipv_rows_api.hip",
+                                                 "ipv_blocks_api.hip", "ipv_blocks_bf16.hip", "ipv_blocks_f32.hip",
+                                                 "ipv_blocks_fp8.hip", "ipv_blocks_fp4.hip")]
 HEADERS = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".hpp")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -38,6 +38,7 @@ struct AttendStream {
 };
 
 struct AttendArgs {
+  static constexpr bool kApart = true;  // (a launch of its own can join parts)
   Pool pool;
   int64_t layer_row;  // rows of a page before the layer's first head
   const char* q;
@@ -299,18 +300,6 @@ __device__ __forceinline__ float v_element(const Pool& p, int64_t row, int d) {
   return v;
 }
 
-// Scale bytes of a row as a 64-bit word.
-template <int D>
-__device__ __forceinline__ uint64_t load_scales(const uint8_t* scales, int64_t row) {
-  const uint8_t* p = scales + row * (D / kScaleBlock);
-  if (D == 32) return *p;
-  if (D == 64) return *reinterpret_cast<const uint16_t*>(p);
-  if (D == 128) return *reinterpret_cast<const uint32_t*>(p);
-  const uint32_t lo = reinterpret_cast<const uint32_t*>(p)[0], hi = reinterpret_cast<const uint32_t*>(p)[1];
-  return ((uint64_t)hi << 32) | lo;
-}
-__device__ __forceinline__ float scale_at(uint64_t w, int block) { return scale_of((uint32_t)(w >> (8 * block)) & 255u); }
-
 // Eight elements at 8 * s of a 16-byte (or shorter) piece of stored bytes, as bf16.
 template <int F>
 __device__ __forceinline__ Raw16 piece8(const uint32_t* w, int s, float scale) {
@@ -398,8 +387,8 @@ constexpr size_t few_wave_lds() {
 
 // Four elements of row r's result, and its lse: v, sum and top are the weighted
 // sum, the sum of the weights and the maximum they are relative to.
-template <int D, bool F32OUT>
-__device__ __forceinline__ void row_out(const AttendArgs& a, int b, int h, int r, int d, const F32x4& v, float top, float sum) {
+template <int D, bool F32OUT, class ARGS>
+__device__ __forceinline__ void row_out(const ARGS& a, int b, int h, int r, int d, const F32x4& v, float top, float sum) {
   const int tok = (int)fast_div((uint32_t)r, a.G_div), head = h * a.G + r - tok * a.G;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const int64_t at = (int64_t)b * a.o_b + (int64_t)head * a.o_h + (int64_t)tok * a.o_m + d;
@@ -412,8 +401,8 @@ __device__ __forceinline__ void row_out(const AttendArgs& a, int b, int h, int r
 // The waves' sums are in LDS: their total is the result of the first `rows` rows of the
 // row tile (rows r0, ... of the stream) or, where the keys are split, a part of it. The row
 // tile's last workgroup to come joins its parts, in their order.
-template <int D, int NR, bool F32OUT, size_t BYTES>
-__device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendStream& st, const Place& pl, int b, int r0, int rows,
+template <int D, int NR, bool F32OUT, size_t BYTES, class ARGS>
+__device__ __forceinline__ void join_parts(const ARGS& a, const AttendStream& st, const Place& pl, int b, int r0, int rows,
                                            char (&lds)[kFewWaves][BYTES], float (&lds_ml)[kFewWaves][NR][2], uint32_t* lds_last) {
   constexpr int STRIDE = JoinLds<D, NR>::STRIDE;
   static_assert(BYTES >= JoinLds<D, NR>::kWaveBytes && kFewWaves * BYTES >= sizeof(float) * NR * kMaxSplits, "LDS of the joining");
@@ -438,8 +427,11 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendStre
       row_out<D, F32OUT>(a, b, pl.h, r0 + r, d, v, top, sum);
     }
   }
-  if (st.splits <= 1 || a.join_apart) return;
-  if (!F32OUT && NR > 16 && join_rounds(17, D) > kJoinTrips) return;  // (as many rows always are)
+  if (st.splits <= 1) return;
+  if constexpr (ARGS::kApart) {
+    if (a.join_apart) return;
+    if (!F32OUT && NR > 16 && join_rounds(17, D) > kJoinTrips) return;  // (as many rows always are)
+  }
 
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's parts are written
   __syncthreads();

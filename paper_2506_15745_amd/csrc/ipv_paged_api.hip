@@ -7,80 +7,11 @@
 
 #include "../../include/ipv.h"
 #include "ipv_attend.hpp"
+#include "ipv_paged_host.hpp"
 
 using namespace ipv;
 
-#define IPV_TRY(x)               \
-  do {                           \
-    const ipv_status _s = (x);   \
-    if (_s != IPV_OK) return _s; \
-  } while (0)
-
 namespace {
-
-static_assert(kFmtBf16 == IPV_PAGES_BF16 && kFmtF32 == IPV_PAGES_F32 && kFmtFp8 == IPV_PAGES_FP8 && kFmtFp4 == IPV_PAGES_FP4,
-              "the formats of the header");
-static_assert((int)kFmtBf16 == IPV_BF16 && (int)kFmtF32 == IPV_F32, "rows in the cache's types");
-static_assert(kDevNan == IPV_DEV_NAN && kDevBadPage == IPV_DEV_BAD_PAGE, "the error bits of the header");
-
-constexpr int32_t kMaxPosition = 1 << 30;  // positions and their tiles' ends stay in 31 bits
-constexpr int64_t kGridThreads = 0xffffffffll;  // threads of a grid along one dimension, at most
-
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-ipv_status launched(hipError_t e) { return e == hipSuccess ? IPV_OK : IPV_ERR_HIP; }
-
-ipv_status check_pool_shape(const ipv_page_shape* s) {
-  if (!s) return IPV_ERR_NULL;
-  if (s->format < IPV_PAGES_BF16 || s->format > IPV_PAGES_FP4) return IPV_ERR_DTYPE;
-  if (s->pages < 1 || s->layers < 1 || s->kv_heads < 1 || s->page_rows < 1 || s->page_rows > kMaxPosition) return IPV_ERR_SHAPE;
-  if (s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128 && s->head_dim != 256) return IPV_ERR_SHAPE;
-  // rows of the pool, and their bytes, in 63 bits
-  const double rows = (double)s->pages * s->layers * s->kv_heads * s->page_rows;
-  if (rows > 0x1p50) return IPV_ERR_SHAPE;
-  return IPV_OK;
-}
-
-ipv_status check_pool(const ipv_page_shape* s, const void* K, const void* V, const uint8_t* Ks, const uint8_t* Vs,
-                      const int32_t* table, int32_t cols, int32_t streams, Pool* p) {
-  IPV_TRY(check_pool_shape(s));
-  const bool scaled = fmt_scaled(s->format);
-  if (!K || !V || (scaled && (!Ks || !Vs))) return IPV_ERR_NULL;
-  if (!aligned(K, 16) || !aligned(V, 16)) return IPV_ERR_ALIGN;
-  if (scaled && (!aligned(Ks, 4) || !aligned(Vs, 4))) return IPV_ERR_ALIGN;
-  if (table && !aligned(table, 4)) return IPV_ERR_ALIGN;
-  if (streams < 1 || cols < 1) return IPV_ERR_SHAPE;
-  if (!table && (cols != 1 || streams > s->pages)) return IPV_ERR_SHAPE;
-  p->K = static_cast<char*>(const_cast<void*>(K));
-  p->V = static_cast<char*>(const_cast<void*>(V));
-  p->Ks = const_cast<uint8_t*>(Ks);
-  p->Vs = const_cast<uint8_t*>(Vs);
-  p->table = table;
-  p->cols = cols;
-  p->pages = s->pages;
-  p->layer_rows = (int64_t)s->kv_heads * s->page_rows;
-  p->page_rows_all = (int64_t)s->layers * p->layer_rows;
-  p->T = make_fastdiv((uint32_t)s->page_rows);
-  return IPV_OK;
-}
-
-// Rows that a stream's table covers (at most: positions stay in 31 bits).
-int64_t table_rows(const ipv_page_shape* s, int32_t cols) {
-  return std::min<int64_t>((int64_t)cols * s->page_rows, kMaxPosition);
-}
-
-ipv_status check_strides(const int64_t* strides, int n) {
-  if (!strides) return IPV_ERR_NULL;
-  for (int i = 0; i < n; ++i)
-    if (strides[i] % 8 != 0) return IPV_ERR_ALIGN;
-  return IPV_OK;
-}
-
-ipv_status check_word(const void* ws, size_t ws_bytes, size_t need) {
-  if (!ws) return IPV_ERR_WORKSPACE;
-  if (!aligned(ws, 256)) return IPV_ERR_ALIGN;
-  return ws_bytes < need ? IPV_ERR_WORKSPACE : IPV_OK;
-}
 
 template <bool WRITE, int F, int X, int D>
 hipError_t page_launch(const PageCall& c, dim3 grid, hipStream_t st) {
@@ -173,7 +104,6 @@ ipv_status page_rows(const ipv_page_shape* s, const void* K_pages, const void* V
 int32_t attend_fill(AttendKind k, int D, int format) {
   return 256 * (k == kTile ? 1 : k == kF32 ? (D <= 64 ? 2 : 1) : few_per_cu(format, D, k == kFew1 ? 1 : 2));
 }
-constexpr int32_t kMaxParts = 1024;  // workgroups of a launch that splits, at most
 
 // The kernel for a call whose widest stream has `rows` rows a KV head.
 AttendKind attend_kind(int format, int64_t rows) {
@@ -188,16 +118,6 @@ int64_t max_parts(AttendKind k, int D, int32_t streams, int32_t kv_heads, int64_
 }
 
 size_t part_bytes(AttendKind k, int D, int64_t parts) { return (size_t)parts * attend_rows(k, D) * (size_t)(D + 2) * sizeof(float); }
-
-// The workspace: error word, counters (zero before and after a call), parts' maxima and sums, parts.
-constexpr size_t kZeroed = kWsHeader + kMaxParts * sizeof(uint32_t);
-static_assert(kZeroed == 4352, "the bytes to be zeroed that the header names");
-
-ipv_status check_heads(const ipv_page_shape* s, int32_t streams, int32_t q_heads, int32_t max_rows) {
-  if (streams < 1 || q_heads < 1 || max_rows < 1 || q_heads % s->kv_heads != 0) return IPV_ERR_SHAPE;
-  if ((int64_t)q_heads * max_rows > kMaxPosition) return IPV_ERR_SHAPE;
-  return IPV_OK;
-}
 
 // Every launch's row tiles as a grid (parts only add to it where it stays within kMaxParts).
 ipv_status check_grids(const ipv_page_shape* s, int32_t streams, const int32_t* q_rows, int32_t q_heads) {

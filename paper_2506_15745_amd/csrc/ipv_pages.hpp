@@ -55,6 +55,17 @@ __device__ __forceinline__ int64_t pool_row(const Pool& p, int32_t page, uint32_
   return (int64_t)(*bad ? 0 : page) * p.page_rows_all + (j - fast_div(j, p.T) * p.T.d);
 }
 
+// Where the bounds of blocks are: [page][slice][block of the page's slice].
+struct BlockMap {
+  FastDiv R;       // rows of a block, which divide a page's
+  int64_t slices;  // of a page: layers times heads
+  uint32_t per;    // blocks of a page's slice
+  // Number of the block that starts at that position, which lies in that page.
+  __device__ __forceinline__ int64_t block(int64_t page, uint32_t slice, uint32_t position, const FastDiv& T) const {
+    return (page * slices + slice) * per + fast_div(position - fast_div(position, T) * T.d, R);
+  }
+};
+
 // A scale byte as the power of two that the conversions take (255: NaN).
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
@@ -82,6 +93,18 @@ __device__ __forceinline__ Raw16 fp4_to_bf16(uint32_t x, float scale) {
   r.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3));
   return r;
 }
+
+// Scale bytes of a row as a 64-bit word.
+template <int D>
+__device__ __forceinline__ uint64_t load_scales(const uint8_t* scales, int64_t row) {
+  const uint8_t* p = scales + row * (D / kScaleBlock);
+  if (D == 32) return *p;
+  if (D == 64) return *reinterpret_cast<const uint16_t*>(p);
+  if (D == 128) return *reinterpret_cast<const uint32_t*>(p);
+  const uint32_t lo = reinterpret_cast<const uint32_t*>(p)[0], hi = reinterpret_cast<const uint32_t*>(p)[1];
+  return ((uint64_t)hi << 32) | lo;
+}
+__device__ __forceinline__ float scale_at(uint64_t w, int block) { return scale_of((uint32_t)(w >> (8 * block)) & 255u); }
 
 // ------------------------------------------------------------ rows in and out
 constexpr int kPageStreams = 128;  // streams of one launch (their counts travel in its arguments)
@@ -165,11 +188,13 @@ __device__ __forceinline__ uint32_t max_abs_bits(const float (&f)[8]) {
 
 // The scale byte of a block whose largest magnitude has these bits: the
 // smallest e >= -126 with amax <= TOP * 2^e, plus 127; TOP is 1.75 * 2^8
-// (e4m3) or 1.5 * 2^2 (e2m1). 255 for infinities and NaN.
-template <int F>
+// (e4m3) or 1.5 * 2^2 (e2m1). 255 for infinities and NaN. AGAIN: of stored values turned
+// anew, whose largest is often TOP * 2^e itself: up to (1 + 2^-16) times that, so that one that
+// a turn of next to nothing, or its rounding, made larger does not cost the block a bit.
+template <int F, bool AGAIN = false>
 __device__ __forceinline__ uint32_t scale_byte(uint32_t bits) {
   constexpr int shift = F == kFmtFp8 ? 8 : 2;
-  constexpr uint32_t top = F == kFmtFp8 ? 0x600000u : 0x400000u;  // mantissa bits of 1.75, 1.5
+  constexpr uint32_t top = (F == kFmtFp8 ? 0x600000u : 0x400000u) + (!AGAIN ? 0u : F == kFmtFp8 ? 224u : 192u);  // mantissa bits of 1.75, 1.5
   const int e = (int)(bits >> 23) - shift + ((bits & 0x7fffffu) > top ? 1 : 0);
   return bits >= 0x7f800000u ? 255u : (uint32_t)max(e, 1);
 }
@@ -228,6 +253,39 @@ __device__ __forceinline__ void store_scales(uint8_t* at, int thread, uint32_t e
   }
 }
 
+// A row into the pool, from the threads that hold it (lo and hi: eight elements of either half).
+// wl, wh: what is stored, as dwords of e4m3 (two) or e2m1 (one); el, eh: the scales' bytes.
+template <int F, int D, bool AGAIN = false>
+__device__ __forceinline__ void put_row(char* pages, uint8_t* scales, int64_t row, int d, const float (&lo)[8], const float (&hi)[8],
+                                        uint32_t* err, uint32_t (&wl)[2], uint32_t (&wh)[2], uint32_t& el, uint32_t& eh) {
+  if (!fmt_scaled(F)) {
+    store_row8<F, false>(pages, row * D + d, lo);
+    store_row8<F, false>(pages, row * D + D / 2 + d, hi);
+  } else {
+    uint32_t ml = max_abs_bits(lo), mh = max_abs_bits(hi);
+    if (D == 32) ml = mh = max(ml, mh);
+    ml = max(ml, dpp_u32<kDppXor1>(ml));
+    mh = max(mh, dpp_u32<kDppXor1>(mh));
+    if (D > 32) {
+      ml = max(ml, dpp_u32<kDppXor2>(ml));
+      mh = max(mh, dpp_u32<kDppXor2>(mh));
+    }
+    el = scale_byte<F, AGAIN>(ml), eh = scale_byte<F, AGAIN>(mh);
+    encode8<F>(lo, el, wl);
+    encode8<F>(hi, eh, wh);
+    char* at = pages + row * fmt_row_bytes(F, D);
+    if (F == kFmtFp8) {
+      *reinterpret_cast<U32x2*>(at + d) = U32x2{wl[0], wl[1]};
+      *reinterpret_cast<U32x2*>(at + D / 2 + d) = U32x2{wh[0], wh[1]};
+    } else {
+      *reinterpret_cast<uint32_t*>(at + d / 2) = wl[0];
+      *reinterpret_cast<uint32_t*>(at + D / 4 + d / 2) = wh[0];
+    }
+    store_scales<D>(scales + row * (D / kScaleBlock), d / 8, el, eh);
+    if (el == 255u || eh == 255u) atomicOr(err, kDevNan);
+  }
+}
+
 // blockIdx.x: kRows positions of a stream; .y: kPageSlices slices, of K or of V;
 // .z: stream. A workgroup's rows follow each other in the caller's slices and,
 // page by page, in the pool. Bound by the bytes: 28 layers of 4 heads of 3136 rows of 128, bf16 to
@@ -269,34 +327,8 @@ __global__ __launch_bounds__(kPageThreads) void k_page_write(PageCall c) {
     const uint32_t lh = g * kPageSlices + u;
     if (lh >= (uint32_t)c.LH) break;
     if (rot) turn(lo[u], hi[u], cs, sn, false);
-    const int64_t row = row0 + (int64_t)lh * c.pool.T.d;
-    if (!fmt_scaled(F)) {
-      store_row8<F, false>(dst, row * D + d, lo[u]);
-      store_row8<F, false>(dst, row * D + D / 2 + d, hi[u]);
-    } else {
-      uint32_t ml = max_abs_bits(lo[u]), mh = max_abs_bits(hi[u]);
-      if (D == 32) ml = mh = max(ml, mh);
-      ml = max(ml, dpp_u32<kDppXor1>(ml));
-      mh = max(mh, dpp_u32<kDppXor1>(mh));
-      if (D > 32) {
-        ml = max(ml, dpp_u32<kDppXor2>(ml));
-        mh = max(mh, dpp_u32<kDppXor2>(mh));
-      }
-      const uint32_t el = scale_byte<F>(ml), eh = scale_byte<F>(mh);
-      uint32_t wl[2], wh[2];
-      encode8<F>(lo[u], el, wl);
-      encode8<F>(hi[u], eh, wh);
-      char* at = dst + row * fmt_row_bytes(F, D);
-      if (F == kFmtFp8) {
-        *reinterpret_cast<U32x2*>(at + d) = U32x2{wl[0], wl[1]};
-        *reinterpret_cast<U32x2*>(at + D / 2 + d) = U32x2{wh[0], wh[1]};
-      } else {
-        *reinterpret_cast<uint32_t*>(at + d / 2) = wl[0];
-        *reinterpret_cast<uint32_t*>(at + D / 4 + d / 2) = wh[0];
-      }
-      store_scales<D>(sc + row * (D / kScaleBlock), d / 8, el, eh);
-      if (el == 255u || eh == 255u) atomicOr(c.err, kDevNan);
-    }
+    uint32_t wl[2], wh[2], el, eh;
+    put_row<F, D>(dst, sc, row0 + (int64_t)lh * c.pool.T.d, d, lo[u], hi[u], c.err, wl, wh, el, eh);
   }
 }
 

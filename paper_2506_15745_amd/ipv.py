@@ -40,7 +40,9 @@ TAR_REVERSE, VAN_REVERSE, TAR_ADJACENT, HEAD_SHARED, UNIFORM_SELECT = 1, 2, 4, 8
 PAGES_BF16, PAGES_F32, PAGES_FP8, PAGES_FP4 = range(4)
 SCALE_BLOCK = 32
 
-PAGED_EXPORTS = ("ipv_page_write", "ipv_page_read", "ipv_attend_workspace_bytes", "ipv_attend")
+PAGED_EXPORTS = ("ipv_page_write", "ipv_page_read", "ipv_attend_workspace_bytes", "ipv_attend", "ipv_qkv_write",
+                 "ipv_block_bounds", "ipv_blocks_workspace_bytes", "ipv_block_select", "ipv_attend_blocks", "ipv_page_compact",
+                 "ipv_page_copy")
 EXPORTS = PAGED_EXPORTS + (
            "ipv_workspace_bytes", "ipv_tar_scores", "ipv_van_scores", "ipv_select", "ipv_compact",
            "ipv_compress", "ipv_compress_timed", "ipv_compress_noalloc", "ipv_append", "ipv_ckv_step", "ipv_ckv_stream",
@@ -127,6 +129,15 @@ def _paged() -> ctypes.CDLL:
         L.ipv_attend_workspace_bytes.argtypes = [ps, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
         L.ipv_attend.argtypes = [ps, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, i32, vp, vp, i32, i32, f64, i32, i32, vp,
                                  vp, vp, vp, sz, vp]
+        L.ipv_qkv_write.argtypes = [ps, vp, vp, vp, vp, vp, i32, vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, vp, vp, i32, vp, vp, f64,
+                                    vp, i32, vp, vp, vp, sz, vp]
+        L.ipv_block_bounds.argtypes = [ps, vp, vp, vp, i32, vp, i32, i32, vp, vp, i32, i32, vp, sz, vp]
+        L.ipv_blocks_workspace_bytes.argtypes = [ps, i32, i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+        L.ipv_block_select.argtypes = [ps, vp, i32, vp, i32, i32, vp, vp, vp, i32, vp, vp, i32, i32, i32, i32, i32, vp, vp, sz, vp]
+        L.ipv_attend_blocks.argtypes = [ps, vp, vp, vp, vp, vp, i32, vp, i32, i32, vp, vp, vp, i32, vp, vp, i32, i32, f64, i32, i32,
+                                        i32, vp, vp, vp, vp, vp, sz, vp]
+        L.ipv_page_compact.argtypes = [ps, vp, vp, vp, vp, vp, i32, vp, i32, vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, sz, vp]
+        L.ipv_page_copy.argtypes = [ps, vp, vp, vp, vp, vp, i32, vp, vp, i32, i32, vp, sz, vp]
         for name in PAGED_EXPORTS:
             getattr(L, name).restype = ctypes.c_int
         _paged_lib = L
@@ -723,6 +734,269 @@ def ipv_attend(pool, page_table, n_tokens, q_first, layer, q, out, ws, q_rows=No
                              None if lse is None else _ptr(lse), at, ws.nbytes, _stream(stream))
     if rc != OK:
         _check(rc, "ipv_attend")
+
+
+class BlockBounds:
+    """Bounds of the keys of every block of `block_rows` rows of a pool's pages (a multiple of
+    16 that divides their rows): values [P, L, H, T / block_rows, 2, D] in the pool's dtype, each
+    channel's lowest and highest element (zeros until they are made)."""
+
+    def __init__(self, pool: PagePool, block_rows: int, values=None):
+        s = pool.shape
+        if block_rows < 16 or block_rows % 16 or s.page_rows % block_rows:
+            raise IpvError(ERR_SHAPE, "blocks of %d rows in pages of %d" % (block_rows, s.page_rows))
+        shape = (s.pages, s.layers, s.kv_heads, s.page_rows // block_rows, 2, pool.head_dim)
+        if values is None:
+            values = torch.zeros(shape, dtype=pool.dtype, device=pool.device)
+        _expect("values", values, shape, pool.dtype, pool.device)
+        self.pool, self.block_rows, self._values, self._at = pool, block_rows, values, _ptr(values)
+
+    # not to be replaced: its address is made into an argument once
+    values = property(lambda self: self._values)
+
+
+def _bounds_args(pool, bounds):
+    if bounds is None:
+        return None, 0
+    if bounds.pool is not pool:
+        raise IpvError(ERR_ARG, "bounds of another pool")
+    return bounds._at, bounds.block_rows
+
+
+def _float_row(what, t, n, pool):
+    """(pointer of) an fp32 row of n elements, or None."""
+    if t is None:
+        return None
+    _expect(what, t, (n,), torch.float32, pool.device)
+    return _ptr(t)
+
+
+def _angle_args(pool, rotary, at):
+    """(pointer, positions) of a table of angles, or of none."""
+    if rotary is None:
+        return None, 0
+    if rotary.dtype is not torch.float32 or rotary.dim() != 3 or tuple(rotary.shape[1:]) != (pool.head_dim // 2, 2):
+        raise IpvError(ERR_SHAPE, "rotary must be fp32 [positions, %d, 2]" % (pool.head_dim // 2))
+    if rotary.get_device() != pool._dev:
+        raise IpvError(ERR_ARG, "rotary is on %s, the pool on %s" % (rotary.device, pool.device))
+    return _ptr(rotary) or at, rotary.shape[0]
+
+
+def ipv_qkv_write(pool, page_table, first_row, layer, q, k, v, q_out, ws, rows=None, q_norm=None, k_norm=None, eps=1e-6, rotary=None,
+                  bounds=None, stream=None):
+    """New tokens of one layer: queries q [B, q_heads, M, D] and keys and values k, v [B, H, M, D]
+    (bf16 or fp32, any strides with the last dimension contiguous, k's and v's the same) of tokens at positions
+    first_row[b], first_row[b] + 1, ... Each head of the queries and of the keys is divided by the root of its
+    mean square plus eps and multiplied by q_norm or k_norm (fp32 [D]; None: not), then turned to its position by
+    rotary (fp32 [positions, D / 2, 2], or None). Queries go to q_out (the pool's dtype; q itself where it is that),
+    keys and values into the pages; bounds (BlockBounds, or None) of the blocks written to are brought up to date. rows: all
+    M, or how many of each stream."""
+    shape, kv, dev, table, cols = q.shape, k.shape, pool._dev, None, 1
+    if len(shape) != 4 or shape[3] != pool.head_dim:
+        raise IpvError(ERR_SHAPE, "q must be [B, q_heads, rows, %d]" % pool.head_dim)
+    B, A, M, D = shape
+    if kv != (B, pool.shape.kv_heads, M, D) or v.shape != kv:
+        raise IpvError(ERR_SHAPE, "k and v must be [%d, %d, %d, %d]" % (B, pool.shape.kv_heads, M, D))
+    if k.dtype is not q.dtype or v.dtype is not q.dtype:
+        raise IpvError(ERR_DTYPE, "q, k and v must have one dtype")
+    if q_out.shape != shape:
+        raise IpvError(ERR_SHAPE, "q_out must have q's shape")
+    if q_out.dtype is not pool.dtype:
+        raise IpvError(ERR_DTYPE, "q_out must be %s" % pool.dtype)
+    k_strides, out_strides = k.stride(), q_out.stride()
+    q_at, k_at, out_at = _stride_array(q.stride(), shape), _stride_array(k_strides, kv), _stride_array(out_strides, shape)
+    if v.stride() != k_strides and list(_stride_array(v.stride(), kv)) != list(k_at):
+        raise IpvError(ERR_SHAPE, "k and v must have the same strides")
+    if 0 in out_strides:
+        _not_expanded("q_out", out_strides, shape)
+    if rows is None:
+        rows = M
+    elif (rows if isinstance(rows, int) else max(rows, default=0)) > M:
+        raise IpvError(ERR_SHAPE, "more rows than the tensor's %d" % M)
+    if page_table is not None:
+        table, cols = _table(pool, page_table, B)
+    if ws is None or ws.get_device() != dev or q.get_device() != dev or k.get_device() != dev or v.get_device() != dev or \
+            q_out.get_device() != dev:
+        _same_gpu(pool, ws, q=q, k=k, v=v, q_out=q_out)
+    first, counts_ = _host_counts(first_row, B, "first_row"), _host_counts(rows, B, "rows")
+    if not -_I32 <= layer < _I32:
+        _whole32("layer", layer)
+    at = _ptr(ws)  # also stands for tensors without elements, whose own addresses are null
+    angles, positions = _angle_args(pool, rotary, at)
+    bound, block_rows = _bounds_args(pool, bounds)
+    rc = _paged().ipv_qkv_write(*pool._args, bound, block_rows, table, cols, B, first.buffer_info()[0], counts_.buffer_info()[0], layer,
+                                q.data_ptr() or at, q_at, A, k.data_ptr() or at, v.data_ptr() or at, k_at, _dtype_code(q),
+                                _float_row("q_norm", q_norm, D, pool), _float_row("k_norm", k_norm, D, pool), eps, angles, positions,
+                                q_out.data_ptr() or at, out_at, at, ws.nbytes, _stream(stream))
+    if rc != OK:
+        _check(rc, "ipv_qkv_write")
+
+
+def ipv_block_bounds(pool, page_table, first_row, rows, bounds, ws, first_layer=0, layers=None, stream=None):
+    """The bounds (BlockBounds) of every block that holds one of the positions first_row[b], ...,
+    first_row[b] + rows[b] - 1, made from its rows before first_row[b] + rows[b] (ints, or sequences with one per
+    stream; without a page_table both ints mean all of the pool's pages), of layers first_layer, ... (layers: how many; None: all)."""
+    if page_table is not None:
+        table, cols = _table(pool, page_table, page_table.shape[0])
+        B = page_table.shape[0]
+    else:
+        table, cols, B = None, 1, next((len(x) for x in (first_row, rows) if not isinstance(x, int)), pool.shape.pages)
+    _same_gpu(pool, ws)
+    first, counts_ = _host_counts(first_row, B, "first_row"), _host_counts(rows, B, "rows")
+    layers = pool.shape.layers - first_layer if layers is None else layers
+    _whole32("first_layer, layers", first_layer, layers)
+    if bounds is None:
+        raise IpvError(ERR_NULL, "bounds are required")
+    bound, block_rows = _bounds_args(pool, bounds)
+    _check(_paged().ipv_block_bounds(pool._args[0], pool._args[1], pool._args[3], bound, block_rows, table, cols, B,
+                                     first.buffer_info()[0], counts_.buffer_info()[0], first_layer, layers, _ptr(ws), ws.nbytes,
+                                     _stream(stream)), "ipv_block_bounds")
+
+
+def blocks_workspace_bytes(pool: PagePool, block_rows: int, streams: int, q_heads: int, max_rows: int, top: int, max_tokens: int) -> int:
+    _whole32("ipv_blocks_workspace_bytes", block_rows, streams, q_heads, max_rows, top, max_tokens)
+    out = ctypes.c_size_t(0)
+    _check(_paged().ipv_blocks_workspace_bytes(pool._args[0], block_rows, streams, q_heads, max_rows, top, max_tokens, ctypes.byref(out)),
+           "ipv_blocks_workspace_bytes")
+    return out.value
+
+
+def alloc_blocks_workspace(bounds: BlockBounds, streams: int, q_heads: int, max_rows: int, top: int, max_tokens: int) -> torch.Tensor:
+    """A workspace for ipv_block_select and ipv_attend_blocks calls of at most these sizes (top: blocks a query; max_tokens:
+    rows of a stream): zeros where it has to be."""
+    pool = bounds.pool
+    ws = torch.empty(blocks_workspace_bytes(pool, bounds.block_rows, streams, q_heads, max_rows, top, max_tokens), dtype=torch.uint8,
+                     device=pool.device)
+    ws[:4352] = 0
+    return ws
+
+
+def _lists(pool, blocks, B, M):
+    """(pointer, entries) of lists of blocks [B, H, M, top]."""
+    shape = blocks.shape
+    if blocks.dtype is not torch.int32 or len(shape) != 4 or shape[:3] != (B, pool.shape.kv_heads, M):
+        raise IpvError(ERR_SHAPE, "blocks must be int32 [%d, %d, %d, entries]" % (B, pool.shape.kv_heads, M))
+    if blocks.get_device() != pool._dev:
+        raise IpvError(ERR_ARG, "blocks is on %s, the pool on %s" % (blocks.device, pool.device))
+    return _ptr(blocks), shape[3]
+
+
+def ipv_block_select(pool, page_table, bounds, n_tokens, q_first, layer, q, blocks, ws, q_rows=None, first_blocks=0, last_blocks=1,
+                     stream=None):
+    """For each query of q ([B, q_heads, M, D], the pool's dtype; query i of stream b at position q_first[b] + i) and KV
+    head the blocks, among those that hold one of the first n_tokens[b] rows up to the query, whose bounds allow the largest
+    sum of its heads' scores: into blocks, int32 [B, H, M, top], in ascending order, then -1. The first first_blocks and the
+    last last_blocks of them are always picked. q_rows: queries of each stream (M if None)."""
+    shape, dev, table, cols = q.shape, pool._dev, None, 1
+    if len(shape) != 4 or shape[3] != pool.head_dim:
+        raise IpvError(ERR_SHAPE, "q must be [B, q_heads, rows, %d]" % pool.head_dim)
+    if q.dtype is not pool.dtype:
+        raise IpvError(ERR_DTYPE, "q must be %s" % pool.dtype)
+    B, A, M, _ = shape
+    if page_table is not None:
+        table, cols = _table(pool, page_table, B)
+    if bounds is None:
+        raise IpvError(ERR_NULL, "bounds are required")
+    bound, block_rows = _bounds_args(pool, bounds)
+    listed, top = _lists(pool, blocks, B, M)
+    _same_gpu(pool, ws, q=q)
+    n, first = _host_counts(n_tokens, B, "n_tokens"), _host_counts(q_first, B, "q_first")
+    rows = _host_counts(M if q_rows is None else q_rows, B, "q_rows")
+    _whole32("layer, first_blocks, last_blocks", layer, first_blocks, last_blocks)
+    at = _ptr(ws)
+    _check(_paged().ipv_block_select(pool._args[0], bound, block_rows, table, cols, B, n.buffer_info()[0], first.buffer_info()[0],
+                                     rows.buffer_info()[0], layer, q.data_ptr() or at, _stride_array(q.stride(), shape), A, M or 1,
+                                     first_blocks, last_blocks, top, listed or at, at, ws.nbytes, _stream(stream)), "ipv_block_select")
+
+
+def ipv_attend_blocks(pool, page_table, n_tokens, q_first, layer, q, blocks, out, ws, bounds=None, block_rows=None, q_rows=None,
+                      scale=None, first_blocks=0, last_blocks=1, lse=None, stream=None):
+    """Attention as ipv_attend's over the rows of the blocks that blocks (int32 [B, H, M, top]) lists for each query and KV
+    head. With bounds the lists are made first, as ipv_block_select does, and left in blocks; without, they are
+    read as they are (in any order, negative entries and blocks past the query adding nothing) and block_rows says how many
+    rows a block has."""
+    shape, dev, table, cols = q.shape, pool._dev, None, 1
+    if len(shape) != 4 or shape[3] != pool.head_dim:
+        raise IpvError(ERR_SHAPE, "q must be [B, q_heads, rows, %d]" % pool.head_dim)
+    if q.dtype is not pool.dtype or out.dtype is not pool.dtype:
+        raise IpvError(ERR_DTYPE, "q and out must be %s" % pool.dtype)
+    if out.shape != shape:
+        raise IpvError(ERR_SHAPE, "out must have q's shape")
+    B, A, M, D = shape
+    if lse is not None:
+        _expect("lse", lse, (B, A, M), torch.float32, pool.device)
+    if page_table is not None:
+        table, cols = _table(pool, page_table, B)
+    bound, rows_of = _bounds_args(pool, bounds)
+    if bounds is None:
+        if block_rows is None:
+            raise IpvError(ERR_ARG, "without bounds block_rows is required")
+        _whole32("block_rows", block_rows)
+        rows_of = block_rows
+    elif block_rows is not None and block_rows != rows_of:
+        raise IpvError(ERR_ARG, "bounds are of blocks of %d rows" % rows_of)
+    listed, top = _lists(pool, blocks, B, M)
+    if ws is None or ws.get_device() != dev or q.get_device() != dev or out.get_device() != dev:
+        _same_gpu(pool, ws, q=q, out=out)
+    n, first = _host_counts(n_tokens, B, "n_tokens"), _host_counts(q_first, B, "q_first")
+    rows = _host_counts(M if q_rows is None else q_rows, B, "q_rows")
+    q_strides, out_strides = q.stride(), out.stride()
+    q_at = _stride_array(q_strides, shape)
+    if 0 in out_strides:
+        _not_expanded("out", out_strides, shape)
+    if not (-_I32 <= layer < _I32 and -_I32 <= first_blocks < _I32 and -_I32 <= last_blocks < _I32):
+        _whole32("layer, first_blocks, last_blocks", layer, first_blocks, last_blocks)
+    at = _ptr(ws)  # also stands for tensors without elements, whose own addresses are null
+    rc = _paged().ipv_attend_blocks(*pool._args, bound, rows_of, table, cols, B, n.buffer_info()[0], first.buffer_info()[0],
+                                    rows.buffer_info()[0], layer, q.data_ptr() or at, q_at, A, M or 1,
+                                    D ** -0.5 if scale is None else scale, first_blocks, last_blocks, top, listed or at,
+                                    out.data_ptr() or at, q_at if out_strides == q_strides else _stride_array(out_strides, shape),
+                                    None if lse is None else _ptr(lse) or at, at, ws.nbytes, _stream(stream))
+    if rc != OK:
+        _check(rc, "ipv_attend_blocks")
+
+
+def ipv_page_compact(pool, page_table, new_table, n_tokens, keep_idx, ws, rows=None, rotary=None, bounds=None, stream=None):
+    """Row j < rows[b] (all C if None) of every slice of stream b, in the pages of new_table[b], becomes row keep_idx[b, l, h, j]
+    (int32 [B, L, H, C], as ipv_select writes it) of the n_tokens[b] rows in the pages of page_table[b], which may not be
+    among the new ones. With rotary keys are turned from the position that they had to the one that they get; bounds
+    (BlockBounds, or None) of the new blocks are made."""
+    s, shape, table, cols = pool.shape, keep_idx.shape, None, 1
+    if keep_idx.dtype is not torch.int32 or len(shape) != 4 or tuple(shape[1:3]) != (s.layers, s.kv_heads):
+        raise IpvError(ERR_SHAPE, "keep_idx must be int32 [B, %d, %d, C]" % (s.layers, s.kv_heads))
+    B, C = shape[0], shape[3]
+    if page_table is not None:
+        table, cols = _table(pool, page_table, B)
+    if new_table is None:
+        raise IpvError(ERR_NULL, "new_table is required")
+    new, new_cols = _table(pool, new_table, B)
+    _same_gpu(pool, ws, keep_idx=keep_idx)
+    n, counts_ = _host_counts(n_tokens, B, "n_tokens"), _host_counts(C if rows is None else rows, B, "rows")
+    at = _ptr(ws)
+    angles, positions = _angle_args(pool, rotary, at)
+    bound, block_rows = _bounds_args(pool, bounds)
+    rc = _paged().ipv_page_compact(*pool._args, bound, block_rows, table, cols, new, new_cols, B, n.buffer_info()[0], _ptr(keep_idx) or at,
+                                   C, counts_.buffer_info()[0], angles, positions, at, ws.nbytes, _stream(stream))
+    if rc != OK:
+        _check(rc, "ipv_page_compact")
+
+
+def ipv_page_copy(pool, from_pages, to_pages, ws, rows=None, bounds=None, stream=None):
+    """Pages from_pages[i] onto to_pages[i] (int32 [N], on the pool's GPU), or the first `rows` rows of their slices, with
+    their scales and bounds (BlockBounds, or None). No page may be written twice, or written and read by one call (but that
+    one copied onto itself is left alone)."""
+    for what, t in (("from_pages", from_pages), ("to_pages", to_pages)):
+        if t.dtype is not torch.int32 or t.dim() != 1 or t.shape != from_pages.shape:
+            raise IpvError(ERR_SHAPE, "%s must be int32 [N]" % what)
+    _same_gpu(pool, ws, from_pages=from_pages, to_pages=to_pages)
+    rows = pool.shape.page_rows if rows is None else rows
+    _whole32("rows", rows)
+    at = _ptr(ws)
+    bound, block_rows = _bounds_args(pool, bounds)
+    rc = _paged().ipv_page_copy(*pool._args, bound, block_rows, _ptr(from_pages) or at, _ptr(to_pages) or at, from_pages.shape[0], rows,
+                                at, ws.nbytes, _stream(stream))
+    if rc != OK:
+        _check(rc, "ipv_page_copy")
 
 
 class Compressor:
