@@ -13,8 +13,8 @@ namespace ipv {
 
 typedef double F64x4 __attribute__((ext_vector_type(4)));
 
-// ------------------------------------------------------------ scores
-constexpr int kSelectThreads = 256;
+// ------------------------------------------------------------ selection
+constexpr int kSelectThreads = 256, kSelectWaves = kSelectThreads / kWave;
 constexpr int kScoreTile = 16;  // queries, and blocks, of a product
 
 struct SelectArgs {
@@ -32,6 +32,8 @@ struct SelectArgs {
   double* scores;  // [stream][head][query of the launch][padded]
   int32_t* blocks;
   uint32_t* err;
+  uint32_t* arrived;  // workgroups of a tile of queries that have left their scores: zero before and after a call
+  int32_t spread;     // counters from one to the next: apart, since one line takes them one after the other
   int32_t n[kAttendStreams], first[kAttendStreams], rows[kAttendStreams];
 };
 
@@ -41,69 +43,6 @@ __device__ __forceinline__ int32_t candidates(const SelectArgs& a, int b, int i)
   return (int32_t)fast_div((uint32_t)held + a.map.R.d - 1u, a.map.R);
 }
 
-// blockIdx.x: tiles of blocks, a wave each in turn; .y: head and tile of queries; .z: stream. Q+ and Q- of
-// the tile's queries are made in LDS in the order in which the product takes them: step 8 c + e has channel
-// 8 (4 c + k) + e in its place k, so that a lane's 16 bytes of bounds are operands of eight steps.
-template <int FB, int D>
-__global__ __launch_bounds__(kSelectThreads) void k_block_scores(SelectArgs a) {
-  constexpr int STEPS = D / 2, CHUNKS = D / 16;  // of four terms; of eight steps
-  __shared__ double lds[STEPS * kWave];
-  const int b = blockIdx.z, q_tiles = (a.mq + kScoreTile - 1) / kScoreTile;
-  const int h = blockIdx.y / q_tiles, i0 = a.m0 + blockIdx.y % q_tiles * kScoreTile;
-  const int i1 = min(min(i0 + kScoreTile, a.m0 + a.mq), a.rows[b]);
-  if (i0 >= i1) return;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int32_t most = candidates(a, b, i1 - 1), tiles = (most + kScoreTile - 1) / kScoreTile;
-  if ((int)blockIdx.x * (kSelectThreads / kWave) >= tiles) return;  // the whole workgroup
-  for (int x = threadIdx.x; x < kScoreTile * (D / 8); x += kSelectThreads) {
-    const int col = x % kScoreTile, piece = x / kScoreTile;
-    const int64_t at = (int64_t)(a.b0 + b) * a.q_b + (int64_t)h * a.G * a.q_h + (int64_t)min(i0 + col, i1 - 1) * a.q_m + piece * 8;
-    double plus[8], minus[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) plus[e] = minus[e] = 0;
-    for (int g = 0; g < a.G; ++g) {
-      float f[8];
-      load_row8<FB>(a.q, at + g * a.q_h, f);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {  // (a NaN reaches both)
-        plus[e] += (double)(f[e] < 0.f ? 0.f : f[e]);
-        minus[e] += (double)(f[e] > 0.f ? 0.f : f[e]);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {  // the bounds' first D channels are the lowest elements
-      lds[((piece / 4 * 8 + e) * 4 + piece % 4) * kScoreTile + col] = minus[e];
-      lds[(((piece + D / 8) / 4 * 8 + e) * 4 + (piece + D / 8) % 4) * kScoreTile + col] = plus[e];
-    }
-  }
-  __syncthreads();
-  const int row = lane % kScoreTile, k = lane / kScoreTile;
-  bool bad = false;
-  for (int tile = blockIdx.x * (kSelectThreads / kWave) + wave; tile < tiles; tile += gridDim.x * (kSelectThreads / kWave)) {
-    const uint32_t j = (uint32_t)min(tile * kScoreTile + row, most - 1), p = j * a.map.R.d;
-    int32_t page = a.table ? a.table[(int64_t)(a.b0 + b) * a.cols + fast_div(p, a.T)] : a.b0 + b;
-    if ((uint32_t)page >= (uint32_t)a.pages) page = 0, bad = true;
-    const char* at = a.bounds + a.map.block(page, (uint32_t)(a.layer * a.H + h), p, a.T) * (2 * D * (FB == kFmtF32 ? 4 : 2));
-    F64x4 s[2] = {};
-    float f[CHUNKS][8];
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) load_row8<FB>(at, (c * 4 + k) * 8, f[c]);
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        s[e % 2] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)f[c][e], lds[(c * 8 + e) * kWave + lane], s[e % 2], 0, 0, 0);
-    // a lane has the scores of its query (lane % 16) and of the tile's blocks 4 e + lane / 16
-    const int i = i0 + row;
-    if (i >= i1) continue;
-    double* to = a.scores + (((int64_t)b * a.H + h) * a.mq + (i - a.m0)) * a.padded + tile * kScoreTile + k;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) to[4 * e] = s[0][e] + s[1][e];
-  }
-  if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, kDevBadPage);
-}
-
-// ------------------------------------------------------------ the highest scores
 // A score as 64 bits whose order as a whole number is the scores' (-0 as +0): 0 for what cannot be picked,
 // all ones for what always is, and NaN just below that.
 __device__ __forceinline__ uint64_t score_key(double s, bool candidate, bool always) {
@@ -117,35 +56,48 @@ __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// A wave a query: the k-th highest key bit by bit, its upper half first, until as many keys as wanted are
-// at least the bits so far; then the keys above it and, of those equal to it, the lowest blocks'. NR: a lane's
-// keys, in registers (0: any number, read again for every bit).
+// A wave's list for query i: a histogram of 256 equal parts of the keys' range (of their upper words) says which part holds
+// the k-th highest; among the few keys there it is found bit by bit, until as many keys as wanted are at least the
+// bits so far. Then the keys above it and, of those equal to it, the lowest blocks'. NR: a lane's keys, in
+// registers (0: any number, read again each time); cross: other workgroups wrote scores; hist: 256 words of LDS. The next
+// query's scores are on their way meanwhile.
 template <int NR>
-__global__ __launch_bounds__(kSelectThreads) void k_block_pick(SelectArgs a) {
-  const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x % kWave;
-  const int i = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * (kSelectThreads / kWave) + threadIdx.x / kWave)) + a.m0;
-  if (i >= min(a.m0 + a.mq, a.rows[b])) return;
+struct Scores {
+  double s[NR > 0 ? NR : 1];
+  // block r * 64 + lane's score (past the last one's: the last)
+  static __device__ __forceinline__ double at(const SelectArgs& a, int b, int h, int i, int32_t count, int r, bool cross) {
+    double* p = a.scores + (((int64_t)b * a.H + h) * a.mq + (i - a.m0)) * a.padded + min(r * kWave + (int)threadIdx.x % kWave, count - 1);
+    return cross ? __builtin_bit_cast(double, __hip_atomic_load(reinterpret_cast<uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
+                 : *p;
+  }
+  __device__ __forceinline__ void load(const SelectArgs& a, int b, int h, int i, bool cross) {
+    const int32_t count = candidates(a, b, i);
+#pragma unroll
+    for (int r = 0; r < NR; ++r) s[r] = r * kWave < count ? at(a, b, h, i, count, r, cross) : 0;
+  }
+};
+template <int NR>
+__device__ __forceinline__ void pick_blocks(const SelectArgs& a, const Scores<NR>& scores, int b, int h, int i, bool cross, uint32_t* hist) {
+  const int lane = threadIdx.x % kWave;
   const int32_t count = candidates(a, b, i), want = min(a.top, count);
-  const double* scores = a.scores + (((int64_t)b * a.H + h) * a.mq + (i - a.m0)) * a.padded;
   int32_t* to = a.blocks + (((int64_t)(a.b0 + b) * a.H + h) * a.max_rows + i) * a.top;
   const int turns = (count + kWave - 1) / kWave;
-  const auto load_key = [&](int r) __attribute__((always_inline)) {
+  const auto key_of = [&](int r, double s) __attribute__((always_inline)) {
     const int j = r * kWave + lane;
-    const double s = scores[min(j, count - 1)];
     return score_key(s, j < count, (j < a.first_blocks) | (j >= count - a.last_blocks));
   };
   constexpr int N = NR > 0 ? NR : 1;
   uint64_t key[N];
   if constexpr (NR > 0) {
 #pragma unroll
-    for (int r = 0; r < NR; ++r) key[r] = r < turns ? load_key(r) : 0;
+    for (int r = 0; r < NR; ++r) key[r] = key_of(r, scores.s[r]);
   }
   const auto each = [&](auto&& what) __attribute__((always_inline)) {
     if constexpr (NR > 0) {
 #pragma unroll
       for (int r = 0; r < NR; ++r) what(r, key[r]);
     } else {
-      for (int r = 0; r < turns; ++r) what(r, load_key(r));
+      for (int r = 0; r < turns; ++r) what(r, key_of(r, Scores<NR>::at(a, b, h, i, count, r, cross)));
     }
   };
   const auto at_least = [&](uint64_t x) __attribute__((always_inline)) {
@@ -153,21 +105,71 @@ __global__ __launch_bounds__(kSelectThreads) void k_block_pick(SelectArgs a) {
     each([&](int, uint64_t y) __attribute__((always_inline)) { c += __builtin_popcountll(__ballot(y >= x)); });
     return c;
   };
+  const auto upper_at_least = [&](uint32_t x) __attribute__((always_inline)) {
+    int c = 0;
+    each([&](int, uint64_t y) __attribute__((always_inline)) { c += __builtin_popcountll(__ballot((uint32_t)(y >> 32) >= x)); });
+    return c;
+  };
   uint64_t limit = 1;  // the least key that is picked
   int equal = 0;       // of those equal to it, as many (all, if `all`)
   bool all = true;
-  if (want < count) {
-    limit = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const uint64_t x = limit | 1ull << bit;
-      const int c = at_least(x);
-      if (c < want) continue;
-      limit = x;
-      if (c == want) break;
+  const int forced = a.first_blocks + a.last_blocks;  // (of which there are as many where there are more blocks than wanted)
+  if (want < count && want == forced) {
+    limit = ~0ull;
+  } else if (want < count) {
+    // the range of the others' upper words, from `from` on
+    uint32_t least, most;
+    const auto range = [&](uint32_t from, uint32_t size) __attribute__((always_inline)) {
+      least = ~0u, most = 0;
+      each([&](int, uint64_t y) __attribute__((always_inline)) {
+        const uint32_t u = (uint32_t)(y >> 32);
+        const bool in = (y != 0) & (y != ~0ull) & (u - from <= size);
+        least = in ? min(least, u) : least, most = in ? max(most, u) : most;
+      });
+      wave_min_max(least, most);
+    };
+    range(0, ~0u);
+    all = false;
+    limit = (uint64_t)least << 32;
+    if (least < most) {
+      const int shift = max(24 - __builtin_clz(most - least), 0);
+      U32x4* bins = reinterpret_cast<U32x4*>(hist);
+      bins[lane] = U32x4{0, 0, 0, 0};
+      asm volatile("" ::: "memory");
+      each([&](int, uint64_t y) __attribute__((always_inline)) {
+        if ((y != 0) & (y != ~0ull)) atomicAdd(&hist[((uint32_t)(y >> 32) - least) >> shift], 1u);
+      });
+      asm volatile("" ::: "memory");
+      // lane 0 has the four highest parts: keys of them and of all before
+      const U32x4 c = bins[kWave - 1 - lane];
+      const int32_t sum = (int32_t)(c[0] + c[1] + c[2] + c[3]), upto = wave_inclusive_scan(sum), rest = want - forced;
+      const int32_t a3 = upto - sum + (int32_t)c[3], a2 = a3 + (int32_t)c[2], a1 = a2 + (int32_t)c[1];
+      const int part = a3 >= rest ? 3 : a2 >= rest ? 2 : a1 >= rest ? 1 : 0;
+      const int32_t reached = a3 >= rest ? a3 : a2 >= rest ? a2 : a1 >= rest ? a1 : upto;
+      const int at = __builtin_ctzll(__ballot(upto >= rest));
+      const uint32_t from = least + ((uint32_t)((kWave - 1 - at) * 4 + __builtin_amdgcn_readlane(part, at)) << shift);
+      all = __builtin_amdgcn_readlane(reached, at) == rest;
+      limit = (uint64_t)from << 32;
+      if (!all && shift > 0) {
+        range(from, (1u << shift) - 1u);
+        const int top_bit = least < most ? 31 - __builtin_clz(least ^ most) : -1;
+        uint32_t upper = top_bit < 0 ? least : least >> top_bit >> 1 << top_bit << 1;
+        for (int bit = top_bit; bit >= 0 && !all; --bit) {
+          const uint32_t x = upper | 1u << bit;
+          const int n = upper_at_least(x);
+          if (n >= want) upper = x;
+          all = n == want;
+        }
+        limit = (uint64_t)upper << 32;
+      }
     }
-    const int above = limit == ~0ull ? 0 : at_least(limit + 1);
-    all = at_least(limit) == want;
-    equal = want - above;
+    for (int bit = 31; bit >= 0 && !all; --bit) {
+      const uint64_t x = limit | 1ull << bit;
+      const int n = at_least(x);
+      if (n >= want) limit = x;
+      all = n == want;
+    }
+    if (!all) equal = want - at_least(limit + 1);
   }
   int pos = 0;
   each([&](int r, uint64_t y) __attribute__((always_inline)) {
@@ -182,6 +184,185 @@ __global__ __launch_bounds__(kSelectThreads) void k_block_pick(SelectArgs a) {
     pos += __builtin_popcountll(mask);
   });
   for (int x = pos + lane; x < a.top; x += kWave) to[x] = -1;
+}
+
+// Where channel ch (of 2 D) of query col is: step 8 (ch / 32) + ch % 8, place ch / 8 % 4, and the queries of a place in an
+// order by which the channels that a wave writes together lie in different banks.
+__device__ __forceinline__ int select_place(int ch, int col) {
+  const int c = ch / 32, k = ch / 8 % 4;
+  return (c * 8 + ch % 8) * kWave + k * kScoreTile + (col ^ (k * 4 + c % 4));
+}
+
+// The lists of up to 16 queries of a head. blockIdx.x: tiles of 16 blocks, in turn; .y: head and tile of queries; .z:
+// stream. Q+ and Q- of the queries are made in LDS in the order in which the product takes them: step 8 c + e has channel
+// 8 (4 c + k) + e in its place k, so that a lane's 16 bytes of bounds are operands of eight steps. A wave takes a tile
+// of blocks or, where there are few queries (SPLIT), a quarter of its steps, added up through LDS: then the way through
+// all of them is what a tile costs. The scores go to memory; the workgroup, the last one to come where several share the
+// blocks, picks from them. Bound by the 64-bit products where there are many queries (1024 tokens of 8 KV heads over 512
+// blocks 72 us, 27 of them the products at their rate), by the trips to memory for one (9 us).
+template <int FB, int D, int NR, bool SPLIT>
+__global__ __launch_bounds__(kSelectThreads) void k_block_select(SelectArgs a) {
+  constexpr int STEPS = D / 2, PART = SPLIT ? STEPS / kSelectWaves : STEPS;  // of four terms; of a wave
+  constexpr int CHUNKS = PART < 8 ? 1 : PART / 8;                            // of eight steps, that a wave loads
+  constexpr int WAVES = SPLIT ? 1 : kSelectWaves;                            // tiles at a time
+  __shared__ double lds[STEPS * kWave];
+  __shared__ double sums[SPLIT ? 2 : 1][SPLIT ? kSelectWaves : 1][kScoreTile * kScoreTile];
+  __shared__ bool lds_last;
+  const int b = blockIdx.z, q_tiles = (a.mq + kScoreTile - 1) / kScoreTile;
+  const int h = blockIdx.y / q_tiles, i0 = a.m0 + blockIdx.y % q_tiles * kScoreTile;
+  const int i1 = min(min(i0 + kScoreTile, a.m0 + a.mq), a.rows[b]);
+  if (i0 >= i1) return;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int row = lane % kScoreTile, k = lane / kScoreTile;
+  const int32_t most = candidates(a, b, i1 - 1), tiles = (most + kScoreTile - 1) / kScoreTile;
+  const int sharing = max(min((int)gridDim.x, tiles), 1);
+  if ((int)blockIdx.x >= sharing) return;  // the whole workgroup
+  const int c0 = SPLIT ? wave * PART / 8 : 0, e0 = SPLIT ? wave * PART % 8 : 0;  // the wave's first chunk and step there
+  bool bad = false;
+  // the page of the lane's block of a tile (a tile past the last: the last block); its bounds, in the wave's channels
+  const auto page_of = [&](int tile) __attribute__((always_inline)) {
+    const uint32_t p = (uint32_t)min(tile * kScoreTile + row, most - 1) * a.map.R.d;
+    return a.table ? a.table[(int64_t)(a.b0 + b) * a.cols + fast_div(p, a.T)] : a.b0 + b;
+  };
+  struct Piece {
+    Raw16 r[CHUNKS * (FB == kFmtF32 ? 2 : 1)];
+  };
+  const auto load_tile = [&](int tile, int32_t page) __attribute__((always_inline)) {
+    const uint32_t p = (uint32_t)min(tile * kScoreTile + row, most - 1) * a.map.R.d;
+    if ((uint32_t)page >= (uint32_t)a.pages) page = 0, bad = true;
+    constexpr int E = FB == kFmtF32 ? 4 : 2;
+    const char* at = a.bounds + a.map.block(page, (uint32_t)(a.layer * a.H + h), p, a.T) * (2 * D * E) + (c0 * 4 + k) * 8 * E;
+    Piece x;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) x.r[c * (E / 2) + i] = load16(at + c * 32 * E + 16 * i);
+    return x;
+  };
+  const int first = (int)blockIdx.x * WAVES + (SPLIT ? 0 : wave), step = (int)gridDim.x * WAVES;
+  Piece next = {};
+  int32_t page = 0;  // of the tile after the next
+  if (first < tiles) {
+    next = load_tile(first, page_of(first));
+    page = page_of(first + step);
+  }
+  // four channels of a query a thread (of the queries that there are: what is in the other columns reaches no score of these)
+  for (int x = threadIdx.x; x < (i1 - i0) * (D / 4); x += kSelectThreads) {
+    const int col = x / (D / 4), channel = x % (D / 4) * 4;
+    const int64_t at = (int64_t)(a.b0 + b) * a.q_b + (int64_t)h * a.G * a.q_h + (int64_t)(i0 + col) * a.q_m + channel;
+    double plus[4], minus[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) plus[e] = minus[e] = 0;
+    constexpr int HEADS = 8;  // on their way at once
+    for (int g0 = 0; g0 < a.G; g0 += HEADS) {
+      float f[HEADS][4];
+#pragma unroll
+      for (int g = 0; g < HEADS; ++g) {
+        const int64_t from = at + min(g0 + g, a.G - 1) * a.q_h;
+        if constexpr (FB == kFmtF32) {
+          Lane<float>::decode(load16(a.q + from * 4), f[g]);
+        } else {
+          const U32x2 w = *reinterpret_cast<const U32x2*>(a.q + from * 2);
+          f[g][0] = __uint_as_float(w.x << 16), f[g][1] = __uint_as_float(w.x & 0xffff0000u);
+          f[g][2] = __uint_as_float(w.y << 16), f[g][3] = __uint_as_float(w.y & 0xffff0000u);
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < HEADS; ++g) {
+        if (g0 + g >= a.G) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {  // (a NaN reaches both)
+          plus[e] += (double)(f[g][e] < 0.f ? 0.f : f[g][e]);
+          minus[e] += (double)(f[g][e] > 0.f ? 0.f : f[g][e]);
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {  // the bounds' first D channels are the lowest elements
+      lds[select_place(channel + e, col)] = minus[e];
+      lds[select_place(D + channel + e, col)] = plus[e];
+    }
+  }
+  __syncthreads();
+  // the wave's operands of the queries' side in registers, where those suffice
+  constexpr bool HELD = PART <= 64;
+  double q[HELD ? PART : 1];
+  const auto operand = [&](int i) __attribute__((always_inline)) {
+    const int step = (SPLIT ? wave * PART : 0) + i;
+    return lds[select_place(step / 8 * 32 + k * 8 + step % 8, row)];
+  };
+  if constexpr (HELD)
+#pragma unroll
+    for (int i = 0; i < PART; ++i) q[i] = operand(i);
+  int buf = 0;
+  for (int tile = first; tile < tiles; tile += step, buf ^= 1) {
+    const Piece x = next;
+    if (tile + step < tiles) {
+      next = load_tile(tile + step, page);
+      page = page_of(tile + 2 * step);
+    }
+    float f[CHUNKS][8];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+      if constexpr (FB == kFmtF32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[c][i] = __uint_as_float(x.r[2 * c].w[i]), f[c][4 + i] = __uint_as_float(x.r[2 * c + 1].w[i]);
+      } else {
+        Lane<uint16_t>::decode(x.r[c], f[c]);
+      }
+    }
+    F64x4 s = {}, s1 = {};
+#pragma unroll
+    for (int i = 0; i < PART; ++i) {
+      float v = f[i / 8][i % 8];
+      if constexpr (PART < 8) v = e0 ? f[0][4 + i] : f[0][i];
+      F64x4& sum = i % 2 ? s1 : s;  // (two, since each waits for its last product)
+      sum = __builtin_amdgcn_mfma_f64_16x16x4f64((double)v, HELD ? q[HELD ? i : 0] : operand(i), sum, 0, 0, 0);
+    }
+    s += s1;
+    // a lane has the scores, or their parts, of its query (lane % 16) and of the tile's blocks 4 e + lane / 16
+    const auto keep = [&](int col, int i, double v) __attribute__((always_inline)) {
+      if (i0 + col >= i1) return;
+      double* to = a.scores + (((int64_t)b * a.H + h) * a.mq + (i0 + col - a.m0)) * a.padded + tile * kScoreTile + i;
+      if (sharing > 1)
+        __hip_atomic_store(reinterpret_cast<uint64_t*>(to), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      else *to = v;
+    };
+    if constexpr (SPLIT) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sums[buf][wave][e * kWave + lane] = s[e];
+      __syncthreads();
+      double total = 0;
+#pragma unroll
+      for (int w = 0; w < kSelectWaves; ++w) total += sums[buf][w][threadIdx.x];
+      keep(threadIdx.x % kScoreTile, threadIdx.x / kScoreTile, total);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) keep(row, 4 * e + k, s[e]);
+    }
+  }
+  if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, kDevBadPage);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's scores are written
+  __syncthreads();
+  if (sharing > 1) {
+    if (threadIdx.x == 0) {
+      uint32_t* count = a.arrived + (blockIdx.z * gridDim.y + blockIdx.y) * a.spread;
+      const uint32_t before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      lds_last = before + 1 == (uint32_t)sharing;
+      if (lds_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!lds_last) return;
+  }
+  static_assert(sizeof(lds) >= kSelectWaves * 256 * sizeof(uint32_t), "a histogram a wave");
+  uint32_t* hist = reinterpret_cast<uint32_t*>(lds) + wave * 256;
+  Scores<NR> later;
+  if (i0 + wave < i1) later.load(a, b, h, i0 + wave, sharing > 1);
+  for (int i = i0 + wave; i < i1; i += kSelectWaves) {
+    const Scores<NR> scores = later;
+    if (i + kSelectWaves < i1) later.load(a, b, h, i + kSelectWaves, sharing > 1);
+    pick_blocks<NR>(a, scores, b, h, i, sharing > 1, hist);
+  }
 }
 
 // ------------------------------------------------------------ attention over lists
@@ -215,14 +396,17 @@ struct BlocksArgs {
   BlockStream s[kAttendStreams];
 };
 
-// A workgroup's query and part: tokens of a head follow each other on an XCD, since their lists are often alike.
+// The query and part of a workgroup, or (SOLO) of a wave: tokens of a head follow each other on an XCD, since
+// their lists are often alike.
 struct BlockPlace : Place {
   int32_t token;
 };
-__device__ __forceinline__ BlockPlace block_place(const BlocksArgs& a) {
-  const uint32_t per = (uint32_t)(a.slots + 7) / 8u;
+template <bool SOLO>
+__device__ __forceinline__ BlockPlace block_place(const BlocksArgs& a, int wave) {
+  constexpr uint32_t EACH = SOLO ? kFewWaves : 1;  // places of a workgroup
+  const uint32_t per = ((uint32_t)a.slots + 8u * EACH - 1u) / (8u * EACH);
   BlockPlace p;
-  p.slot = (int32_t)((blockIdx.x % 8u) * per + blockIdx.x / 8u);
+  p.slot = (int32_t)(((blockIdx.x % 8u) * per + blockIdx.x / 8u) * EACH + (SOLO ? wave : 0));
   p.b = 0;
   if (p.slot >= a.slots) {
     p.slot = -1;
@@ -278,26 +462,31 @@ struct Runs {
   __device__ __forceinline__ int32_t seen_at(int lane_) const { return __builtin_amdgcn_readlane(seen, lane_); }
 };
 
+// Workgroups of a CU, by the registers that they take.
+constexpr int blocks_per_cu(int F, int D, int NB) {
+  return NB * D <= 64 || (fmt_scaled(F) && NB * D <= 128) ? 3 : NB * D <= 128 || (fmt_scaled(F) && D <= 128) ? 2 : 1;
+}
+
 // As k_attend_few, but that the keys are those of a list, and all rows of the workgroup are one token's: a
 // row of the cache is seen by all of them or by none.
-template <int F, int D, int NB>
-__global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend_blocks(BlocksArgs a) {
+template <int F, int D, int NB, bool SOLO>
+__global__ __launch_bounds__(64 * kFewWaves, blocks_per_cu(F, D, NB)) void k_attend_blocks(BlocksArgs a) {
   using C = FewCfg<F, D>;
-  __shared__ __attribute__((aligned(16))) char lds[kFewWaves][few_wave_lds<F, D, NB>()];
-  __shared__ float lds_ml[kFewWaves][16 * NB][2];
-  __shared__ uint32_t lds_last;
-  const BlockPlace pl = block_place(a);
-  if (pl.slot < 0) return;  // the whole workgroup
+  constexpr size_t KTILE = kFewKeys * C::RB, VTILE = kFewKeys * D * 2, JOIN = JoinLds<D, 16 * NB>::kWaveBytes;
+  __shared__ __attribute__((aligned(16))) char lds[kFewWaves][SOLO || JOIN < KTILE + VTILE ? KTILE + VTILE : JOIN];
   const int lane = threadIdx.x % kWave, g = lane / 16, l16 = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const BlockPlace pl = block_place<SOLO>(a, wave);
+  if (pl.slot < 0) return;  // the whole workgroup, or a wave that no other waits for
   const int b = a.b0 + pl.b;
   const int64_t head_row = a.layer_row + (int64_t)pl.h * a.pool.T.d;
   const int32_t held = min(a.s[pl.b].n, a.s[pl.b].first + pl.token + 1);
   const int32_t* list = a.blocks + (((int64_t)b * a.H + pl.h) * a.max_rows + pl.token) * a.top;
   const int32_t count = (int32_t)(((int64_t)a.entries * a.halves.d + 1) / 2);  // key tiles of the list
   const int32_t t_end = (int32_t)((int64_t)count * (pl.split + 1) / a.splits);
-  const int32_t t_begin = (int32_t)((int64_t)count * pl.split / a.splits) + wave;
-  const int heads = min(a.G - pl.tile * 16 * NB, 16 * NB);  // of the workgroup
+  const int32_t t_begin = (int32_t)((int64_t)count * pl.split / a.splits) + (SOLO ? 0 : wave);
+  constexpr int STEP = SOLO ? 1 : kFewWaves;
+  const int heads = min(a.G - pl.tile * 16 * NB, 16 * NB);
 
   F32x4 o[NB][D / 16];
   float m[NB], l[NB];
@@ -319,155 +508,174 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
         q[nb][c * (C::KE / 8) + s] = __builtin_bit_cast(Bf16x8, load16(at + 2 * ((c * 4 + g) * C::KE + 8 * s)));
   }
 
-  constexpr bool COPY = F == kFmtBf16;
-  constexpr int VTILE = kFewKeys * D * 2;
-  uint32_t kr[2][C::KQ / 4], vr[COPY ? 1 : C::NV][4];
-  uint64_t ks[2], vs[COPY ? 1 : C::NV];
-  char* tile = lds[wave];
-  int vbuf = 0;
+  // A tile's rows as they are stored, on their way from when they are fetched until they are used: keys as well as values
+  // in the order of memory and through LDS. Keys straight into the product's operand, where neighbouring lanes have
+  // different rows, cost the cache a line for each lane: 1024 tokens of 64 heads with 16 blocks of 64 of
+  // 32768 positions of 128 take 304 us so and 222 through LDS.
+  // (Keys lie there as they are stored, values as bf16.)
+  struct Rows {
+    uint32_t k[C::NV][4], v[C::NV][4];
+    uint64_t ks[2], vs[C::NV];  // scales of the operand's keys, and of the values' pieces
+    int32_t seen0, seen1;
+  };
+  char* k_tile = lds[wave];
+  char* v_tile = lds[wave] + KTILE;
+  // places of 16-byte chunks of a key's row: those that 16 rows' lanes read together lie in different banks
+  const auto k_swz = [](int row) __attribute__((always_inline)) {
+    return C::CPR >= 8 ? row & 7 : C::CPR == 4 ? (row >> 1) & 3 : C::CPR == 2 ? (row >> 2) & 1 : 0;
+  };
   bool bad = false;
-  // the rows of both runs set out
-  const auto fetch = [&](int64_t r0, int64_t r1, char* v_tile) __attribute__((always_inline)) {
+  const auto fetch = [&](Rows& x, const Runs& runs, int at) __attribute__((always_inline)) {
+    const int64_t r0 = runs.row_at(at), r1 = runs.row_at(at + 1);
+    x.seen0 = runs.seen_at(at), x.seen1 = runs.seen_at(at + 1);
+    constexpr int PER = kWave / C::CPR;  // rows a load
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      const int64_t row = kb ? r1 : r0;
-      const char* p = a.pool.K + row * C::RB;
+    for (int i = 0; i < C::NV; ++i) {
+      if constexpr (PER <= 16) {
+        const int64_t row = i * PER < 16 ? r0 + i * PER : r1 + (i * PER - 16);
+        load_piece<16>(a.pool.K + row * C::RB + (uint32_t)(lane * 16), x.k[i]);
+        load_piece<16>(a.pool.V + row * C::RB + (uint32_t)(lane * 16), x.v[i]);
+        if (fmt_scaled(F)) x.vs[i] = load_scales<D>(a.pool.Vs + row * (D / kScaleBlock), lane / C::CPR);
+      } else {
+        const int key = lane / C::CPR % kFewKeys;  // (a piece too many is the first ones' again)
+        const int64_t row = (key < 16 ? r0 : r1) + key % 16;
+        load_piece<16>(a.pool.K + row * C::RB + lane % C::CPR * 16, x.k[i]);
+        load_piece<16>(a.pool.V + row * C::RB + lane % C::CPR * 16, x.v[i]);
+        if (fmt_scaled(F)) x.vs[i] = load_scales<D>(a.pool.Vs, row);
+      }
+    }
+    if (fmt_scaled(F)) x.ks[0] = load_scales<D>(a.pool.Ks, r0 + l16), x.ks[1] = load_scales<D>(a.pool.Ks, r1 + l16);
+  };
+  // a tile's scores, weights and sums; `next` sets out the rows of the next one when these are in LDS
+  const auto use = [&](Rows& x, auto&& next) __attribute__((always_inline)) {
+    const int32_t seen0 = x.seen0, seen1 = x.seen1;
+    const bool full = (seen0 == 16) & (seen1 == 16);
+    if (!full) {  // values of rows that are not seen as zeros
 #pragma unroll
-      for (int c = 0; c < C::KN; ++c)
-        load_piece<C::KB>(p + c * 4 * C::KB + (uint32_t)(l16 * C::RB + g * C::KB), kr[kb] + c * (C::KB / 4));
-      if (fmt_scaled(F)) ks[kb] = load_scales<D>(a.pool.Ks + row * (D / kScaleBlock), l16);
+      for (int i = 0; i < C::NV; ++i) {
+        const int key = (i * kWave + lane) / C::CPR % kFewKeys;
+        if (key % 16 < (key < 16 ? seen0 : seen1)) continue;
+        x.v[i][0] = x.v[i][1] = x.v[i][2] = x.v[i][3] = 0;
+        x.vs[i] = 0;
+      }
     }
 #pragma unroll
     for (int i = 0; i < C::NV; ++i) {
-      const int key = (i * kWave + lane) / C::CPR % kFewKeys;  // (a piece too many is the first ones' again)
-      constexpr int PER = kWave / C::CPR;                      // rows a load
-      if constexpr (COPY) {
-        const char* p = a.pool.V + (i * PER < 16 ? r0 + i * PER : r1 + (i * PER - 16)) * C::RB;
-        const int ch = lane % C::CPR ^ C::swz(key);  // the source column makes up for the place
-        copy_to_lds(p, (uint32_t)(lane / C::CPR * C::RB + ch * 16), __builtin_amdgcn_readfirstlane(lds_address(v_tile) + i * 1024));
-      } else if constexpr (PER <= 16) {
-        const int64_t row = i * PER < 16 ? r0 + i * PER : r1 + (i * PER - 16);
-        load_piece<16>(a.pool.V + row * C::RB + (uint32_t)(lane / C::CPR * C::RB + lane % C::CPR * 16), vr[i]);
-        if (fmt_scaled(F)) vs[i] = load_scales<D>(a.pool.Vs + row * (D / kScaleBlock), lane / C::CPR);
-      } else {
-        const int64_t row = (key < 16 ? r0 : r1) + key % 16;
-        load_piece<16>(a.pool.V + row * C::RB + lane % C::CPR * 16, vr[i]);
-        if (fmt_scaled(F)) vs[i] = load_scales<D>(a.pool.Vs, row);
+      const int y = i * kWave + lane, key = y / C::CPR, col = y % C::CPR;
+      if (C::CPR == 1 && y >= kFewKeys) continue;
+      *reinterpret_cast<Raw16*>(k_tile + key * C::RB + 16 * (col ^ k_swz(key))) = Raw16{x.k[i][0], x.k[i][1], x.k[i][2], x.k[i][3]};
+      const float scale = fmt_scaled(F) ? scale_at(x.vs[i], col * C::VE / kScaleBlock) : 0.f;
+#pragma unroll
+      for (int e = 0; e < C::VE / 8; ++e)
+        *reinterpret_cast<Raw16*>(v_tile + key * (D * 2) + 16 * ((col * (C::VE / 8) + e) ^ C::swz(key))) = piece8<F>(x.v[i], e, scale);
+    }
+    __builtin_amdgcn_wave_barrier();
+    const uint64_t ks[2] = {x.ks[0], x.ks[1]};
+    const bool more = next(x);
+    F32x4 sc[NB][2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) sc[nb][kb] = F32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < C::KN; ++c) {
+        const int byte = (c * 4 + g) * C::KB;
+        uint32_t kr[4];
+        load_piece<C::KB>(k_tile + (kb * 16 + l16) * C::RB + 16 * ((byte / 16) ^ k_swz(l16)) + byte % 16, kr);
+#pragma unroll
+        for (int s = 0; s < C::KE / 8; ++s) {
+          const float scale = fmt_scaled(F) ? scale_at(ks[kb], ((c * 4 + g) * C::KE + 8 * s) / kScaleBlock) : 0.f;
+          const Bf16x8 k = __builtin_bit_cast(Bf16x8, piece8<F>(kr, s, scale));
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            sc[nb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[nb][c * (C::KE / 8) + s], sc[nb][kb], 0, 0, 0);
+        }
       }
     }
-  };
-  for (int32_t t0 = t_begin; t0 < t_end; t0 += 32 * kFewWaves) {
-    Runs runs;
-    runs.look_up(a, list, b, head_row, held, t0, kFewWaves, t_end, bad);
-    uint64_t todo = runs.some;
-    if (todo == 0) continue;
-    int at = __builtin_ctzll(todo);
-    fetch(runs.row_at(at), runs.row_at(at + 1), tile + vbuf * VTILE);
-    while (todo != 0) {
-      todo &= todo - 1;
-      if constexpr (COPY) copies_done();
-      const int32_t seen0 = runs.seen_at(at), seen1 = runs.seen_at(at + 1);
-      const bool full = (seen0 == 16) & (seen1 == 16);
-      F32x4 sc[NB][2];
+    Bf16x8 w[NB];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) sc[nb][kb] = F32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < C::KN; ++c)
-#pragma unroll
-          for (int s = 0; s < C::KE / 8; ++s) {
-            const float scale = fmt_scaled(F) ? scale_at(ks[kb], ((c * 4 + g) * C::KE + 8 * s) / kScaleBlock) : 0.f;
-            const Bf16x8 k = __builtin_bit_cast(Bf16x8, piece8<F>(kr[kb] + c * (C::KB / 4), s, scale));
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-              sc[nb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[nb][c * (C::KE / 8) + s], sc[nb][kb], 0, 0, 0);
-          }
-      }
-      // V into LDS as bf16, rows that are not seen as zeros
+    for (int nb = 0; nb < NB; ++nb) {
       if (!full) {
 #pragma unroll
-        for (int i = 0; i < C::NV; ++i) {
-          const int x = i * kWave + lane, key = x / C::CPR % kFewKeys;
-          if (key % 16 < (key < 16 ? seen0 : seen1)) continue;
-          if constexpr (COPY) {
-            *reinterpret_cast<Raw16*>(tile + vbuf * VTILE + x * 16) = Raw16{0, 0, 0, 0};  // as this lane copied it
-          } else {
-            vr[i][0] = vr[i][1] = vr[i][2] = vr[i][3] = 0;
-            vs[i] = 0;
-          }
+        for (int i = 0; i < 4; ++i) {
+          if (4 * g + i >= seen0) sc[nb][0][i] = -INFINITY;
+          if (4 * g + i >= seen1) sc[nb][1][i] = -INFINITY;
         }
       }
-      if constexpr (!COPY)
+      float top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < C::NV; ++i) {
-          const int x = i * kWave + lane, key = x / C::CPR, col = x % C::CPR;
-          if (C::CPR == 1 && x >= kFewKeys) continue;
-          const float scale = scale_at(vs[i], col * C::VE / kScaleBlock);
+      for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, sc[nb][0][i]), sc[nb][1][i]);
+      top = lanes_max<4>(top) * a.c;
+      if (__ballot(top > m[nb]) != 0) {
+        rare();
+        top = fmaxf(top, m[nb]);
+        const float old = exp2_hw(m[nb] - shift_of(top));
+        m[nb] = top;
+        l[nb] *= old;
 #pragma unroll
-          for (int e = 0; e < C::VE / 8; ++e)
-            *reinterpret_cast<Raw16*>(tile + key * (D * 2) + 16 * ((col * (C::VE / 8) + e) ^ C::swz(key))) = piece8<F>(vr[i], e, scale);
+        for (int i = 0; i < D / 16; ++i) {
+          if constexpr (NB * D > 256) in_acc(o[nb][i]);
+          o[nb][i] *= old;
+          if constexpr (NB * D > 256) in_acc(o[nb][i]);
         }
-      if (todo != 0) {
-        at = __builtin_ctzll(todo);
-        fetch(runs.row_at(at), runs.row_at(at + 1), tile + (COPY ? (vbuf ^ 1) * VTILE : 0));
       }
-      Bf16x8 w[NB];
+      const float shift = shift_of(m[nb]);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        if (!full) {
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (4 * g + i >= seen0) sc[nb][0][i] = -INFINITY;
-            if (4 * g + i >= seen1) sc[nb][1][i] = -INFINITY;
-          }
+        for (int i = 0; i < 4; ++i) {
+          const float e = exp2_hw(__builtin_fmaf(sc[nb][kb][i], a.c, -shift));
+          l[nb] += e;
+          w[nb][kb * 4 + i] = (__bf16)e;
         }
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, sc[nb][0][i]), sc[nb][1][i]);
-        top = lanes_max<4>(top) * a.c;
-        if (__ballot(top > m[nb]) != 0) {
-          rare();
-          top = fmaxf(top, m[nb]);
-          const float old = exp2_hw(m[nb] - shift_of(top));
-          m[nb] = top;
-          l[nb] *= old;
-#pragma unroll
-          for (int i = 0; i < D / 16; ++i) {
-            if constexpr (NB * D > 256) in_acc(o[nb][i]);
-            o[nb][i] *= old;
-            if constexpr (NB * D > 256) in_acc(o[nb][i]);
-          }
-        }
-        const float shift = shift_of(m[nb]);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float e = exp2_hw(__builtin_fmaf(sc[nb][kb][i], a.c, -shift));
-            l[nb] += e;
-            w[nb][kb * 4 + i] = (__bf16)e;
-          }
-      }
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int db = 0; db < D / 16; ++db) {
-        const int k0 = 4 * g + l16 / 4, ch = 2 * db + (l16 % 4) / 2, in = 8 * (l16 & 1);
-        const char* from = tile + (COPY ? vbuf * VTILE : 0);
-        const U32x2 x = lds_column4(from + k0 * (D * 2) + 16 * (ch ^ C::swz(k0)) + in);
-        const U32x2 y = lds_column4(from + (k0 + 16) * (D * 2) + 16 * (ch ^ C::swz(k0 + 16)) + in);
-        const Raw16 r = {x.x, x.y, y.x, y.y};
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf16x8, r), w[nb], o[nb][db], 0, 0, 0);
-      }
-      __builtin_amdgcn_wave_barrier();
-      if (COPY) vbuf ^= 1;
     }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) {
+      const int k0 = 4 * g + l16 / 4, ch = 2 * db + (l16 % 4) / 2, in = 8 * (l16 & 1);
+      const U32x2 v0 = lds_column4(v_tile + k0 * (D * 2) + 16 * (ch ^ C::swz(k0)) + in);
+      const U32x2 v1 = lds_column4(v_tile + (k0 + 16) * (D * 2) + 16 * (ch ^ C::swz(k0 + 16)) + in);
+      const Raw16 r = {v0.x, v0.y, v1.x, v1.y};
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+        o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf16x8, r), w[nb], o[nb][db], 0, 0, 0);
+    }
+    __builtin_amdgcn_wave_barrier();
+    return more;
+  };
+  for (int32_t t0 = t_begin; t0 < t_end; t0 += 32 * STEP) {
+    Runs runs;
+    runs.look_up(a, list, b, head_row, held, t0, STEP, t_end, bad);
+    uint64_t todo = runs.some;
+    // the next tile's rows set out (if there is one)
+    const auto next = [&](Rows& x) __attribute__((always_inline)) {
+      if (todo == 0) return false;
+      const int at = __builtin_ctzll(todo);
+      todo &= todo - 1;
+      fetch(x, runs, at);
+      return true;
+    };
+    Rows x;
+    bool more = next(x);
+    while (more) more = use(x, next);
   }
   if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, kDevBadPage);
 
+  if constexpr (SOLO) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const float sum = lanes_sum<4>(l[nb]);
+      const int r = nb * 16 + l16;
+      if (r >= heads) continue;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db)
+        row_out<D, false>(a, b, pl.h, pl.token * a.G + pl.tile * 16 * NB + r, 16 * db + 4 * g, o[nb][db], m[nb], sum);
+    }
+    return;
+  }
   // join the waves: each scales its sums to the largest maximum
+  __shared__ float lds_ml[kFewWaves][16 * NB][2];
+  __shared__ uint32_t lds_last;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     l[nb] = lanes_sum<4>(l[nb]);
@@ -489,7 +697,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_per_cu(F, D, NB)) void k_attend
   __syncthreads();
   AttendStream st;
   st.splits = a.splits;
-  join_parts<D, 16 * NB, false>(a, st, pl, b, pl.token * a.G + pl.tile * 16 * NB, heads, lds, lds_ml, &lds_last);
+  if constexpr (!SOLO) join_parts<D, 16 * NB, false>(a, st, pl, b, pl.token * a.G + pl.tile * 16 * NB, heads, lds, lds_ml, &lds_last);
 }
 
 // As k_attend_f32: fp32 pools, up to 32 query heads of a token.
@@ -498,10 +706,10 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_bloc
   __shared__ __attribute__((aligned(16))) char lds[kFewWaves][JoinLds<D, 32>::kWaveBytes];
   __shared__ float lds_ml[kFewWaves][32][2];
   __shared__ uint32_t lds_last;
-  const BlockPlace pl = block_place(a);
-  if (pl.slot < 0) return;
   const int lane = threadIdx.x % kWave, h = lane / 32, l32 = lane % 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const BlockPlace pl = block_place<false>(a, wave);
+  if (pl.slot < 0) return;
   const int b = a.b0 + pl.b;
   const int64_t head_row = a.layer_row + (int64_t)pl.h * a.pool.T.d;
   const int32_t held = min(a.s[pl.b].n, a.s[pl.b].first + pl.token + 1);
@@ -618,6 +826,6 @@ __global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_bloc
 
 // What a format's translation unit offers.
 template <int F>
-hipError_t launch_attend_blocks(int D, bool wide, uint32_t grid, const BlocksArgs& a, hipStream_t st);
+hipError_t launch_attend_blocks(int D, bool wide, bool solo, const BlocksArgs& a, hipStream_t st);
 
 }  // namespace ipv

@@ -58,14 +58,21 @@ struct Select {
   int64_t room;  // bytes for scores
 };
 
-template <int FB>
-void launch_scores(int D, dim3 grid, const SelectArgs& a, hipStream_t st) {
+template <int FB, int D, bool SPLIT>
+void launch_select_n(dim3 grid, const SelectArgs& a, hipStream_t st) {
   const dim3 block(kSelectThreads);
-  switch (D) {
-    case 32: k_block_scores<FB, 32><<<grid, block, 0, st>>>(a); break;
-    case 64: k_block_scores<FB, 64><<<grid, block, 0, st>>>(a); break;
-    case 128: k_block_scores<FB, 128><<<grid, block, 0, st>>>(a); break;
-    default: k_block_scores<FB, 256><<<grid, block, 0, st>>>(a); break;
+  if (a.padded <= 8 * kWave) k_block_select<FB, D, 8, SPLIT><<<grid, block, 0, st>>>(a);
+  else if (a.padded <= 32 * kWave) k_block_select<FB, D, 32, SPLIT><<<grid, block, 0, st>>>(a);
+  else k_block_select<FB, D, 0, SPLIT><<<grid, block, 0, st>>>(a);
+}
+template <bool SPLIT>
+void launch_select(const ipv_page_shape* s, dim3 grid, const SelectArgs& a, hipStream_t st) {
+  const bool f32 = s->format == IPV_PAGES_F32;
+  switch (s->head_dim) {
+    case 32: f32 ? launch_select_n<kFmtF32, 32, SPLIT>(grid, a, st) : launch_select_n<kFmtBf16, 32, SPLIT>(grid, a, st); break;
+    case 64: f32 ? launch_select_n<kFmtF32, 64, SPLIT>(grid, a, st) : launch_select_n<kFmtBf16, 64, SPLIT>(grid, a, st); break;
+    case 128: f32 ? launch_select_n<kFmtF32, 128, SPLIT>(grid, a, st) : launch_select_n<kFmtBf16, 128, SPLIT>(grid, a, st); break;
+    default: f32 ? launch_select_n<kFmtF32, 256, SPLIT>(grid, a, st) : launch_select_n<kFmtBf16, 256, SPLIT>(grid, a, st); break;
   }
 }
 
@@ -89,22 +96,15 @@ ipv_status select_blocks(Select* s, const Counts& c, hipStream_t st) {
     if (fit < most) fit = fit / kScoreTile * kScoreTile;
     fit = std::min<int64_t>(fit, std::max(65535 / a.H, 1) * (int64_t)kScoreTile);
     const int32_t step = (int32_t)std::min<int64_t>(std::max<int64_t>(fit, 1), most);
-    const int32_t tiles = a.padded / kScoreTile, waves = kSelectThreads / kWave;
     for (a.m0 = 0; a.m0 < most; a.m0 += step) {
       a.mq = std::min(step, most - a.m0);
       const int32_t y = a.H * ((a.mq + kScoreTile - 1) / kScoreTile);
-      if (tiles > 0) {
-        // a workgroup makes Q+ and Q- of its queries, then goes over the blocks: alone where the card is full of others
-        const int32_t x = std::min((tiles + waves - 1) / waves, std::max(1, 1024 / std::max(1, y * nb)));
-        const dim3 grid((uint32_t)x, (uint32_t)y, (uint32_t)nb);
-        if (s->pool->format == IPV_PAGES_F32) launch_scores<kFmtF32>(s->pool->head_dim, grid, a, st);
-        else launch_scores<kFmtBf16>(s->pool->head_dim, grid, a, st);
-        IPV_TRY(launched(hipGetLastError()));
-      }
-      const dim3 grid((uint32_t)((a.mq + waves - 1) / waves), (uint32_t)a.H, (uint32_t)nb);
-      if (a.padded <= 8 * kWave) k_block_pick<8><<<grid, dim3(kSelectThreads), 0, st>>>(a);
-      else if (a.padded <= 32 * kWave) k_block_pick<32><<<grid, dim3(kSelectThreads), 0, st>>>(a);
-      else k_block_pick<0><<<grid, dim3(kSelectThreads), 0, st>>>(a);
+      // several workgroups share the blocks where tiles of queries alone leave the card empty
+      const int32_t units = y * nb, x = units >= 256 ? 1 : std::max(1, std::min(a.padded / kScoreTile, 512 / units));
+      a.spread = std::max(kMaxParts / units, 1);
+      const dim3 grid((uint32_t)x, (uint32_t)y, (uint32_t)nb);
+      if (units >= 256) launch_select<false>(s->pool, grid, a, st);
+      else launch_select<true>(s->pool, grid, a, st);
       IPV_TRY(launched(hipGetLastError()));
     }
   }
@@ -133,6 +133,7 @@ ipv_status prepare_select(const ipv_page_shape* pool, const Pool& p, const Block
   a.max_rows = max_rows;
   a.first_blocks = first_blocks, a.last_blocks = last_blocks, a.top = top;
   a.scores = reinterpret_cast<double*>(static_cast<char*>(ws) + kZeroed);
+  a.arrived = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + kWsHeader);
   a.blocks = blocks;
   a.err = static_cast<uint32_t*>(ws);
   s->pool = pool;
@@ -143,7 +144,7 @@ ipv_status prepare_select(const ipv_page_shape* pool, const Pool& p, const Block
 // Workgroups that the card holds at once: with fewer queries than that, lists are split.
 int32_t blocks_fill(const ipv_page_shape* s, int32_t G) {
   const int D = s->head_dim;
-  return 256 * (s->format == IPV_PAGES_F32 ? (D <= 64 ? 2 : 1) : few_per_cu(s->format, D, block_heads(s, G) / 16));
+  return 256 * (s->format == IPV_PAGES_F32 ? (D <= 64 ? 2 : 1) : blocks_per_cu(s->format, D, block_heads(s, G) / 16));
 }
 
 size_t part_bytes(const ipv_page_shape* s, int32_t G, int64_t parts) {
@@ -282,13 +283,14 @@ ipv_status ipv_attend_blocks(const ipv_page_shape* pool, const void* K_pages, co
     }
     a.slots = (int32_t)at;
     a.part = a.part_ml + (size_t)a.slots * BM * 2;  // (a launch that splits has at most kMaxParts)
-    const uint32_t grid = (uint32_t)(a.slots + 7) / 8u * 8u;
+    // a wave a query where that fills the card
+    const bool solo = queries >= (int64_t)fill * kFewWaves;
     hipError_t e;
     switch (pool->format) {
-      case IPV_PAGES_BF16: e = launch_attend_blocks<kFmtBf16>(pool->head_dim, BM == 32, grid, a, st); break;
-      case IPV_PAGES_F32: e = launch_attend_blocks<kFmtF32>(pool->head_dim, true, grid, a, st); break;
-      case IPV_PAGES_FP8: e = launch_attend_blocks<kFmtFp8>(pool->head_dim, BM == 32, grid, a, st); break;
-      default: e = launch_attend_blocks<kFmtFp4>(pool->head_dim, BM == 32, grid, a, st); break;
+      case IPV_PAGES_BF16: e = launch_attend_blocks<kFmtBf16>(pool->head_dim, BM == 32, solo, a, st); break;
+      case IPV_PAGES_F32: e = launch_attend_blocks<kFmtF32>(pool->head_dim, true, false, a, st); break;
+      case IPV_PAGES_FP8: e = launch_attend_blocks<kFmtFp8>(pool->head_dim, BM == 32, solo, a, st); break;
+      default: e = launch_attend_blocks<kFmtFp4>(pool->head_dim, BM == 32, solo, a, st); break;
     }
     IPV_TRY(launched(e));
   }

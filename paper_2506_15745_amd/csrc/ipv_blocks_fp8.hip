@@ -1,4 +1,4 @@
 // Attention over lists of blocks of e4m3 pages.
 #include "ipv_blocks_launch.hpp"
 
-template hipError_t ipv::launch_attend_blocks<ipv::kFmtFp8>(int, bool, uint32_t, const ipv::BlocksArgs&, hipStream_t);
+template hipError_t ipv::launch_attend_blocks<ipv::kFmtFp8>(int, bool, bool, const ipv::BlocksArgs&, hipStream_t);
