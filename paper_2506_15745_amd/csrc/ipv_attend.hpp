@@ -180,12 +180,6 @@ __device__ __forceinline__ float wave_max(float v) {
 }
 __device__ __forceinline__ float wave_sum(float v) { return lanes_sum<4>(group_sum<16>(v)); }
 
-__device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
-  const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)v, lane, kWave);
-  const uint32_t hi = (uint32_t)__shfl((int)(uint32_t)((uint64_t)v >> 32), lane, kWave);
-  return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-
 // Four bf16 of one column from four rows of LDS: the 16 lanes of a group give
 // the addresses of a 4 x 16 block, row by row, 8 bytes each; lane i receives
 // column i.
@@ -306,20 +300,6 @@ __device__ __forceinline__ Raw16 piece8(const uint32_t* w, int s, float scale) {
   if (F == kFmtFp8) return fp8_to_bf16(w[2 * s], w[2 * s + 1], scale);
   if (F == kFmtFp4) return fp4_to_bf16(w[s], scale);
   return Raw16{w[0], w[1], w[2], w[3]};
-}
-
-template <int BYTES>
-__device__ __forceinline__ void load_piece(const char* p, uint32_t* w) {
-  if (BYTES == 16) {
-    const Raw16 r = load16(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = r.w[i];
-  } else if (BYTES == 8) {
-    const U32x2 r = *reinterpret_cast<const U32x2*>(p);
-    w[0] = r.x, w[1] = r.y;
-  } else {
-    w[0] = *reinterpret_cast<const uint32_t*>(p);
-  }
 }
 
 // Sixteen bytes a lane from memory straight into LDS: lane i's to `at` + 16 i, `at` the

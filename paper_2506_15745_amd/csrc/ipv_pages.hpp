@@ -106,6 +106,26 @@ __device__ __forceinline__ uint64_t load_scales(const uint8_t* scales, int64_t r
 }
 __device__ __forceinline__ float scale_at(uint64_t w, int block) { return scale_of((uint32_t)(w >> (8 * block)) & 255u); }
 
+__device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
+  const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)v, lane, kWave);
+  const uint32_t hi = (uint32_t)__shfl((int)(uint32_t)((uint64_t)v >> 32), lane, kWave);
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+template <int BYTES>
+__device__ __forceinline__ void load_piece(const char* p, uint32_t* w) {
+  if (BYTES == 16) {
+    const Raw16 r = load16(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = r.w[i];
+  } else if (BYTES == 8) {
+    const U32x2 r = *reinterpret_cast<const U32x2*>(p);
+    w[0] = r.x, w[1] = r.y;
+  } else {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  }
+}
+
 // ------------------------------------------------------------ rows in and out
 constexpr int kPageStreams = 128;  // streams of one launch (their counts travel in its arguments)
 constexpr int kPageThreads = 256;
@@ -255,12 +275,12 @@ __device__ __forceinline__ void store_scales(uint8_t* at, int thread, uint32_t e
 
 // A row into the pool, from the threads that hold it (lo and hi: eight elements of either half).
 // wl, wh: what is stored, as dwords of e4m3 (two) or e2m1 (one); el, eh: the scales' bytes.
-template <int F, int D, bool AGAIN = false>
+template <int F, int D, bool AGAIN = false, bool STREAM = false>
 __device__ __forceinline__ void put_row(char* pages, uint8_t* scales, int64_t row, int d, const float (&lo)[8], const float (&hi)[8],
                                         uint32_t* err, uint32_t (&wl)[2], uint32_t (&wh)[2], uint32_t& el, uint32_t& eh) {
   if (!fmt_scaled(F)) {
-    store_row8<F, false>(pages, row * D + d, lo);
-    store_row8<F, false>(pages, row * D + D / 2 + d, hi);
+    store_row8<F, STREAM>(pages, row * D + d, lo);
+    store_row8<F, STREAM>(pages, row * D + D / 2 + d, hi);
   } else {
     uint32_t ml = max_abs_bits(lo), mh = max_abs_bits(hi);
     if (D == 32) ml = mh = max(ml, mh);

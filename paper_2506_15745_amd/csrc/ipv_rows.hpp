@@ -124,8 +124,8 @@ struct Bounds {
         hi[s][i] = higher<F>(hi[s][i], dpp_u32<CTRL>(hi[s][i]));
       }
   }
-  // All threads of the workgroup: the block's bounds to `at`.
-  __device__ __forceinline__ void store(char* at, uint32_t* lds) {
+  // Over the wave's rows, in all of its lanes.
+  __device__ __forceinline__ void over_wave() {
     constexpr int RT = RowSplit<D>::kThreads;
     // within rows of 16 lanes the lanes RT apart hold the same channels: rotations by RT, 2 RT, .. 8
     if constexpr (RT <= 2) with_lane<0x122>();
@@ -144,6 +144,28 @@ struct Bounds {
         a = __builtin_amdgcn_permlane32_swap(h, h, false, false);
         hi[s][i] = higher<F>(a[0], a[1]);
       }
+  }
+  // The bounds of a wave's rows to `at`.
+  __device__ __forceinline__ void store_wave(char* at) {
+    over_wave();
+    const int lane = threadIdx.x % kWave;
+    if (lane >= RowSplit<D>::kThreads) return;
+    U32x4* to = reinterpret_cast<U32x4*>(at);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int i = 0; i < W; i += 4) {
+        const int piece = (s * (D / 16) + lane) * (W / 4) + i / 4;
+        U32x4 l, h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l[e] = ordered<F>(lo[s][i + e]), h[e] = ordered<F>(hi[s][i + e]);
+        to[piece] = l, to[D / 8 * (W / 4) + piece] = h;
+      }
+  }
+  // All threads of the workgroup: the bounds of its rows to `at`.
+  __device__ __forceinline__ void store(char* at, uint32_t* lds) {
+    constexpr int RT = RowSplit<D>::kThreads;
+    over_wave();
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     U32x4* to = reinterpret_cast<U32x4*>(lds);  // [wave][lo, hi][piece of eight channels][W]
     if (lane < RT) {
@@ -176,6 +198,42 @@ struct Bounds {
 
 // Bytes of a block's bounds.
 constexpr int bound_bytes(int F, int D) { return 2 * D * (F == kFmtF32 ? 4 : 2); }
+
+// ------------------------------------------------------------ angles of a wave's rows
+// The cosines and sines of a position lie in 4 D bytes, of which a thread of RowSplit needs 64. Loaded so by each, four
+// neighbouring lanes ask for four lines at a time, and the cache takes them one after the other; so the wave
+// loads its rows' angles in the order of memory and spreads them through LDS.
+template <int D>
+struct Angles {
+  static constexpr int PIECES = D / 4, LOADS = 4, LDS = LOADS * kWave * 16;  // 16-byte pieces of a position; bytes of LDS a wave
+  F32x4 piece[LOADS];
+  // pos(r): the position of the wave's row r (of kWave / RowSplit<D>::kThreads)
+  template <class POS>
+  __device__ __forceinline__ void load(const float* table, const POS& pos) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int x = i * kWave + threadIdx.x % kWave;
+      piece[i] = *reinterpret_cast<const F32x4*>(table + (int64_t)pos(x / PIECES) * D + x % PIECES * 4);
+    }
+  }
+  // The thread's eight pairs. A piece's place: those that neighbouring lanes read together lie in different banks.
+  __device__ __forceinline__ void spread(char* lds, float (&c)[8], float (&s)[8]) const {
+    const int lane = threadIdx.x % kWave;
+    F32x4* at = reinterpret_cast<F32x4*>(lds);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int x = i * kWave + lane;
+      at[x ^ (x / 4 % 4)] = piece[i];
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const F32x4 v = at[lane * 4 + (i ^ lane % 4)];
+      c[2 * i] = v.x, s[2 * i] = v.y, c[2 * i + 1] = v.z, s[2 * i + 1] = v.w;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+};
 
 // ------------------------------------------------------------ new tokens
 struct TokenCall {
@@ -385,96 +443,138 @@ struct CompactCall {
   BlockMap map;  // (the slices also without bounds)
   int32_t n[kPageStreams], rows[kPageStreams];
 };
-constexpr int kCompactRows = 2;  // rows that a thread has in hand
+constexpr int kCompactWaves = kPageThreads / kWave;
 
-// blockIdx.x: rows of the new pages, kCompactRows * kRows of them or (of keys, with bounds) a block; .y: slice, of K or
-// of V; .z: stream. A row's place takes two trips (keep_idx, the table) before its own; workgroups cover for
-// each other. Bound by the rows' bytes.
-template <int F, int D>
+// Rows that a wave takes: whole blocks where it makes their bounds.
+__host__ __device__ inline int64_t compact_run(bool bounds, uint32_t R) { return !bounds ? 32 : R >= 64 ? R : 64 / R * R; }
+
+// blockIdx.x: runs of rows of the new pages, a wave each; .y: slice, of K or of V; .z: stream. A wave looks up its next 64
+// rows at once, a row a lane (their places take two trips, to keep_idx and to the table); a block's bounds stay in the wave. Bound by the rows' bytes.
+template <int F, int D, bool TURN, bool BOUNDS>
 __global__ __launch_bounds__(kPageThreads) void k_page_compact(CompactCall c) {
-  using S = RowSplit<D>;
-  constexpr int W = kWords<F>, RB = fmt_row_bytes(F, D), PIECE = RB / S::kThreads / 2;  // stored bytes of eight elements
-  __shared__ __attribute__((aligned(16))) uint32_t lds[Bounds<F, D>::kLds];
-  const int b = blockIdx.z, thread = (int)(threadIdx.x % S::kThreads), d = thread * 8;
-  const uint32_t slice = blockIdx.y >> 1;
-  const bool isv = blockIdx.y & 1, block = !isv && c.bounds != nullptr;
-  const int per = block ? (int)c.map.R.d : kCompactRows * S::kRows;
-  const int64_t j0 = (int64_t)blockIdx.x * per, end = min(j0 + per, (int64_t)c.rows[b]);
-  if (j0 >= end) return;
-  const bool rot = !isv && c.rotary != nullptr;
+  constexpr int W = kWords<F>, RB = fmt_row_bytes(F, D), RT = RowSplit<D>::kThreads, PIECE = RB / RT / 2;  // stored bytes of eight elements
+  constexpr int ROWS = kWave / RT;  // of a step
+  __shared__ __attribute__((aligned(16))) char lds_angles[kCompactWaves][Angles<D>::LDS];
+  const int b = blockIdx.z, lane = threadIdx.x % kWave, thread = lane % RT, d = thread * 8;
+  const uint32_t slice = (blockIdx.y >> 1) * kCompactWaves + threadIdx.x / kWave;
+  if (slice >= (uint32_t)c.map.slices) return;  // the whole wave
+  const bool isv = blockIdx.y & 1, block = BOUNDS && !isv;
+  const int64_t run = compact_run(block, c.map.R.d);
+  const int64_t begin = (int64_t)blockIdx.x * run;
+  const int64_t end = min(begin + run, (int64_t)c.rows[b]);
+  if (begin >= end) return;  // the whole wave
   char* pages = isv ? c.pool.V : c.pool.K;
   uint8_t* scales = isv ? c.pool.Vs : c.pool.Ks;
   const int64_t slice_row = (int64_t)slice * c.pool.T.d;
   const int32_t* keep = c.keep + ((int64_t)(c.b0 + b) * c.map.slices + slice) * c.C;
   const int32_t* table = c.new_table + (int64_t)(c.b0 + b) * c.new_cols;
-  bool bad_page = false, bad_keep = false;
+  const int32_t n = c.n[b];
+  // rows of a step: they lie in one block
+  const int step = block && c.map.R.d % ROWS != 0 ? 16 : ROWS;
+  // what is stored of a row, eight elements of either half, and the row's scales
+  struct Stored {
+    uint32_t w[2][PIECE / 4];
+    uint64_t scales;
+  };
+  uint32_t errors = 0;
   Bounds<F, D> got;
-  for (int64_t j1 = j0 + threadIdx.x / S::kThreads; j1 < end; j1 += kCompactRows * S::kRows) {
-    int32_t at[kCompactRows];
-    int64_t from[kCompactRows], to[kCompactRows];
-    bool fine[kCompactRows];
-#pragma unroll
-    for (int u = 0; u < kCompactRows; ++u) at[u] = keep[min(j1 + u * S::kRows, end - 1)];
-#pragma unroll
-    for (int u = 0; u < kCompactRows; ++u) {
-      const uint32_t j = (uint32_t)min(j1 + u * S::kRows, end - 1);
+  for (int64_t j0 = begin; j0 < end; j0 += kWave) {
+    const int held = (int)min(end - j0, (int64_t)min((int64_t)kWave, run));
+    int32_t at;          // the lane's row's old position
+    int64_t from, to;    // where it was, where it goes (-1: nowhere)
+    int32_t new_page;
+    {
+      const uint32_t j = (uint32_t)(j0 + min(lane, held - 1));
+      at = keep[j];
+      new_page = table[fast_div(j, c.pool.T)];
+      const bool out = (uint32_t)at >= (uint32_t)n;
+      if (out) at = 0;
+      const uint32_t p = (uint32_t)at;
       bool x, y;
-      const bool out = (uint32_t)at[u] >= (uint32_t)c.n[b];
-      const uint32_t p = out ? 0u : (uint32_t)at[u];
-      const int32_t new_page = table[fast_div(j, c.pool.T)];
-      from[u] = pool_row(c.pool, c.n[b] > 0 ? pool_page(c.pool, c.b0 + b, p) : 0, p, &x) + slice_row;
-      to[u] = pool_row(c.pool, new_page, j, &y) + slice_row;
-      fine[u] = j1 + u * S::kRows < end && !out && !x && !y;
-      bad_keep |= out;
-      bad_page |= (x & !out) | y;
+      from = pool_row(c.pool, n > 0 ? pool_page(c.pool, c.b0 + b, p) : 0, p, &x) + slice_row;
+      to = pool_row(c.pool, new_page, j, &y) + slice_row;
+      if (out) errors |= kDevBadKeep;
+      if ((x & !out) | y) errors |= kDevBadPage;
+      if (out | x | y) to = -1;
     }
-    // what is stored, eight elements of either half, and the row's scales
-    uint32_t w[kCompactRows][2][PIECE / 4];
-    uint64_t sc[kCompactRows];
-#pragma unroll
-    for (int u = 0; u < kCompactRows; ++u) {
+    const auto fetch = [&](int64_t row, Stored& x) __attribute__((always_inline)) {
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const char* x = pages + from[u] * RB + s * (RB / 2) + thread * PIECE;
-#pragma unroll
-        for (int i = 0; i < PIECE / 4; ++i) w[u][s][i] = 0;
+        const char* at = pages + row * RB + s * (RB / 2) + thread * PIECE;
         if constexpr (PIECE >= 16) {
 #pragma unroll
-          for (int i = 0; i < PIECE / 16; ++i) {
-            const Raw16 r = load16(x + 16 * i);
+          for (int i = 0; i < PIECE / 16; ++i) load_piece<16>(at + 16 * i, x.w[s] + 4 * i);
+        } else {
+          load_piece<PIECE>(at, x.w[s]);
+        }
+      }
+      if constexpr (fmt_scaled(F)) x.scales = load_scales<D>(scales, row);
+    };
+    const auto store = [&](int64_t row, const Stored& x) __attribute__((always_inline)) {  // past the caches, as it is not read soon
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[u][s][4 * i + e] = r.w[e];
-          }
+      for (int s = 0; s < 2; ++s) {
+        char* at = pages + row * RB + s * (RB / 2) + thread * PIECE;
+        if constexpr (PIECE >= 16) {
+#pragma unroll
+          for (int i = 0; i < PIECE / 16; ++i)
+            __builtin_nontemporal_store(U32x4{x.w[s][4 * i], x.w[s][4 * i + 1], x.w[s][4 * i + 2], x.w[s][4 * i + 3]},
+                                        reinterpret_cast<U32x4*>(at + 16 * i));
         } else if constexpr (PIECE == 8) {
-          const U32x2 r = *reinterpret_cast<const U32x2*>(x);
-          w[u][s][0] = r.x, w[u][s][1] = r.y;
+          *reinterpret_cast<U32x2*>(at) = U32x2{x.w[s][0], x.w[s][1]};
         } else {
-          w[u][s][0] = *reinterpret_cast<const uint32_t*>(x);
+          *reinterpret_cast<uint32_t*>(at) = x.w[s][0];
         }
       }
-      sc[u] = 0;
-      if constexpr (fmt_scaled(F)) sc[u] = load_scales<D>(scales, from[u]);
+      if constexpr (fmt_scaled(F)) {
+        if (thread == 0) {
+          uint8_t* at = scales + row * (D / kScaleBlock);
+          if (D == 32) *at = (uint8_t)x.scales;
+          else if (D == 64) *reinterpret_cast<uint16_t*>(at) = (uint16_t)x.scales;
+          else if (D == 128) *reinterpret_cast<uint32_t*>(at) = (uint32_t)x.scales;
+          else reinterpret_cast<uint32_t*>(at)[0] = (uint32_t)x.scales, reinterpret_cast<uint32_t*>(at)[1] = (uint32_t)(x.scales >> 32);
+        }
+      }
+    };
+    if (isv || !(TURN || BOUNDS)) {  // copied: four steps at a time
+      constexpr int STEPS = 4;
+      for (int r0 = 0; r0 < held; r0 += STEPS * ROWS) {
+        Stored x[STEPS];
+#pragma unroll
+        for (int u = 0; u < STEPS; ++u) fetch(shfl64(from, min(r0 + u * ROWS + lane / RT, held - 1)), x[u]);
+#pragma unroll
+        for (int u = 0; u < STEPS; ++u) {
+          const int r = r0 + u * ROWS + lane / RT;
+          const int64_t row = shfl64(to, min(r, held - 1));
+          if (r < held && row >= 0) store(row, x[u]);
+        }
+      }
+      continue;
     }
-#pragma unroll
-    for (int u = 0; u < kCompactRows; ++u) {
-      if (!fine[u]) continue;
-      const uint32_t j = (uint32_t)(j1 + u * S::kRows);
-      // as bf16 or fp32, where they are looked into
-      uint32_t a[W], z[W];
-      if (!isv) {
-        if constexpr (!fmt_scaled(F)) {
-#pragma unroll
-          for (int i = 0; i < W; ++i) a[i] = w[u][0][i], z[i] = w[u][1][i];
-        } else {
-          const float fl = scale_at(sc[u], d / kScaleBlock), fh = scale_at(sc[u], (D / 2 + d) / kScaleBlock);
-          const Raw16 x = F == kFmtFp8 ? fp8_to_bf16(w[u][0][0], w[u][0][PIECE / 4 - 1], fl) : fp4_to_bf16(w[u][0][0], fl);
-          const Raw16 y = F == kFmtFp8 ? fp8_to_bf16(w[u][1][0], w[u][1][PIECE / 4 - 1], fh) : fp4_to_bf16(w[u][1][0], fh);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) a[i] = x.w[i], z[i] = y.w[i];
-        }
+    if constexpr (TURN || BOUNDS) for (int r0 = 0; r0 < held; r0 += step) {
+      const int r = r0 + lane / RT, own = min(r, held - 1);
+      Stored x;
+      fetch(shfl64(from, own), x);
+      const int64_t row = shfl64(to, own);
+      const uint32_t j = (uint32_t)(j0 + r), p = (uint32_t)__shfl(at, own, kWave);
+      Angles<D> old, now;
+      if constexpr (TURN) {
+        old.load(c.rotary, [&](int y) __attribute__((always_inline)) { return __shfl(at, min(r0 + y, held - 1), kWave); });
+        now.load(c.rotary, [&](int y) __attribute__((always_inline)) { return j0 + min(r0 + y, held - 1); });
       }
-      if (rot && (uint32_t)at[u] != j) {
-        float lo[8], hi[8], cs[8], sn[8];
+      // as bf16 or fp32
+      uint32_t a[W], z[W];
+      if constexpr (!fmt_scaled(F)) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) a[i] = x.w[0][i], z[i] = x.w[1][i];
+      } else {
+        const float fl = scale_at(x.scales, d / kScaleBlock), fh = scale_at(x.scales, (D / 2 + d) / kScaleBlock);
+        const Raw16 u = F == kFmtFp8 ? fp8_to_bf16(x.w[0][0], x.w[0][PIECE / 4 - 1], fl) : fp4_to_bf16(x.w[0][0], fl);
+        const Raw16 v = F == kFmtFp8 ? fp8_to_bf16(x.w[1][0], x.w[1][PIECE / 4 - 1], fh) : fp4_to_bf16(x.w[1][0], fh);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = u.w[i], z[i] = v.w[i];
+      }
+      float lo[8], hi[8];
+      if constexpr (TURN) {
         if constexpr (F == kFmtF32) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) lo[i] = __uint_as_float(a[i]), hi[i] = __uint_as_float(z[i]);
@@ -482,45 +582,33 @@ __global__ __launch_bounds__(kPageThreads) void k_page_compact(CompactCall c) {
           Lane<uint16_t>::decode(Raw16{a[0], a[1], a[2], a[3]}, lo);
           Lane<uint16_t>::decode(Raw16{z[0], z[1], z[2], z[3]}, hi);
         }
-        load_angles(c.rotary, at[u], D / 2, d, cs, sn);
+        float cs[8], sn[8];
+        old.spread(lds_angles[threadIdx.x / kWave], cs, sn);
         turn(lo, hi, cs, sn, true);
-        load_angles(c.rotary, j, D / 2, d, cs, sn);
+        now.spread(lds_angles[threadIdx.x / kWave], cs, sn);
         turn(lo, hi, cs, sn, false);
-        uint32_t el, eh, xl[2], xh[2];
-        put_row<F, D, true>(pages, scales, to[u], d, lo, hi, c.err, xl, xh, el, eh);
-        if (block) got.add_put(lo, hi, xl, xh, el, eh);
-        continue;
       }
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        char* x = pages + to[u] * RB + s * (RB / 2) + thread * PIECE;
-        if constexpr (PIECE >= 16) {
-#pragma unroll
-          for (int i = 0; i < PIECE / 16; ++i)
-            *reinterpret_cast<Raw16*>(x + 16 * i) = Raw16{w[u][s][4 * i], w[u][s][4 * i + 1], w[u][s][4 * i + 2], w[u][s][4 * i + 3]};
-        } else if constexpr (PIECE == 8) {
-          *reinterpret_cast<U32x2*>(x) = U32x2{w[u][s][0], w[u][s][1]};
+      if ((lane / RT < step) & (r < held) & (row >= 0)) {  // (whole rows' threads together)
+        if (TURN && p != j) {
+          uint32_t el, eh, xl[2], xh[2];
+          put_row<F, D, true, true>(pages, scales, row, d, lo, hi, c.err, xl, xh, el, eh);
+          if constexpr (BOUNDS) got.add_put(lo, hi, xl, xh, el, eh);
         } else {
-          *reinterpret_cast<uint32_t*>(x) = w[u][s][0];
+          store(row, x);
+          if constexpr (BOUNDS) got.add(a, z);
         }
       }
-      if constexpr (fmt_scaled(F)) {
-        if (thread == 0) {
-          uint8_t* x = scales + to[u] * (D / kScaleBlock);
-          if (D == 32) *x = (uint8_t)sc[u];
-          else if (D == 64) *reinterpret_cast<uint16_t*>(x) = (uint16_t)sc[u];
-          else if (D == 128) *reinterpret_cast<uint32_t*>(x) = (uint32_t)sc[u];
-          else reinterpret_cast<uint32_t*>(x)[0] = (uint32_t)sc[u], reinterpret_cast<uint32_t*>(x)[1] = (uint32_t)(sc[u] >> 32);
-        }
-      }
-      if (block) got.add(a, z);
+      if constexpr (!BOUNDS) continue;
+      // the block's last step: its bounds
+      const uint32_t done = (uint32_t)(j0 + min(r0 + step, held)), before = (uint32_t)(j0 + r0);
+      if (done < (uint32_t)end && done - fast_div(done, c.map.R) * c.map.R.d != 0) continue;
+      const int32_t page = __shfl(new_page, r0, kWave);
+      if ((uint32_t)page < (uint32_t)c.pool.pages)  // (else reported above)
+        got.store_wave(c.bounds + c.map.block(page, slice, fast_div(before, c.map.R) * c.map.R.d, c.pool.T) * bound_bytes(F, D));
+      got = Bounds<F, D>();
     }
   }
-  if (bad_page || bad_keep) atomicOr(c.err, (bad_page ? kDevBadPage : 0u) | (bad_keep ? kDevBadKeep : 0u));
-  if (!block) return;
-  const int32_t page = table[fast_div((uint32_t)j0, c.pool.T)];
-  if ((uint32_t)page >= (uint32_t)c.pool.pages) return;  // the whole workgroup (reported above)
-  got.store(c.bounds + c.map.block(page, slice, (uint32_t)j0, c.pool.T) * bound_bytes(F, D), lds);
+  if (errors != 0) atomicOr(c.err, errors);
 }
 
 // ------------------------------------------------------------ pages onto pages

@@ -15,8 +15,8 @@ static_assert(kDevBadKeep == IPV_DEV_BAD_KEEP, "the error bits of the header");
 
 namespace {
 
-int64_t row_blocks(int D, int64_t rows, int64_t per_thread = 1) {
-  const int64_t per = kPageThreads / (D / 16) * per_thread;
+int64_t row_blocks(int D, int64_t rows) {
+  const int64_t per = kPageThreads / (D / 16);
   return (rows + per - 1) / per;
 }
 
@@ -185,14 +185,21 @@ ipv_status ipv_page_compact(const ipv_page_shape* pool, void* K_pages, void* V_p
     int64_t blocks = 0;
     for (int32_t i = 0; i < nb; ++i) {
       c.n[i] = n_tokens[b0 + i], c.rows[i] = rows[b0 + i];
-      blocks = std::max(blocks, row_blocks(pool->head_dim, c.rows[i], kCompactRows));
-      if (bounds) blocks = std::max(blocks, touched(0, c.rows[i], block_rows));
+      for (bool with : {false, bounds != nullptr}) {
+        const int64_t per = compact_run(with, c.map.R.d);
+        blocks = std::max(blocks, (c.rows[i] + per - 1) / per);
+      }
     }
     if (blocks == 0) continue;
     c.b0 = b0;
-    const dim3 grid((uint32_t)blocks, (uint32_t)(2 * c.map.slices), (uint32_t)nb);
+    const dim3 grid((uint32_t)blocks, (uint32_t)(2 * ((c.map.slices + kCompactWaves - 1) / kCompactWaves)), (uint32_t)nb);
     IPV_TRY(launched(by_shape(pool, [&](auto f, auto d) {
-      k_page_compact<decltype(f)::value, decltype(d)::value><<<grid, dim3(kPageThreads), 0, st>>>(c);
+      constexpr int F = decltype(f)::value, D = decltype(d)::value;
+      const dim3 block(kPageThreads);
+      if (rotary && bounds) k_page_compact<F, D, true, true><<<grid, block, 0, st>>>(c);
+      else if (rotary) k_page_compact<F, D, true, false><<<grid, block, 0, st>>>(c);
+      else if (bounds) k_page_compact<F, D, false, true><<<grid, block, 0, st>>>(c);
+      else k_page_compact<F, D, false, false><<<grid, block, 0, st>>>(c);
     })));
   }
   return IPV_OK;
