@@ -65,19 +65,22 @@ template <int NR>
 struct Scores {
   double s[NR > 0 ? NR : 1];
   // block r * 64 + lane's score (past the last one's: the last)
-  static __device__ __forceinline__ double at(const SelectArgs& a, int b, int h, int i, int32_t count, int r, bool cross) {
-    double* p = a.scores + (((int64_t)b * a.H + h) * a.mq + (i - a.m0)) * a.padded + min(r * kWave + (int)threadIdx.x % kWave, count - 1);
+  static __device__ __forceinline__ double at(double* scores, int32_t count, int r, bool cross) {
+    double* p = scores + min(r * kWave + (int)threadIdx.x % kWave, count - 1);
     return cross ? __builtin_bit_cast(double, __hip_atomic_load(reinterpret_cast<uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
                  : *p;
   }
-  __device__ __forceinline__ void load(const SelectArgs& a, int b, int h, int i, bool cross) {
-    const int32_t count = candidates(a, b, i);
+  __device__ __forceinline__ void load(double* scores, int32_t count, bool cross) {
 #pragma unroll
-    for (int r = 0; r < NR; ++r) s[r] = r * kWave < count ? at(a, b, h, i, count, r, cross) : 0;
+    for (int r = 0; r < NR; ++r) s[r] = r * kWave < count ? at(scores, count, r, cross) : 0;
   }
 };
+__device__ __forceinline__ double* scores_of(const SelectArgs& a, int b, int h, int i) {
+  return a.scores + (((int64_t)b * a.H + h) * a.mq + (i - a.m0)) * a.padded;
+}
 template <int NR>
-__device__ __forceinline__ void pick_blocks(const SelectArgs& a, const Scores<NR>& scores, int b, int h, int i, bool cross, uint32_t* hist) {
+__device__ __forceinline__ void pick_blocks(const SelectArgs& a, const Scores<NR>& held, double* scores, int b, int h, int i, bool cross,
+                                            uint32_t* hist) {
   const int lane = threadIdx.x % kWave;
   const int32_t count = candidates(a, b, i), want = min(a.top, count);
   int32_t* to = a.blocks + (((int64_t)(a.b0 + b) * a.H + h) * a.max_rows + i) * a.top;
@@ -90,14 +93,14 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, const Scores<NR
   uint64_t key[N];
   if constexpr (NR > 0) {
 #pragma unroll
-    for (int r = 0; r < NR; ++r) key[r] = key_of(r, scores.s[r]);
+    for (int r = 0; r < NR; ++r) key[r] = key_of(r, held.s[r]);
   }
   const auto each = [&](auto&& what) __attribute__((always_inline)) {
     if constexpr (NR > 0) {
 #pragma unroll
       for (int r = 0; r < NR; ++r) what(r, key[r]);
     } else {
-      for (int r = 0; r < turns; ++r) what(r, key_of(r, Scores<NR>::at(a, b, h, i, count, r, cross)));
+      for (int r = 0; r < turns; ++r) what(r, key_of(r, Scores<NR>::at(scores, count, r, cross)));
     }
   };
   const auto at_least = [&](uint64_t x) __attribute__((always_inline)) {
@@ -186,6 +189,134 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, const Scores<NR
   for (int x = pos + lane; x < a.top; x += kWave) to[x] = -1;
 }
 
+// Q+ and Q- of four channels: sums over the group's heads, the first one's elements at `at`.
+template <int FB>
+__device__ __forceinline__ void group_queries(const SelectArgs& a, int64_t at, double (&plus)[4], double (&minus)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) plus[e] = minus[e] = 0;
+  constexpr int HEADS = 8;  // on their way at once
+  for (int g0 = 0; g0 < a.G; g0 += HEADS) {
+    float f[HEADS][4];
+#pragma unroll
+    for (int g = 0; g < HEADS; ++g) {
+      const int64_t from = at + min(g0 + g, a.G - 1) * a.q_h;
+      if constexpr (FB == kFmtF32) {
+        Lane<float>::decode(load16(a.q + from * 4), f[g]);
+      } else {
+        const U32x2 w = *reinterpret_cast<const U32x2*>(a.q + from * 2);
+        f[g][0] = __uint_as_float(w.x << 16), f[g][1] = __uint_as_float(w.x & 0xffff0000u);
+        f[g][2] = __uint_as_float(w.y << 16), f[g][3] = __uint_as_float(w.y & 0xffff0000u);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < HEADS; ++g) {
+      if (g0 + g >= a.G) break;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {  // (a NaN reaches both)
+        plus[e] += (double)(f[g][e] < 0.f ? 0.f : f[g][e]);
+        minus[e] += (double)(f[g][e] > 0.f ? 0.f : f[g][e]);
+      }
+    }
+  }
+}
+
+// The list of one query of a head. blockIdx.x: query; .y: head; .z: stream. Eight lanes have a block's bounds, eight blocks
+// a wave at a time, and add up their products in the vector unit: the matrix unit would take 16 queries' time for one.
+// Scores stay in LDS, and no workgroup waits for another. For few queries over up to 64 NR blocks; one token of 16 streams
+// of four heads over 512 blocks of 128 15 us, over 98 8: the way to the rows and back, and the products (64 bits a channel).
+constexpr int kOneThreads = 512;
+template <int FB, int D, int NR>
+__global__ __launch_bounds__(kOneThreads) void k_block_select_one(SelectArgs a) {
+  constexpr int E = FB == kFmtF32 ? 4 : 2, PER = 16 / E, PIECES = 2 * D / 8 / PER;  // bytes of an element; elements of 16 bytes; of these, a lane's
+  constexpr bool HELD = D <= 128;  // the lane's part of the queries in registers
+  constexpr int WAVES = kOneThreads / kWave, AHEAD = PIECES <= 4 ? 4 : PIECES <= 8 ? 2 : 1;  // eights of blocks on their way
+  __shared__ __attribute__((aligned(16))) double lds_q[2 * D];
+  __shared__ double lds_scores[NR * kWave];
+  __shared__ __attribute__((aligned(16))) uint32_t hist[256];
+  const int b = blockIdx.z, h = blockIdx.y, i = a.m0 + (int)blockIdx.x;
+  if (i >= min(a.m0 + a.mq, a.rows[b])) return;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int32_t count = candidates(a, b, i);
+  const int own = lane / 8, part = lane % 8;
+  bool bad = false;
+  struct Piece {
+    Raw16 r[PIECES];
+  };
+  // the page of the lane's block, and its part of the bounds there (blocks past the last: the last one again)
+  const auto page_of = [&](int j0) __attribute__((always_inline)) {
+    const uint32_t p = (uint32_t)min(j0 + own, count - 1) * a.map.R.d;
+    return a.table ? a.table[(int64_t)(a.b0 + b) * a.cols + fast_div(p, a.T)] : a.b0 + b;
+  };
+  const auto load_block = [&](int j0, int32_t page) __attribute__((always_inline)) {
+    const uint32_t p = (uint32_t)min(j0 + own, count - 1) * a.map.R.d;
+    if ((uint32_t)page >= (uint32_t)a.pages) page = 0, bad = true;
+    const char* at = a.bounds + a.map.block(page, (uint32_t)(a.layer * a.H + h), p, a.T) * (2 * D * E) + part * 16;
+    Piece x;
+#pragma unroll
+    for (int c = 0; c < PIECES; ++c) x.r[c] = load16(at + c * 128);
+    return x;
+  };
+  Piece ahead[AHEAD] = {};
+  int j0 = wave * 8;
+  constexpr int STEP = WAVES * 8;
+  int32_t page = 0;  // of the blocks after those on their way
+  if (j0 < count) {
+    int32_t pages[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) pages[u] = page_of(j0 + u * STEP);
+    page = page_of(j0 + AHEAD * STEP);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (j0 + u * STEP < count) ahead[u] = load_block(j0 + u * STEP, pages[u]);
+  }
+  if (threadIdx.x < D / 4) {
+    const int channel = threadIdx.x * 4;
+    double plus[4], minus[4];
+    group_queries<FB>(a, (int64_t)(a.b0 + b) * a.q_b + (int64_t)h * a.G * a.q_h + (int64_t)i * a.q_m + channel, plus, minus);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) lds_q[channel + e] = minus[e], lds_q[D + channel + e] = plus[e];
+  }
+  __syncthreads();
+  const auto query = [&](int c, int e) __attribute__((always_inline)) { return lds_q[(c * 8 + part) * PER + e]; };
+  double q[HELD ? PIECES : 1][HELD ? PER : 1];
+  if constexpr (HELD) {
+#pragma unroll
+    for (int c = 0; c < PIECES; ++c)
+#pragma unroll
+      for (int e = 0; e < PER; ++e) q[c][e] = query(c, e);
+  }
+  for (; j0 < count; j0 += STEP) {
+    const Piece x = ahead[0];
+#pragma unroll
+    for (int u = 0; u + 1 < AHEAD; ++u) ahead[u] = ahead[u + 1];
+    if (j0 + AHEAD * STEP < count) {
+      ahead[AHEAD - 1] = load_block(j0 + AHEAD * STEP, page);
+      page = page_of(j0 + (AHEAD + 1) * STEP);
+    }
+    double s = 0, s1 = 0;
+#pragma unroll
+    for (int c = 0; c < PIECES; ++c) {
+      float f[PER];
+      if constexpr (FB == kFmtF32) Lane<float>::decode(x.r[c], f);
+      else Lane<uint16_t>::decode(x.r[c], f);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        const double v = HELD ? q[HELD ? c : 0][HELD ? e : 0] : query(c, e);
+        if (e % 2) s1 = __builtin_fma((double)f[e], v, s1);
+        else s = __builtin_fma((double)f[e], v, s);
+      }
+    }
+    s = group_sum64<8>(s + s1);
+    if (part == 0 && j0 + own < count) lds_scores[j0 + own] = s;
+  }
+  if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, kDevBadPage);
+  __syncthreads();
+  if (wave != 0) return;
+  Scores<NR> scores;
+  scores.load(lds_scores, count, false);
+  pick_blocks<NR>(a, scores, lds_scores, b, h, i, false, hist);
+}
+
 // Where channel ch (of 2 D) of query col is: step 8 (ch / 32) + ch % 8, place ch / 8 % 4, and the queries of a place in an
 // order by which the channels that a wave writes together lie in different banks.
 __device__ __forceinline__ int select_place(int ch, int col) {
@@ -249,34 +380,8 @@ __global__ __launch_bounds__(kSelectThreads) void k_block_select(SelectArgs a) {
   // four channels of a query a thread (of the queries that there are: what is in the other columns reaches no score of these)
   for (int x = threadIdx.x; x < (i1 - i0) * (D / 4); x += kSelectThreads) {
     const int col = x / (D / 4), channel = x % (D / 4) * 4;
-    const int64_t at = (int64_t)(a.b0 + b) * a.q_b + (int64_t)h * a.G * a.q_h + (int64_t)(i0 + col) * a.q_m + channel;
     double plus[4], minus[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) plus[e] = minus[e] = 0;
-    constexpr int HEADS = 8;  // on their way at once
-    for (int g0 = 0; g0 < a.G; g0 += HEADS) {
-      float f[HEADS][4];
-#pragma unroll
-      for (int g = 0; g < HEADS; ++g) {
-        const int64_t from = at + min(g0 + g, a.G - 1) * a.q_h;
-        if constexpr (FB == kFmtF32) {
-          Lane<float>::decode(load16(a.q + from * 4), f[g]);
-        } else {
-          const U32x2 w = *reinterpret_cast<const U32x2*>(a.q + from * 2);
-          f[g][0] = __uint_as_float(w.x << 16), f[g][1] = __uint_as_float(w.x & 0xffff0000u);
-          f[g][2] = __uint_as_float(w.y << 16), f[g][3] = __uint_as_float(w.y & 0xffff0000u);
-        }
-      }
-#pragma unroll
-      for (int g = 0; g < HEADS; ++g) {
-        if (g0 + g >= a.G) break;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {  // (a NaN reaches both)
-          plus[e] += (double)(f[g][e] < 0.f ? 0.f : f[g][e]);
-          minus[e] += (double)(f[g][e] > 0.f ? 0.f : f[g][e]);
-        }
-      }
-    }
+    group_queries<FB>(a, (int64_t)(a.b0 + b) * a.q_b + (int64_t)h * a.G * a.q_h + (int64_t)(i0 + col) * a.q_m + channel, plus, minus);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {  // the bounds' first D channels are the lowest elements
       lds[select_place(channel + e, col)] = minus[e];
@@ -323,7 +428,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_block_select(SelectArgs a) {
     // a lane has the scores, or their parts, of its query (lane % 16) and of the tile's blocks 4 e + lane / 16
     const auto keep = [&](int col, int i, double v) __attribute__((always_inline)) {
       if (i0 + col >= i1) return;
-      double* to = a.scores + (((int64_t)b * a.H + h) * a.mq + (i0 + col - a.m0)) * a.padded + tile * kScoreTile + i;
+      double* to = scores_of(a, b, h, i0 + col) + tile * kScoreTile + i;
       if (sharing > 1)
         __hip_atomic_store(reinterpret_cast<uint64_t*>(to), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       else *to = v;
@@ -357,11 +462,12 @@ __global__ __launch_bounds__(kSelectThreads) void k_block_select(SelectArgs a) {
   static_assert(sizeof(lds) >= kSelectWaves * 256 * sizeof(uint32_t), "a histogram a wave");
   uint32_t* hist = reinterpret_cast<uint32_t*>(lds) + wave * 256;
   Scores<NR> later;
-  if (i0 + wave < i1) later.load(a, b, h, i0 + wave, sharing > 1);
+  if (i0 + wave < i1) later.load(scores_of(a, b, h, i0 + wave), candidates(a, b, i0 + wave), sharing > 1);
   for (int i = i0 + wave; i < i1; i += kSelectWaves) {
     const Scores<NR> scores = later;
-    if (i + kSelectWaves < i1) later.load(a, b, h, i + kSelectWaves, sharing > 1);
-    pick_blocks<NR>(a, scores, b, h, i, sharing > 1, hist);
+    const int then = i + kSelectWaves;
+    if (then < i1) later.load(scores_of(a, b, h, then), candidates(a, b, then), sharing > 1);
+    pick_blocks<NR>(a, scores, scores_of(a, b, h, i), b, h, i, sharing > 1, hist);
   }
 }
 

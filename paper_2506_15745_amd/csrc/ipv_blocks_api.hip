@@ -14,6 +14,13 @@ using namespace ipv;
 namespace {
 
 constexpr int32_t kMaxTop = 4096;
+// Whether each query of a launch has a workgroup of its own: for up to 2048 blocks (its scores are in LDS), unless
+// there are so many scores that the matrix unit is faster, or so few queries that sharing one's blocks out is. One token over 512
+// blocks of 128: 8 of them (a stream of 8 KV heads) 12.8 us so and 8.7 shared out, 32 13.2 and 13.2, 64 14.9 and 16.9; 128 and
+// 784 of them over 98 blocks 8.4 and 18, 21 and 22; 8192 over 512 about 100 and 72.
+bool select_alone(int64_t queries, int32_t padded) {
+  return padded <= 32 * kWave && queries * padded <= 1 << 20 && (padded <= 256 || queries >= 32);
+}
 constexpr int64_t kScoreBytes = 128ll << 20;  // of scores at a time, where 16 queries of each stream need no more
 
 int32_t padded_blocks(int32_t n, int32_t block_rows) {
@@ -76,6 +83,21 @@ void launch_select(const ipv_page_shape* s, dim3 grid, const SelectArgs& a, hipS
   }
 }
 
+template <int FB, int D>
+void launch_one_d(dim3 grid, const SelectArgs& a, hipStream_t st) {
+  if (a.padded <= 8 * kWave) k_block_select_one<FB, D, 8><<<grid, dim3(kOneThreads), 0, st>>>(a);
+  else k_block_select_one<FB, D, 32><<<grid, dim3(kOneThreads), 0, st>>>(a);
+}
+void launch_one(const ipv_page_shape* s, dim3 grid, const SelectArgs& a, hipStream_t st) {
+  const bool f32 = s->format == IPV_PAGES_F32;
+  switch (s->head_dim) {
+    case 32: f32 ? launch_one_d<kFmtF32, 32>(grid, a, st) : launch_one_d<kFmtBf16, 32>(grid, a, st); break;
+    case 64: f32 ? launch_one_d<kFmtF32, 64>(grid, a, st) : launch_one_d<kFmtBf16, 64>(grid, a, st); break;
+    case 128: f32 ? launch_one_d<kFmtF32, 128>(grid, a, st) : launch_one_d<kFmtBf16, 128>(grid, a, st); break;
+    default: f32 ? launch_one_d<kFmtF32, 256>(grid, a, st) : launch_one_d<kFmtBf16, 256>(grid, a, st); break;
+  }
+}
+
 // The lists of every stream's queries.
 ipv_status select_blocks(Select* s, const Counts& c, hipStream_t st) {
   SelectArgs& a = s->a;
@@ -101,6 +123,11 @@ ipv_status select_blocks(Select* s, const Counts& c, hipStream_t st) {
       const int32_t y = a.H * ((a.mq + kScoreTile - 1) / kScoreTile);
       // several workgroups share the blocks where tiles of queries alone leave the card empty
       const int32_t units = y * nb, x = units >= 256 ? 1 : std::max(1, std::min(a.padded / kScoreTile, 512 / units));
+      if (select_alone((int64_t)nb * a.H * a.mq, a.padded)) {
+        launch_one(s->pool, dim3((uint32_t)a.mq, (uint32_t)a.H, (uint32_t)nb), a, st);
+        IPV_TRY(launched(hipGetLastError()));
+        continue;
+      }
       a.spread = std::max(kMaxParts / units, 1);
       const dim3 grid((uint32_t)x, (uint32_t)y, (uint32_t)nb);
       if (units >= 256) launch_select<false>(s->pool, grid, a, st);

@@ -2,6 +2,8 @@
 // kernels that write rows into pages and read them back.
 #pragma once
 
+#include <type_traits>
+
 #include "ipv_device.hpp"
 
 namespace ipv {
@@ -124,6 +126,21 @@ __device__ __forceinline__ void load_piece(const char* p, uint32_t* w) {
   } else {
     w[0] = *reinterpret_cast<const uint32_t*>(p);
   }
+}
+
+// Sum over aligned groups of G lanes (2, 4, 8 or 16), the same in all of them.
+template <int G>
+__device__ __forceinline__ double group_sum64(double v) {
+  const auto other = [](double x, auto ctrl) __attribute__((always_inline)) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = dpp_u32<decltype(ctrl)::value>((uint32_t)u), hi = dpp_u32<decltype(ctrl)::value>((uint32_t)(u >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  };
+  v += other(v, std::integral_constant<int, kDppXor1>());
+  if (G >= 4) v += other(v, std::integral_constant<int, kDppXor2>());
+  if (G >= 8) v += other(v, std::integral_constant<int, kDppHalfMirror>());
+  if (G >= 16) v += other(v, std::integral_constant<int, kDppRowMirror>());
+  return v;
 }
 
 // ------------------------------------------------------------ rows in and out

@@ -3,8 +3,6 @@
 // new pages; pages onto pages.
 #pragma once
 
-#include <type_traits>
-
 #include "ipv_pages.hpp"
 
 namespace ipv {
@@ -254,21 +252,6 @@ struct TokenCall {
   BlockMap map;                // (with bounds)
   int32_t first[kPageStreams], rows[kPageStreams];
 };
-
-// Sum over the threads of a row, in all of them.
-template <int G>
-__device__ __forceinline__ double group_sum64(double v) {
-  const auto other = [](double x, auto ctrl) __attribute__((always_inline)) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = dpp_u32<decltype(ctrl)::value>((uint32_t)u), hi = dpp_u32<decltype(ctrl)::value>((uint32_t)(u >> 32));
-    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-  };
-  v += other(v, std::integral_constant<int, kDppXor1>());
-  if (G >= 4) v += other(v, std::integral_constant<int, kDppXor2>());
-  if (G >= 8) v += other(v, std::integral_constant<int, kDppHalfMirror>());
-  if (G >= 16) v += other(v, std::integral_constant<int, kDppRowMirror>());
-  return v;
-}
 
 // x * s * norm, s = 1 / sqrt(mean x^2 + eps). The mean is in 64 bits, so that s is the same fp32 number
 // whatever the order of the sum: rows are rounded to few bits next, where a last bit of 32 decides now and then.

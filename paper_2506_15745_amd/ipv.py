@@ -767,7 +767,8 @@ def _float_row(what, t, n, pool):
     """(pointer of) an fp32 row of n elements, or None."""
     if t is None:
         return None
-    _expect(what, t, (n,), torch.float32, pool.device)
+    if t.dtype is not torch.float32 or t.shape != (n,) or t.get_device() != pool._dev:
+        _expect(what, t, (n,), torch.float32, pool.device)
     return _ptr(t)
 
 
@@ -775,11 +776,22 @@ def _angle_args(pool, rotary, at):
     """(pointer, positions) of a table of angles, or of none."""
     if rotary is None:
         return None, 0
-    if rotary.dtype is not torch.float32 or rotary.dim() != 3 or tuple(rotary.shape[1:]) != (pool.head_dim // 2, 2):
+    shape = rotary.shape
+    if rotary.dtype is not torch.float32 or len(shape) != 3 or shape[1] * 2 != pool.head_dim or shape[2] != 2:
         raise IpvError(ERR_SHAPE, "rotary must be fp32 [positions, %d, 2]" % (pool.head_dim // 2))
     if rotary.get_device() != pool._dev:
         raise IpvError(ERR_ARG, "rotary is on %s, the pool on %s" % (rotary.device, pool.device))
-    return _ptr(rotary) or at, rotary.shape[0]
+    return _ptr(rotary) or at, shape[0]
+
+
+@functools.lru_cache(maxsize=256)
+def _token_strides(q, k, v, out, shape, kv):
+    """Stride arrays of q, of k and v, and of q_out."""
+    arrays = _stride_array(q, shape), _stride_array(k, kv), _stride_array(out, shape)
+    if list(_stride_array(v, kv)) != list(arrays[1]):
+        raise IpvError(ERR_SHAPE, "k and v must have the same strides")
+    _not_expanded("q_out", out, shape)
+    return arrays
 
 
 def ipv_qkv_write(pool, page_table, first_row, layer, q, k, v, q_out, ws, rows=None, q_norm=None, k_norm=None, eps=1e-6, rotary=None,
@@ -797,18 +809,14 @@ def ipv_qkv_write(pool, page_table, first_row, layer, q, k, v, q_out, ws, rows=N
     B, A, M, D = shape
     if kv != (B, pool.shape.kv_heads, M, D) or v.shape != kv:
         raise IpvError(ERR_SHAPE, "k and v must be [%d, %d, %d, %d]" % (B, pool.shape.kv_heads, M, D))
-    if k.dtype is not q.dtype or v.dtype is not q.dtype:
+    kind = q.dtype
+    if k.dtype is not kind or v.dtype is not kind:
         raise IpvError(ERR_DTYPE, "q, k and v must have one dtype")
     if q_out.shape != shape:
         raise IpvError(ERR_SHAPE, "q_out must have q's shape")
     if q_out.dtype is not pool.dtype:
         raise IpvError(ERR_DTYPE, "q_out must be %s" % pool.dtype)
-    k_strides, out_strides = k.stride(), q_out.stride()
-    q_at, k_at, out_at = _stride_array(q.stride(), shape), _stride_array(k_strides, kv), _stride_array(out_strides, shape)
-    if v.stride() != k_strides and list(_stride_array(v.stride(), kv)) != list(k_at):
-        raise IpvError(ERR_SHAPE, "k and v must have the same strides")
-    if 0 in out_strides:
-        _not_expanded("q_out", out_strides, shape)
+    q_at, k_at, out_at = _token_strides(q.stride(), k.stride(), v.stride(), q_out.stride(), shape, kv)
     if rows is None:
         rows = M
     elif (rows if isinstance(rows, int) else max(rows, default=0)) > M:
@@ -825,7 +833,8 @@ def ipv_qkv_write(pool, page_table, first_row, layer, q, k, v, q_out, ws, rows=N
     angles, positions = _angle_args(pool, rotary, at)
     bound, block_rows = _bounds_args(pool, bounds)
     rc = _paged().ipv_qkv_write(*pool._args, bound, block_rows, table, cols, B, first.buffer_info()[0], counts_.buffer_info()[0], layer,
-                                q.data_ptr() or at, q_at, A, k.data_ptr() or at, v.data_ptr() or at, k_at, _dtype_code(q),
+                                q.data_ptr() or at, q_at, A, k.data_ptr() or at, v.data_ptr() or at, k_at,
+                                BF16 if kind is torch.bfloat16 else _dtype_code(q),
                                 _float_row("q_norm", q_norm, D, pool), _float_row("k_norm", k_norm, D, pool), eps, angles, positions,
                                 q_out.data_ptr() or at, out_at, at, ws.nbytes, _stream(stream))
     if rc != OK:
