@@ -56,11 +56,8 @@ __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// A wave's list for query i: a histogram of 256 equal parts of the keys' range (of their upper words) says which part holds
-// the k-th highest; among the few keys there it is found bit by bit, until as many keys as wanted are at least the
-// bits so far. Then the keys above it and, of those equal to it, the lowest blocks'. NR: a lane's keys, in
-// registers (0: any number, read again each time); cross: other workgroups wrote scores; hist: 256 words of LDS. The next
-// query's scores are on their way meanwhile.
+// A wave's scores of one query. NR: a lane's, in registers (0: any number, read again each time); cross: other
+// workgroups wrote some of them.
 template <int NR>
 struct Scores {
   double s[NR > 0 ? NR : 1];
@@ -78,6 +75,9 @@ struct Scores {
 __device__ __forceinline__ double* scores_of(const SelectArgs& a, int b, int h, int i) {
   return a.scores + (((int64_t)b * a.H + h) * a.mq + (i - a.m0)) * a.padded;
 }
+// A wave's list for query i: a histogram of 256 equal parts of the keys' range (of their upper words) says which part holds
+// the k-th highest; among the few keys there it is found bit by bit, until as many keys as wanted are at least the
+// bits so far. Then the keys above it and, of those equal to it, the lowest blocks'. hist: 256 words of LDS.
 template <int NR>
 __device__ __forceinline__ void pick_blocks(const SelectArgs& a, const Scores<NR>& held, double* scores, int b, int h, int i, bool cross,
                                             uint32_t* hist) {

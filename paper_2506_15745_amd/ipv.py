@@ -1008,6 +1008,135 @@ def ipv_page_copy(pool, from_pages, to_pages, ws, rows=None, bounds=None, stream
         _check(rc, "ipv_page_copy")
 
 
+class PageTables:
+    """Which pages of a pool its streams have: `table` (int32 [streams, columns], on the pool's GPU, -1 where a stream has no
+    page) is what the other calls take. Streams may share pages (fork); a shared one is copied before a stream writes to it
+    (reserve). A page that goes back can be handed out again at once, so the calls that use them run on one HIP stream, these
+    methods on it as the current one, outside of captures: they write the table, whose memory stays the same."""
+
+    def __init__(self, pool: PagePool, streams: int, columns: int):
+        if streams < 1 or columns < 1:
+            raise IpvError(ERR_SHAPE, "a table of %d streams and %d columns" % (streams, columns))
+        self.pool, self.columns = pool, columns
+        self.pages = [[] for _ in range(streams)]  # of each stream, in order
+        self._users = [0] * pool.shape.pages
+        self._free = list(range(pool.shape.pages - 1, -1, -1))
+        self._table = torch.full((streams, columns), -1, dtype=torch.int32, device=pool.device)
+
+    table = property(lambda self: self._table)
+    free_pages = property(lambda self: len(self._free))
+
+    def _columns_of(self, end):
+        cols = -(-end // self.pool.shape.page_rows)
+        if cols > self.columns:
+            raise IpvError(ERR_SHAPE, "%d rows take %d pages, the table has %d columns" % (end, cols, self.columns))
+        return cols
+
+    def _stream_of(self, *streams):
+        for b in streams:
+            if not 0 <= b < len(self.pages):
+                raise IpvError(ERR_ARG, "stream %d of %d" % (b, len(self.pages)))
+
+    def _have(self, wanted):
+        if wanted > len(self._free):
+            raise IpvError(ERR_ARG, "%d pages wanted, %d are free" % (wanted, len(self._free)))
+
+    def _take(self):
+        page = self._free.pop()
+        self._users[page] = 1
+        return page
+
+    def _give_back(self, pages):
+        for page in pages:
+            self._users[page] -= 1
+            if self._users[page] == 0:
+                self._free.append(page)
+
+    def _int32(self, values):
+        return torch.tensor(values, dtype=torch.int32).to(self.pool.device)
+
+    def _publish(self):
+        self._table.copy_(torch.tensor([x + [-1] * (self.columns - len(x)) for x in self.pages], dtype=torch.int32))
+
+    def reserve(self, first_row, rows, ws, bounds=None):
+        """Pages for the rows[b] rows from first_row[b] on of every stream, and for all before them: new ones where it has none;
+        where it shares one that holds some of these rows, a copy (with bounds, if given) of its own. Without enough
+        free pages nothing changes and the call raises."""
+        streams, T = len(self.pages), self.pool.shape.page_rows
+        first, rows = _host_counts(first_row, streams, "first_row"), _host_counts(rows, streams, "rows")
+        own, missing, users = [], [0] * streams, {}  # (stream, column) of shared pages; pages behind those of a stream; users left
+        for b, pages in enumerate(self.pages):
+            if first[b] < 0 or rows[b] < 0:
+                raise IpvError(ERR_SHAPE, "negative rows")
+            if rows[b] == 0:
+                continue
+            cols = self._columns_of(first[b] + rows[b])
+            missing[b] = max(cols - len(pages), 0)
+            for c in range(first[b] // T, min(cols, len(pages))):
+                left = users.get(pages[c], self._users[pages[c]])
+                if left > 1:
+                    own.append((b, c))
+                    users[pages[c]] = left - 1
+        self._have(len(own) + sum(missing))
+        if own:
+            new = self._free[len(self._free) - len(own):][::-1]
+            ipv_page_copy(self.pool, self._int32([self.pages[b][c] for b, c in own]), self._int32(new), ws, bounds=bounds)
+            for b, c in own:
+                self._give_back([self.pages[b][c]])
+                self.pages[b][c] = self._take()
+        for b, pages in enumerate(self.pages):
+            pages.extend([self._take() for _ in range(missing[b])])
+        if own or any(missing):
+            self._publish()
+
+    def fork(self, stream, to, n_tokens):
+        """Stream `to` has the pages of the first n_tokens rows of `stream`, instead of those that it had."""
+        self._stream_of(stream, to)
+        cols = self._columns_of(n_tokens)
+        if n_tokens < 0 or cols > len(self.pages[stream]):
+            raise IpvError(ERR_SHAPE, "stream %d has no %d rows" % (stream, n_tokens))
+        shared = self.pages[stream][:cols]
+        for page in shared:
+            self._users[page] += 1
+        self._give_back(self.pages[to])
+        self.pages[to] = shared
+        self._publish()
+
+    def free(self, stream, n_tokens=0):
+        """The pages behind the first n_tokens rows of a stream go back."""
+        self._stream_of(stream)
+        if n_tokens < 0:
+            raise IpvError(ERR_SHAPE, "negative rows")
+        cols = -(-n_tokens // self.pool.shape.page_rows)
+        self._give_back(self.pages[stream][cols:])
+        del self.pages[stream][cols:]
+        self._publish()
+
+    def compact(self, streams, n_tokens, keep_idx, ws, rows=None, rotary=None, bounds=None):
+        """ipv_page_compact of these streams, keep_idx [len(streams), L, H, C], into pages of their own; those that they had go
+        back. It takes free pages for all new rows first; without enough nothing changes and the call raises."""
+        self._stream_of(*streams)
+        if len(set(streams)) != len(streams):
+            raise IpvError(ERR_ARG, "a stream is named twice")
+        if not streams:
+            return
+        counts_ = _host_counts(keep_idx.shape[-1] if rows is None else rows, len(streams), "rows")
+        if min(counts_) < 0:
+            raise IpvError(ERR_SHAPE, "negative rows")
+        cols = [self._columns_of(r) for r in counts_]
+        self._have(sum(cols))
+        had = [self.pages[b] for b in streams]
+        fresh = iter(self._free[len(self._free) - sum(cols):][::-1])
+        new = [[next(fresh) for _ in range(c)] for c in cols]
+        at = [self._int32([x + [-1] * (self.columns - len(x)) for x in pages]) for pages in (had, new)]
+        ipv_page_compact(self.pool, at[0], at[1], n_tokens, keep_idx, ws, rows=rows, rotary=rotary, bounds=bounds)
+        for b, x in zip(streams, new):
+            self.pages[b] = [self._take() for _ in x]
+        for pages in had:
+            self._give_back(pages)
+        self._publish()
+
+
 class Compressor:
     """Buffers for repeated passes over caches of one shape.
 
