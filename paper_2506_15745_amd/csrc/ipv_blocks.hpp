@@ -14,7 +14,9 @@ namespace ipv {
 typedef double F64x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------ selection
-constexpr int kSelectThreads = 256, kSelectWaves = kSelectThreads / kWave;
+// Threads of a workgroup, and waves of a SIMD at least: as many as the registers that a tile of blocks takes leave.
+constexpr int select_threads(int FB, int D, bool split) { return split || (FB == kFmtF32 && D > 128) ? 256 : 512; }
+constexpr int select_waves(int FB, int D, bool split) { return split || D * (FB == kFmtF32 ? 2 : 1) > 128 ? 1 : 4; }
 constexpr int kScoreTile = 16;  // queries, and blocks, of a product
 
 struct SelectArgs {
@@ -52,6 +54,12 @@ __device__ __forceinline__ uint64_t score_key(double s, bool candidate, bool alw
   return !candidate ? 0 : always ? ~0ull : u;
 }
 
+__device__ __forceinline__ uint64_t readlane64(uint64_t x, int lane) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane);
+  return (uint64_t)hi << 32 | lo;
+}
+
 __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
@@ -76,8 +84,9 @@ __device__ __forceinline__ double* scores_of(const SelectArgs& a, int b, int h, 
   return a.scores + (((int64_t)b * a.H + h) * a.mq + (i - a.m0)) * a.padded;
 }
 // A wave's list for query i: a histogram of 256 equal parts of the keys' range (of their upper words) says which part holds
-// the k-th highest; among the few keys there it is found bit by bit, until as many keys as wanted are at least the
-// bits so far. Then the keys above it and, of those equal to it, the lowest blocks'. hist: 256 words of LDS.
+// the k-th highest. Up to 64 keys there, a key a lane, count those above them; among more it is found bit by bit, until
+// as many keys as wanted are at least the bits so far. Then the keys above it and, of those equal to it, the lowest
+// blocks'. hist: 256 words of LDS.
 template <int NR>
 __device__ __forceinline__ void pick_blocks(const SelectArgs& a, const Scores<NR>& held, double* scores, int b, int h, int i, bool cross,
                                             uint32_t* hist) {
@@ -100,7 +109,14 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, const Scores<NR
 #pragma unroll
       for (int r = 0; r < NR; ++r) what(r, key[r]);
     } else {
-      for (int r = 0; r < turns; ++r) what(r, key_of(r, Scores<NR>::at(scores, count, r, cross)));
+      constexpr int AHEAD = 8;  // on their way at once (past the last ones: keys of 0)
+      for (int r0 = 0; r0 < turns; r0 += AHEAD) {
+        double s[AHEAD];
+#pragma unroll
+        for (int r = 0; r < AHEAD; ++r) s[r] = Scores<NR>::at(scores, count, r0 + r, cross);
+#pragma unroll
+        for (int r = 0; r < AHEAD; ++r) what(r0 + r, key_of(r0 + r, s[r]));
+      }
     }
   };
   const auto at_least = [&](uint64_t x) __attribute__((always_inline)) {
@@ -115,7 +131,7 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, const Scores<NR
   };
   uint64_t limit = 1;  // the least key that is picked
   int equal = 0;       // of those equal to it, as many (all, if `all`)
-  bool all = true;
+  bool all = true, found = false;
   const int forced = a.first_blocks + a.last_blocks;  // (of which there are as many where there are more blocks than wanted)
   if (want < count && want == forced) {
     limit = ~0ull;
@@ -146,14 +162,37 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, const Scores<NR
       // lane 0 has the four highest parts: keys of them and of all before
       const U32x4 c = bins[kWave - 1 - lane];
       const int32_t sum = (int32_t)(c[0] + c[1] + c[2] + c[3]), upto = wave_inclusive_scan(sum), rest = want - forced;
-      const int32_t a3 = upto - sum + (int32_t)c[3], a2 = a3 + (int32_t)c[2], a1 = a2 + (int32_t)c[1];
+      const int32_t before = upto - sum, a3 = before + (int32_t)c[3], a2 = a3 + (int32_t)c[2], a1 = a2 + (int32_t)c[1];
       const int part = a3 >= rest ? 3 : a2 >= rest ? 2 : a1 >= rest ? 1 : 0;
-      const int32_t reached = a3 >= rest ? a3 : a2 >= rest ? a2 : a1 >= rest ? a1 : upto;
+      const int32_t above = part == 3 ? before : part == 2 ? a3 : part == 1 ? a2 : a1;  // keys above that part, and with it
+      const int32_t reached = part == 3 ? a3 : part == 2 ? a2 : part == 1 ? a1 : upto;
       const int at = __builtin_ctzll(__ballot(upto >= rest));
       const uint32_t from = least + ((uint32_t)((kWave - 1 - at) * 4 + __builtin_amdgcn_readlane(part, at)) << shift);
       all = __builtin_amdgcn_readlane(reached, at) == rest;
       limit = (uint64_t)from << 32;
-      if (!all && shift > 0) {
+      const int32_t over = __builtin_amdgcn_readlane(above, at), inside = __builtin_amdgcn_readlane(reached, at) - over, need = rest - over;
+      if (!all && inside <= kWave) {
+        uint64_t* few = reinterpret_cast<uint64_t*>(hist);
+        int put = 0;
+        each([&](int, uint64_t y) __attribute__((always_inline)) {
+          const bool in = (y != 0) & (y != ~0ull) & (((uint32_t)(y >> 32) - from) >> shift == 0);
+          const uint64_t mask = __ballot(in);
+          if (in) few[put + lanes_below(mask)] = y;
+          put += __builtin_popcountll(mask);
+        });
+        asm volatile("" ::: "memory");
+        const uint64_t mine = lane < inside ? few[lane] : 0;
+        int higher = 0, no_less = 0;
+        for (int x = 0; x < inside; ++x) {
+          const uint64_t y = readlane64(mine, x);
+          higher += y > mine, no_less += y >= mine;
+        }
+        const int it = __builtin_ctzll(__ballot((lane < inside) & (higher < need) & (no_less >= need)));
+        limit = readlane64(mine, it);
+        equal = need - __builtin_amdgcn_readlane(higher, it);
+        all = __builtin_amdgcn_readlane(no_less, it) == need;
+        found = true;
+      } else if (!all && shift > 0) {
         range(from, (1u << shift) - 1u);
         const int top_bit = least < most ? 31 - __builtin_clz(least ^ most) : -1;
         uint32_t upper = top_bit < 0 ? least : least >> top_bit >> 1 << top_bit << 1;
@@ -166,13 +205,13 @@ __device__ __forceinline__ void pick_blocks(const SelectArgs& a, const Scores<NR
         limit = (uint64_t)upper << 32;
       }
     }
-    for (int bit = 31; bit >= 0 && !all; --bit) {
+    for (int bit = 31; bit >= 0 && !all && !found; --bit) {
       const uint64_t x = limit | 1ull << bit;
       const int n = at_least(x);
       if (n >= want) limit = x;
       all = n == want;
     }
-    if (!all) equal = want - at_least(limit + 1);
+    if (!all && !found) equal = want - at_least(limit + 1);
   }
   int pos = 0;
   each([&](int r, uint64_t y) __attribute__((always_inline)) {
@@ -330,14 +369,15 @@ __device__ __forceinline__ int select_place(int ch, int col) {
 // of blocks or, where there are few queries (SPLIT), a quarter of its steps, added up through LDS: then the way through
 // all of them is what a tile costs. The scores go to memory; the workgroup, the last one to come where several share the
 // blocks, picks from them. Bound by the 64-bit products where there are many queries (1024 tokens of 8 KV heads over 512
-// blocks 72 us, 27 of them the products at their rate), by the trips to memory for one (9 us).
+// blocks 61 to 68 us, 33 of them the products at the rate of a large one), by the trips to memory for one (9 us).
 template <int FB, int D, int NR, bool SPLIT>
-__global__ __launch_bounds__(kSelectThreads) void k_block_select(SelectArgs a) {
-  constexpr int STEPS = D / 2, PART = SPLIT ? STEPS / kSelectWaves : STEPS;  // of four terms; of a wave
+__global__ __launch_bounds__(select_threads(FB, D, SPLIT), select_waves(FB, D, SPLIT)) void k_block_select(SelectArgs a) {
+  constexpr int THREADS = select_threads(FB, D, SPLIT), SELECT_WAVES = THREADS / kWave;
+  constexpr int STEPS = D / 2, PART = SPLIT ? STEPS / SELECT_WAVES : STEPS;  // of four terms; of a wave
   constexpr int CHUNKS = PART < 8 ? 1 : PART / 8;                            // of eight steps, that a wave loads
-  constexpr int WAVES = SPLIT ? 1 : kSelectWaves;                            // tiles at a time
+  constexpr int WAVES = SPLIT ? 1 : SELECT_WAVES;                            // tiles at a time
   __shared__ double lds[STEPS * kWave];
-  __shared__ double sums[SPLIT ? 2 : 1][SPLIT ? kSelectWaves : 1][kScoreTile * kScoreTile];
+  __shared__ double sums[SPLIT ? 2 : 1][SPLIT ? SELECT_WAVES : 1][kScoreTile * kScoreTile];
   __shared__ bool lds_last;
   const int b = blockIdx.z, q_tiles = (a.mq + kScoreTile - 1) / kScoreTile;
   const int h = blockIdx.y / q_tiles, i0 = a.m0 + blockIdx.y % q_tiles * kScoreTile;
@@ -378,7 +418,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_block_select(SelectArgs a) {
     page = page_of(first + step);
   }
   // four channels of a query a thread (of the queries that there are: what is in the other columns reaches no score of these)
-  for (int x = threadIdx.x; x < (i1 - i0) * (D / 4); x += kSelectThreads) {
+  for (int x = threadIdx.x; x < (i1 - i0) * (D / 4); x += THREADS) {
     const int col = x / (D / 4), channel = x % (D / 4) * 4;
     double plus[4], minus[4];
     group_queries<FB>(a, (int64_t)(a.b0 + b) * a.q_b + (int64_t)h * a.G * a.q_h + (int64_t)(i0 + col) * a.q_m + channel, plus, minus);
@@ -389,8 +429,8 @@ __global__ __launch_bounds__(kSelectThreads) void k_block_select(SelectArgs a) {
     }
   }
   __syncthreads();
-  // the wave's operands of the queries' side in registers, where those suffice
-  constexpr bool HELD = PART <= 64;
+  // the wave's operands of the queries' side in registers, where those suffice for the waves that a CU can have then
+  constexpr bool HELD = SPLIT && PART <= 64;
   double q[HELD ? PART : 1];
   const auto operand = [&](int i) __attribute__((always_inline)) {
     const int step = (SPLIT ? wave * PART : 0) + i;
@@ -439,7 +479,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_block_select(SelectArgs a) {
       __syncthreads();
       double total = 0;
 #pragma unroll
-      for (int w = 0; w < kSelectWaves; ++w) total += sums[buf][w][threadIdx.x];
+      for (int w = 0; w < SELECT_WAVES; ++w) total += sums[buf][w][threadIdx.x];
       keep(threadIdx.x % kScoreTile, threadIdx.x / kScoreTile, total);
     } else {
 #pragma unroll
@@ -459,14 +499,16 @@ __global__ __launch_bounds__(kSelectThreads) void k_block_select(SelectArgs a) {
     __syncthreads();
     if (!lds_last) return;
   }
-  static_assert(sizeof(lds) >= kSelectWaves * 256 * sizeof(uint32_t), "a histogram a wave");
+  static_assert(sizeof(lds) >= SELECT_WAVES * 256 * sizeof(uint32_t), "a histogram a wave");
   uint32_t* hist = reinterpret_cast<uint32_t*>(lds) + wave * 256;
+  constexpr bool NEXT = NR <= 8;  // the next query's scores on their way meanwhile: more would leave room for fewer waves
   Scores<NR> later;
-  if (i0 + wave < i1) later.load(scores_of(a, b, h, i0 + wave), candidates(a, b, i0 + wave), sharing > 1);
-  for (int i = i0 + wave; i < i1; i += kSelectWaves) {
+  if (NEXT && i0 + wave < i1) later.load(scores_of(a, b, h, i0 + wave), candidates(a, b, i0 + wave), sharing > 1);
+  for (int i = i0 + wave; i < i1; i += SELECT_WAVES) {
+    if (!NEXT) later.load(scores_of(a, b, h, i), candidates(a, b, i), sharing > 1);
     const Scores<NR> scores = later;
-    const int then = i + kSelectWaves;
-    if (then < i1) later.load(scores_of(a, b, h, then), candidates(a, b, then), sharing > 1);
+    const int then = i + SELECT_WAVES;
+    if (NEXT && then < i1) later.load(scores_of(a, b, h, then), candidates(a, b, then), sharing > 1);
     pick_blocks<NR>(a, scores, scores_of(a, b, h, i), b, h, i, sharing > 1, hist);
   }
 }
@@ -560,11 +602,7 @@ struct Runs {
     const uint64_t m = __ballot(seen > 0);
     some = (m | m >> 1) & 0x5555555555555555ull;
   }
-  __device__ __forceinline__ int64_t row_at(int lane_) const {
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)row, lane_);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)row >> 32), lane_);
-    return (int64_t)((uint64_t)hi << 32 | lo);
-  }
+  __device__ __forceinline__ int64_t row_at(int lane_) const { return (int64_t)readlane64((uint64_t)row, lane_); }
   __device__ __forceinline__ int32_t seen_at(int lane_) const { return __builtin_amdgcn_readlane(seen, lane_); }
 };
 

@@ -14,12 +14,19 @@ using namespace ipv;
 namespace {
 
 constexpr int32_t kMaxTop = 4096;
-// Whether each query of a launch has a workgroup of its own: for up to 2048 blocks (its scores are in LDS), unless
-// there are so many scores that the matrix unit is faster, or so few queries that sharing one's blocks out is. One token over 512
-// blocks of 128: 8 of them (a stream of 8 KV heads) 12.8 us so and 8.7 shared out, 32 13.2 and 13.2, 64 14.9 and 16.9; 128 and
-// 784 of them over 98 blocks 8.4 and 18, 21 and 22; 8192 over 512 about 100 and 72.
-bool select_alone(int64_t queries, int32_t padded) {
-  return padded <= 32 * kWave && queries * padded <= 1 << 20 && (padded <= 256 || queries >= 32);
+// Whether each query of a launch has a workgroup of its own: for up to 2048 blocks (its scores are in LDS), where the
+// times that the two ways take, as they were measured, say so. A workgroup: what it takes for all blocks, or what all
+// workgroups take on the card, by the bounds' bytes. Tiles of 16 queries: what they take at least, and the matrix
+// unit's time, by the tiles. E. g. us alone and in tiles, 8 KV heads of 128 in bf16: 16 tokens over 64 blocks 7.0
+// and 15, over 512 14 and 18; 64 over 256 16 and 20, over 512 23 and 23; 128 over 64 15 and 15, over 256 27 and 22; 512
+// over 64 50 and 14, over 512 142 and 36; one token of 64 streams over 256 22 and 32, of one over 512 13 and 9. Heads
+// of 256: 64 over 64 13 and 19, 512 over 256 151 and 36; of 32: 256 over 256 18 and 21, 512 over 64 19 and 12.
+bool select_alone(int64_t queries, int32_t of_stream, int32_t units, int32_t padded, int32_t D, int32_t block_bytes) {
+  if (padded > 32 * kWave) return false;
+  const double bytes = block_bytes, blocks = padded, all = (double)queries * bytes;
+  const double alone = std::max(6000.0 + blocks * bytes / 32, 3000.0 + all * (155 + blocks) * 1e-4);  // ns
+  const double tiles = 10000.0 + (units < 256 ? 300 * std::min(of_stream, kScoreTile) : 1000) + (double)units * blocks * D / 850;
+  return alone < tiles;
 }
 constexpr int64_t kScoreBytes = 128ll << 20;  // of scores at a time, where 16 queries of each stream need no more
 
@@ -67,7 +74,7 @@ struct Select {
 
 template <int FB, int D, bool SPLIT>
 void launch_select_n(dim3 grid, const SelectArgs& a, hipStream_t st) {
-  const dim3 block(kSelectThreads);
+  const dim3 block(select_threads(FB, D, SPLIT));
   if (a.padded <= 8 * kWave) k_block_select<FB, D, 8, SPLIT><<<grid, block, 0, st>>>(a);
   else if (a.padded <= 32 * kWave) k_block_select<FB, D, 32, SPLIT><<<grid, block, 0, st>>>(a);
   else k_block_select<FB, D, 0, SPLIT><<<grid, block, 0, st>>>(a);
@@ -121,9 +128,10 @@ ipv_status select_blocks(Select* s, const Counts& c, hipStream_t st) {
     for (a.m0 = 0; a.m0 < most; a.m0 += step) {
       a.mq = std::min(step, most - a.m0);
       const int32_t y = a.H * ((a.mq + kScoreTile - 1) / kScoreTile);
-      // several workgroups share the blocks where tiles of queries alone leave the card empty
-      const int32_t units = y * nb, x = units >= 256 ? 1 : std::max(1, std::min(a.padded / kScoreTile, 512 / units));
-      if (select_alone((int64_t)nb * a.H * a.mq, a.padded)) {
+      // several workgroups share the blocks where tiles of queries alone leave the card empty: two a CU, if LDS takes them
+      const int32_t D = s->pool->head_dim, most_wg = D <= 128 ? 512 : 256;
+      const int32_t units = y * nb, x = units >= 256 ? 1 : std::max(1, std::min(a.padded / kScoreTile, most_wg / units));
+      if (select_alone((int64_t)nb * a.H * a.mq, a.mq, units, a.padded, D, 2 * D * (s->pool->format == IPV_PAGES_F32 ? 4 : 2))) {
         launch_one(s->pool, dim3((uint32_t)a.mq, (uint32_t)a.H, (uint32_t)nb), a, st);
         IPV_TRY(launched(hipGetLastError()));
         continue;

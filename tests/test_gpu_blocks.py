@@ -124,6 +124,38 @@ def test_many_blocks(top, first, last, n):
     check("bf16", pool, table, [n], [n - 3], 0, queries("bf16", 1, 2, 3, D, n), made_bounds(pool, "bf16", table, [n], 16), top, first, last)
 
 
+@pytest.mark.parametrize("fmt,D", [("bf16", 32), ("bf16", 128), ("bf16", 256), ("f32", 64), ("f32", 128), ("f32", 256)])
+@pytest.mark.parametrize("blocks", [100, 600, 1100, 2100])
+@pytest.mark.parametrize("crowd", [False, True])
+def test_many_queries(fmt, D, blocks, crowd):
+    """Tiles of queries without workgroups that share their blocks; scores all over their range, or one far above the others,
+    which are then next to each other in it. (Random scores: none are equal, and 64 bits in any order rank them alike.)"""
+    B, H, G, m, top = 1, 8, 2, 512, 9
+    n = blocks * 16 - 5
+    pool, table = R.filled_pool(fmt, -(-n // 64), 1, H, 64, D, 3), R.shuffled_table(1, -(-n // 64), -(-n // 64), 4)
+    bounds, g = ipv.BlockBounds(pool, 16), torch.Generator(device="cuda").manual_seed(blocks)
+    bounds.values.copy_(torch.randn(bounds.values.shape, generator=g, device="cuda"))
+    if crowd:
+        for h in range(H):
+            X.bounds_at(bounds, table, 0, 0, h, 7).mul_(2.0**60)
+    q = queries(fmt, B, H * G, m, D, 9)
+    print("many queries", fmt, D, blocks, crowd, flush=True)
+    ws = ipv.alloc_blocks_workspace(bounds, B, H * G, m, top, n)
+    got = torch.full((B, H, m, top), 777, dtype=torch.int32, device="cuda")
+    ipv.ipv_block_select(pool, table, bounds, n, n - m, 0, q, got, ws, first_blocks=1, last_blocks=2)
+    torch.cuda.synchronize()
+    assert ipv.ipv_read_device_errors(ws) == 0
+    count = (torch.arange(n - m, n, device="cuda") + 16) // 16
+    j = torch.arange(blocks, device="cuda")
+    for h in range(H):
+        at = torch.stack([X.bounds_at(bounds, table, 0, 0, h, x) for x in range(blocks)]).double()  # [blocks, 2, D]
+        qs = q[0, h * G:(h + 1) * G].double()
+        score = qs.clamp_min(0).sum(0) @ at[:, 1].T + qs.clamp_max(0).sum(0) @ at[:, 0].T
+        forced = (j < 1) | (j >= count[:, None] - 2)
+        score = torch.where(j >= count[:, None], -math.inf, torch.where(forced, math.inf, score))
+        assert torch.equal(got[0, h].long(), score.topk(top, -1).indices.sort(-1).values)
+
+
 @pytest.mark.parametrize("fmt", ("bf16", "f32"))
 def test_equal_scores_go_to_the_lower_block(fmt):
     """Blocks that are copies of a few: ties everywhere, also at the end of what is picked."""
