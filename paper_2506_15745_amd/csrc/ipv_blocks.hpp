@@ -606,8 +606,9 @@ struct Runs {
   __device__ __forceinline__ int32_t seen_at(int lane_) const { return __builtin_amdgcn_readlane(seen, lane_); }
 };
 
-// Workgroups of a CU, by the registers that they take.
+// Workgroups of a CU, by the registers and the LDS that they take.
 constexpr int blocks_per_cu(int F, int D, int NB) {
+  if (F == kFmtF32) return D <= 64 ? 3 : D <= 128 ? 2 : 1;
   return NB * D <= 64 || (fmt_scaled(F) && NB * D <= 128) ? 3 : NB * D <= 128 || (fmt_scaled(F) && D <= 128) ? 2 : 1;
 }
 
@@ -844,128 +845,184 @@ __global__ __launch_bounds__(64 * kFewWaves, blocks_per_cu(F, D, NB)) void k_att
   if constexpr (!SOLO) join_parts<D, 16 * NB, false>(a, st, pl, b, pl.token * a.G + pl.tile * 16 * NB, heads, lds, lds_ml, &lds_last);
 }
 
-// As k_attend_f32: fp32 pools, up to 32 query heads of a token.
-template <int D>
-__global__ __launch_bounds__(64 * kFewWaves, D <= 64 ? 2 : 1) void k_attend_blocks_f32(BlocksArgs a) {
-  __shared__ __attribute__((aligned(16))) char lds[kFewWaves][JoinLds<D, 32>::kWaveBytes];
-  __shared__ float lds_ml[kFewWaves][32][2];
-  __shared__ uint32_t lds_last;
-  const int lane = threadIdx.x % kWave, h = lane / 32, l32 = lane % 32;
+// fp32 pools: as k_attend_blocks, up to 16 query heads of a token, with the fp32 matrix instruction. Keys go through LDS as
+// there; values straight into the product's operand, where 16 lanes have a key's 64 (32) channels: it is its channels
+// that a lane has four of side by side, so that sum 4 j + e has channels 64 j + 4 r + e in its rows r. Tiles of 16 rows, since
+// a token has few: 512 tokens of 64 heads of 128 over 16 blocks of 64 take 383 us (90 TFLOP/s of half filled tiles), with the
+// 32-row instruction and keys straight into its operand 724; one token of four streams over 2048 rows 20 and 23. Bound by
+// the matrix instruction, single tokens by the way to the rows.
+template <int D, bool SOLO>
+__global__ __launch_bounds__(64 * kFewWaves, blocks_per_cu(kFmtF32, D, 1)) void k_attend_blocks_f32(BlocksArgs a) {
+  constexpr size_t RB = D * 4, KTILE = kFewKeys * RB, JOIN = JoinLds<D, 16>::kWaveBytes;
+  constexpr int NP = (int)(KTILE / 1024), RP = 1024 / RB;  // loads of a tile's keys; rows of one
+  constexpr int VE = D >= 64 ? 4 : 1, VN = D / 16 / VE;    // channels side by side; of these, a lane's of a key
+  constexpr int SUMS = D <= 32 ? 1 : D <= 64 ? 2 : 4;      // of a score: with one, heads of 256 are off by 1.4e-6 of their norm, so by 5.4e-7
+  __shared__ __attribute__((aligned(16))) char lds[kFewWaves][SOLO || JOIN < KTILE ? KTILE : JOIN];
+  const int lane = threadIdx.x % kWave, g = lane / 16, l16 = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const BlockPlace pl = block_place<false>(a, wave);
-  if (pl.slot < 0) return;
+  const BlockPlace pl = block_place<SOLO>(a, wave);
+  if (pl.slot < 0) return;  // the whole workgroup, or a wave that no other waits for
   const int b = a.b0 + pl.b;
   const int64_t head_row = a.layer_row + (int64_t)pl.h * a.pool.T.d;
   const int32_t held = min(a.s[pl.b].n, a.s[pl.b].first + pl.token + 1);
   const int32_t* list = a.blocks + (((int64_t)b * a.H + pl.h) * a.max_rows + pl.token) * a.top;
-  const int32_t count = (int32_t)(((int64_t)a.entries * a.halves.d + 1) / 2);
+  const int32_t count = (int32_t)(((int64_t)a.entries * a.halves.d + 1) / 2);  // key tiles of the list
   const int32_t t_end = (int32_t)((int64_t)count * (pl.split + 1) / a.splits);
-  const int32_t t_begin = (int32_t)((int64_t)count * pl.split / a.splits) + wave;
-  const int heads = min(a.G - pl.tile * 32, 32);
-  float q[D / 2];
-  const char* qa = a.q + 4 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + pl.tile * 32 + min(l32, heads - 1)) * a.q_h +
-                              (int64_t)pl.token * a.q_m + 4 * h);
+  const int32_t t_begin = (int32_t)((int64_t)count * pl.split / a.splits) + (SOLO ? 0 : wave);
+  constexpr int STEP = SOLO ? 1 : kFewWaves;
+  const int heads = min(a.G - pl.tile * 16, 16);
+
+  F32x4 q[D / 16];
+  const char* qa = a.q + 4 * ((int64_t)b * a.q_b + (int64_t)(pl.h * a.G + pl.tile * 16 + min(l16, heads - 1)) * a.q_h +
+                              (int64_t)pl.token * a.q_m + 4 * g);
 #pragma unroll
-  for (int k = 0; k < D / 2; k += 4) {
-    const F32x4 v = *reinterpret_cast<const F32x4*>(qa + 8 * k);
-    q[k] = v.x, q[k + 1] = v.y, q[k + 2] = v.z, q[k + 3] = v.w;
-  }
-  F32x16 o[D / 32];
+  for (int c = 0; c < D / 16; ++c) q[c] = *reinterpret_cast<const F32x4*>(qa + 64 * c);
+  F32x4 o[D / 16];
   float m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) o[i] = F32x16{};
+  for (int i = 0; i < D / 16; ++i) o[i] = F32x4{0.f, 0.f, 0.f, 0.f};
+
+  typedef float Channels __attribute__((ext_vector_type(VE)));
+  struct Rows {
+    F32x4 k[NP];
+    Channels v[8][VN];  // of keys 4 g + i and 16 + 4 g + i
+    int32_t seen0, seen1;
+  };
+  char* tile = lds[wave];
+  const auto swz = [](int row) __attribute__((always_inline)) { return row & 7; };  // rows that lanes read together: other banks
   bool bad = false;
-  constexpr int KA = D <= 128 ? D / 8 : 8;  // pieces of a K row in registers
-  F32x4 kx[KA];
-  constexpr int VA = D <= 128 ? 16 : 4;  // keys of V
-  float vx[VA][D / 32];
-  for (int32_t t0 = t_begin; t0 < t_end; t0 += 32 * kFewWaves) {
+  const auto fetch_k = [&](Rows& x, int64_t r0, int64_t r1) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int64_t row = i * RP < 16 ? r0 + i * RP : r1 + (i * RP - 16);
+      x.k[i] = *reinterpret_cast<const F32x4*>(a.pool.K + row * (int64_t)RB + (uint32_t)(lane * 16));
+    }
+  };
+  const auto fetch_v = [&](Rows& x, int64_t r0, int64_t r1) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const char* at = a.pool.V + (i < 4 ? r0 + i : r1 + (i - 4)) * (int64_t)RB + (uint32_t)(4 * g * (int)RB + l16 * VE * 4);
+#pragma unroll
+      for (int j = 0; j < VN; ++j) x.v[i][j] = *reinterpret_cast<const Channels*>(at + j * 64 * VE);
+    }
+  };
+  // a tile's scores, weights and sums; the next one's rows set out as soon as their places are free
+  const auto use = [&](Rows& x, bool more, int64_t n0, int64_t n1) __attribute__((always_inline)) {
+    const int32_t seen0 = x.seen0, seen1 = x.seen1;
+    const bool full = (seen0 == 16) & (seen1 == 16);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int y = i * kWave + lane, key = y / (D / 4), col = y % (D / 4);
+      *reinterpret_cast<F32x4*>(tile + key * (int)RB + 16 * (col ^ swz(key))) = x.k[i];
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (more) fetch_k(x, n0, n1);
+    F32x4 sc[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      F32x4 sums[SUMS];
+#pragma unroll
+      for (int i = 0; i < SUMS; ++i) sums[i] = F32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        const F32x4 k = *reinterpret_cast<const F32x4*>(tile + (kb * 16 + l16) * (int)RB + 16 * ((c * 4 + g) ^ swz(l16)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[i % SUMS] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i], q[c][i], sums[i % SUMS], 0, 0, 0);
+      }
+      sc[kb] = sums[0];
+      if constexpr (SUMS == 2) sc[kb] += sums[1];
+      if constexpr (SUMS == 4) sc[kb] = (sc[kb] + sums[1]) + (sums[2] + sums[3]);
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (!full) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (4 * g + i >= seen0) sc[0][i] = -INFINITY;
+        if (4 * g + i >= seen1) sc[1][i] = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < VN; ++j) {  // values of rows that are not seen as zeros
+          if (4 * g + i >= seen0) x.v[i][j] = (Channels)(0.f);
+          if (4 * g + i >= seen1) x.v[4 + i][j] = (Channels)(0.f);
+        }
+      }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, sc[0][i]), sc[1][i]);
+    top = lanes_max<4>(top) * a.c;
+    if (__ballot(top > m) != 0) {
+      rare();
+      top = fmaxf(top, m);
+      const float old = exp2_hw(m - shift_of(top));
+      m = top;
+      l *= old;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) o[i] *= old;
+    }
+    const float shift = shift_of(m);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float e = exp2_hw(__builtin_fmaf(sc[i / 4][i % 4], a.c, -shift));
+      l += e;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) {
+        float v;
+        if constexpr (VE == 1) v = x.v[i][db][0];
+        else v = x.v[i][db / VE][db % VE];
+        o[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, e, o[db], 0, 0, 0);
+      }
+    }
+    if (more) fetch_v(x, n0, n1);
+  };
+  // what a lane has of the result: four channels from `d` on
+  const auto each_part = [&](auto&& what) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) {
+      if constexpr (VE == 1) what(16 * x + 4 * g, o[x]);
+      else what(64 * (x / 4) + 16 * g + 4 * (x % 4),
+                F32x4{o[x / 4 * 4][x % 4], o[x / 4 * 4 + 1][x % 4], o[x / 4 * 4 + 2][x % 4], o[x / 4 * 4 + 3][x % 4]});
+    }
+  };
+  for (int32_t t0 = t_begin; t0 < t_end; t0 += 32 * STEP) {
     Runs runs;
-    runs.look_up(a, list, b, head_row, held, t0, kFewWaves, t_end, bad);
-    for (uint64_t todo = runs.some; todo != 0; todo &= todo - 1) {
-      const int at = __builtin_ctzll(todo);
-      const int64_t r0 = runs.row_at(at), r1 = runs.row_at(at + 1);
-      const int32_t seen0 = runs.seen_at(at), seen1 = runs.seen_at(at + 1);
-      const bool full = (seen0 == 16) & (seen1 == 16);
-      const float* kp = reinterpret_cast<const float*>(a.pool.K) + ((l32 < 16 ? r0 : r1) + l32 % 16) * D + 4 * h;
-      const auto load_k = [&](int k) __attribute__((always_inline)) { kx[k % KA] = *reinterpret_cast<const F32x4*>(kp + 8 * k); };
-      const auto load_v = [&](int i) __attribute__((always_inline)) {
-        const int key = 8 * (i / 4) + i % 4;  // (+ 4 h)
-        const float* p = reinterpret_cast<const float*>(a.pool.V) + (i < 8 ? r0 + key : r1 + (key - 16)) * D;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) vx[i % VA][db] = p[32 * db + (uint32_t)(4 * h * D + l32)];
-      };
-#pragma unroll
-      for (int k = 0; k < KA; ++k) load_k(k);
-#pragma unroll
-      for (int i = 0; i < VA; ++i) load_v(i);
-      F32x16 s = {};
-#pragma unroll
-      for (int k = 0; k < D / 8; ++k) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kx[k % KA][i], q[4 * k + i], s, 0, 0, 0);
-        if (k + KA < D / 8) load_k(k + KA);
-      }
-      if (!full) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if ((8 * (i / 4) + i % 4) % 16 + 4 * h >= (i < 8 ? seen0 : seen1)) s[i] = -INFINITY;
-      }
-      float top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
-      top = lanes_max<2>(top) * a.c;
-      if (__ballot(top > m + kLazy) != 0) {
-        rare();
-        top = fmaxf(top, m);
-        const float old = exp2_hw(m - shift_of(top));
-        m = top;
-        l *= old;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          if constexpr (D > 64) in_acc(o[i]);
-          o[i] *= old;
-          if constexpr (D > 64) in_acc(o[i]);
-        }
-      }
-      const float shift = shift_of(m);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = exp2_hw(__builtin_fmaf(s[i], a.c, -shift));
-        l += e;
-        float(&v)[D / 32] = vx[i % VA];
-        if (!full) {
-          const bool some = (8 * (i / 4) + i % 4) % 16 + 4 * h < (i < 8 ? seen0 : seen1);
-#pragma unroll
-          for (int db = 0; db < D / 32; ++db)
-            if (!some) v[db] = 0.f;
-        }
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[db], e, o[db], 0, 0, 0);
-        if (i + VA < 16) load_v(i + VA);
-      }
+    runs.look_up(a, list, b, head_row, held, t0, STEP, t_end, bad);
+    uint64_t todo = runs.some;
+    if (todo == 0) continue;
+    Rows x;
+    int at = __builtin_ctzll(todo);
+    fetch_k(x, runs.row_at(at), runs.row_at(at + 1));
+    fetch_v(x, runs.row_at(at), runs.row_at(at + 1));
+    while (todo != 0) {
+      x.seen0 = runs.seen_at(at), x.seen1 = runs.seen_at(at + 1);
+      todo &= todo - 1;
+      at = todo != 0 ? __builtin_ctzll(todo) : 0;
+      use(x, todo != 0, runs.row_at(at), runs.row_at(at + 1));
     }
   }
   if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, kDevBadPage);
 
-  l = lanes_sum<2>(l);
-  if (h == 0) lds_ml[wave][l32][0] = m, lds_ml[wave][l32][1] = l;
+  l = lanes_sum<4>(l);
+  if constexpr (SOLO) {
+    if (l16 < heads)
+      each_part([&](int d, const F32x4& v) __attribute__((always_inline)) {
+        row_out<D, true>(a, b, pl.h, pl.token * a.G + pl.tile * 16 + l16, d, v, m, l);
+      });
+    return;
+  }
+  __shared__ float lds_ml[kFewWaves][16][2];
+  __shared__ uint32_t lds_last;
+  if (lane < 16) lds_ml[wave][lane][0] = m, lds_ml[wave][lane][1] = l;
   __syncthreads();
   float top = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, lds_ml[w][l32][0]);
+  for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, lds_ml[w][l16][0]);
   const float f = exp2_hw(m - shift_of(top));
-  float* mine = reinterpret_cast<float*>(lds[wave]) + l32 * JoinLds<D, 32>::STRIDE;
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<F32x4*>(mine + 32 * db + 8 * i + 4 * h) =
-          F32x4{o[db][4 * i] * f, o[db][4 * i + 1] * f, o[db][4 * i + 2] * f, o[db][4 * i + 3] * f};
+  float* mine = reinterpret_cast<float*>(lds[wave]) + l16 * JoinLds<D, 16>::STRIDE;
+  each_part([&](int d, const F32x4& v) __attribute__((always_inline)) { *reinterpret_cast<F32x4*>(mine + d) = v * f; });
   __syncthreads();
   AttendStream st;
   st.splits = a.splits;
-  join_parts<D, 32, true>(a, st, pl, b, pl.token * a.G + pl.tile * 32, heads, lds, lds_ml, &lds_last);
+  if constexpr (!SOLO) join_parts<D, 16, true>(a, st, pl, b, pl.token * a.G + pl.tile * 16, heads, lds, lds_ml, &lds_last);
 }
 
 // What a format's translation unit offers.

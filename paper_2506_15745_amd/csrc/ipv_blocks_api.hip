@@ -47,7 +47,7 @@ ipv_status check_lists(const ipv_page_shape* s, int32_t block_rows, int32_t top,
 }
 
 // Query heads of a workgroup.
-int32_t block_heads(const ipv_page_shape* s, int32_t G) { return s->format == IPV_PAGES_F32 || G > 16 ? 32 : 16; }
+int32_t block_heads(const ipv_page_shape* s, int32_t G) { return s->format != IPV_PAGES_F32 && G > 16 ? 32 : 16; }
 
 struct Counts {
   int32_t streams, cols;
@@ -178,8 +178,7 @@ ipv_status prepare_select(const ipv_page_shape* pool, const Pool& p, const Block
 
 // Workgroups that the card holds at once: with fewer queries than that, lists are split.
 int32_t blocks_fill(const ipv_page_shape* s, int32_t G) {
-  const int D = s->head_dim;
-  return 256 * (s->format == IPV_PAGES_F32 ? (D <= 64 ? 2 : 1) : blocks_per_cu(s->format, D, block_heads(s, G) / 16));
+  return 256 * blocks_per_cu(s->format, s->head_dim, block_heads(s, G) / 16);
 }
 
 size_t part_bytes(const ipv_page_shape* s, int32_t G, int64_t parts) {
@@ -323,7 +322,7 @@ ipv_status ipv_attend_blocks(const ipv_page_shape* pool, const void* K_pages, co
     hipError_t e;
     switch (pool->format) {
       case IPV_PAGES_BF16: e = launch_attend_blocks<kFmtBf16>(pool->head_dim, BM == 32, solo, a, st); break;
-      case IPV_PAGES_F32: e = launch_attend_blocks<kFmtF32>(pool->head_dim, true, false, a, st); break;
+      case IPV_PAGES_F32: e = launch_attend_blocks<kFmtF32>(pool->head_dim, false, solo, a, st); break;
       case IPV_PAGES_FP8: e = launch_attend_blocks<kFmtFp8>(pool->head_dim, BM == 32, solo, a, st); break;
       default: e = launch_attend_blocks<kFmtFp4>(pool->head_dim, BM == 32, solo, a, st); break;
     }
