@@ -176,6 +176,18 @@ ipv_status prepare_select(const ipv_page_shape* pool, const Pool& p, const Block
   return IPV_OK;
 }
 
+// Whether a query is one wave's, not a workgroup's: by the rounds that either makes on the card, in the times of a key
+// tile; a round's start and end take 2.5 of them, and a wave with fewer others beside it takes less time a tile. us by
+// waves and by workgroups, 64 heads of 128 in bf16, 4, 16 and 64 blocks of 64: 512 queries 14 and 10, 35 and 20, 115 and 56;
+// 1024 14 and 16, 37 and 35, 120 and 105; 2048 19 and 27, 55 and 63, 200 and 210; 8192 59 and 91, 192 and 224, 698 and 744.
+bool wave_a_query(int64_t queries, int32_t fill, int64_t count) {
+  constexpr int SIMDS = 1024;
+  const double waves = std::ceil((double)queries / SIMDS) / ((double)fill * kFewWaves / SIMDS);  // of a SIMD, of those that it can hold
+  const double alone = waves <= 1 ? 2.5 + count * (0.2 + 0.8 * waves) : (double)queries / (fill * kFewWaves) * (2.5 + count);
+  const double shared = std::max(1.0, (double)queries / fill) * (2.5 + std::ceil((double)count / kFewWaves));
+  return alone < shared;
+}
+
 // Workgroups that the card holds at once: with fewer queries than that, lists are split.
 int32_t blocks_fill(const ipv_page_shape* s, int32_t G) {
   return 256 * blocks_per_cu(s->format, s->head_dim, block_heads(s, G) / 16);
@@ -307,7 +319,7 @@ ipv_status ipv_attend_blocks(const ipv_page_shape* pool, const void* K_pages, co
     if (queries < fill && count > kFewWaves) {
       int64_t per = std::max<int64_t>({(count * queries + fill - 1) / fill, kFewWaves, (int64_t)std::sqrt(0.6 * (double)count)});
       per = (per + kFewWaves - 1) / kFewWaves * kFewWaves;
-      a.splits = (int32_t)std::min<int64_t>({(count + per - 1) / per, kMaxSplits, std::max<int64_t>(kMaxParts / queries, 1)});
+      a.splits = (int32_t)std::min<int64_t>({(count + per - 1) / per, kMaxSplits, fill / queries});
     }
     a.by_splits = make_fastdiv((uint32_t)a.splits);
     int64_t at = 0;
@@ -317,8 +329,7 @@ ipv_status ipv_attend_blocks(const ipv_page_shape* pool, const void* K_pages, co
     }
     a.slots = (int32_t)at;
     a.part = a.part_ml + (size_t)a.slots * BM * 2;  // (a launch that splits has at most kMaxParts)
-    // a wave a query where that fills the card
-    const bool solo = queries >= (int64_t)fill * kFewWaves;
+    const bool solo = a.splits == 1 && wave_a_query(queries, fill, count);
     hipError_t e;
     switch (pool->format) {
       case IPV_PAGES_BF16: e = launch_attend_blocks<kFmtBf16>(pool->head_dim, BM == 32, solo, a, st); break;
