@@ -736,6 +736,16 @@ def ipv_attend(pool, page_table, n_tokens, q_first, layer, q, out, ws, q_rows=No
         _check(rc, "ipv_attend")
 
 
+def _pool_stream(pool, stream):
+    """The stream (the current one if None), which must be the pool's GPU's, that GPU being the current one."""
+    if not torch.cuda.is_initialized():
+        return _stream(stream)
+    device = torch._C._cuda_getDevice()
+    if device != pool._dev or (stream is not None and stream.device.index != device):
+        raise IpvError(ERR_ARG, "the pool is on %s, the current device is %d, the stream %s" % (pool.device, device, stream))
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
 class BlockBounds:
     """Bounds of the keys of every block of `block_rows` rows of a pool's pages (a multiple of
     16 that divides their rows): values [P, L, H, T / block_rows, 2, D] in the pool's dtype, each
@@ -836,7 +846,7 @@ def ipv_qkv_write(pool, page_table, first_row, layer, q, k, v, q_out, ws, rows=N
                                 q.data_ptr() or at, q_at, A, k.data_ptr() or at, v.data_ptr() or at, k_at,
                                 BF16 if kind is torch.bfloat16 else _dtype_code(q),
                                 _float_row("q_norm", q_norm, D, pool), _float_row("k_norm", k_norm, D, pool), eps, angles, positions,
-                                q_out.data_ptr() or at, out_at, at, ws.nbytes, _stream(stream))
+                                q_out.data_ptr() or at, out_at, at, ws.nbytes, _pool_stream(pool, stream))
     if rc != OK:
         _check(rc, "ipv_qkv_write")
 
@@ -859,7 +869,7 @@ def ipv_block_bounds(pool, page_table, first_row, rows, bounds, ws, first_layer=
     bound, block_rows = _bounds_args(pool, bounds)
     _check(_paged().ipv_block_bounds(pool._args[0], pool._args[1], pool._args[3], bound, block_rows, table, cols, B,
                                      first.buffer_info()[0], counts_.buffer_info()[0], first_layer, layers, _ptr(ws), ws.nbytes,
-                                     _stream(stream)), "ipv_block_bounds")
+                                     _pool_stream(pool, stream)), "ipv_block_bounds")
 
 
 def blocks_workspace_bytes(pool: PagePool, block_rows: int, streams: int, q_heads: int, max_rows: int, top: int, max_tokens: int) -> int:
@@ -915,7 +925,7 @@ def ipv_block_select(pool, page_table, bounds, n_tokens, q_first, layer, q, bloc
     at = _ptr(ws)
     _check(_paged().ipv_block_select(pool._args[0], bound, block_rows, table, cols, B, n.buffer_info()[0], first.buffer_info()[0],
                                      rows.buffer_info()[0], layer, q.data_ptr() or at, _stride_array(q.stride(), shape), A, M or 1,
-                                     first_blocks, last_blocks, top, listed or at, at, ws.nbytes, _stream(stream)), "ipv_block_select")
+                                     first_blocks, last_blocks, top, listed or at, at, ws.nbytes, _pool_stream(pool, stream)), "ipv_block_select")
 
 
 def ipv_attend_blocks(pool, page_table, n_tokens, q_first, layer, q, blocks, out, ws, bounds=None, block_rows=None, q_rows=None,
@@ -960,7 +970,7 @@ def ipv_attend_blocks(pool, page_table, n_tokens, q_first, layer, q, blocks, out
                                     rows.buffer_info()[0], layer, q.data_ptr() or at, q_at, A, M or 1,
                                     D ** -0.5 if scale is None else scale, first_blocks, last_blocks, top, listed or at,
                                     out.data_ptr() or at, q_at if out_strides == q_strides else _stride_array(out_strides, shape),
-                                    None if lse is None else _ptr(lse) or at, at, ws.nbytes, _stream(stream))
+                                    None if lse is None else _ptr(lse) or at, at, ws.nbytes, _pool_stream(pool, stream))
     if rc != OK:
         _check(rc, "ipv_attend_blocks")
 
@@ -985,7 +995,7 @@ def ipv_page_compact(pool, page_table, new_table, n_tokens, keep_idx, ws, rows=N
     angles, positions = _angle_args(pool, rotary, at)
     bound, block_rows = _bounds_args(pool, bounds)
     rc = _paged().ipv_page_compact(*pool._args, bound, block_rows, table, cols, new, new_cols, B, n.buffer_info()[0], _ptr(keep_idx) or at,
-                                   C, counts_.buffer_info()[0], angles, positions, at, ws.nbytes, _stream(stream))
+                                   C, counts_.buffer_info()[0], angles, positions, at, ws.nbytes, _pool_stream(pool, stream))
     if rc != OK:
         _check(rc, "ipv_page_compact")
 
@@ -1003,7 +1013,7 @@ def ipv_page_copy(pool, from_pages, to_pages, ws, rows=None, bounds=None, stream
     at = _ptr(ws)
     bound, block_rows = _bounds_args(pool, bounds)
     rc = _paged().ipv_page_copy(*pool._args, bound, block_rows, _ptr(from_pages) or at, _ptr(to_pages) or at, from_pages.shape[0], rows,
-                                at, ws.nbytes, _stream(stream))
+                                at, ws.nbytes, _pool_stream(pool, stream))
     if rc != OK:
         _check(rc, "ipv_page_copy")
 

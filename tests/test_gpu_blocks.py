@@ -124,6 +124,16 @@ def test_many_blocks(top, first, last, n):
     check("bf16", pool, table, [n], [n - 3], 0, queries("bf16", 1, 2, 3, D, n), made_bounds(pool, "bf16", table, [n], 16), top, first, last)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D,G", [(64, 3), (128, 20)])
+def test_a_wave_a_query(fmt, D, G):
+    """So many queries that each is one wave's, over lists of ten key tiles, the last ones cut by the query's position."""
+    B, H, M, n = 2, 8, 100, [700, 395]
+    pool, table = R.filled_pool(fmt, 24, 1, H, 64, D, 2), R.shuffled_table(B, 11, 24, 3)
+    check(fmt, pool, table, n, [x - M for x in n], 0, queries(fmt, B, H * G, M, D, 8, token_major=True), made_bounds(pool, fmt, table, n, 16), 20,
+          1, 3)
+
+
 @pytest.mark.parametrize("fmt,D", [("bf16", 32), ("bf16", 128), ("bf16", 256), ("f32", 64), ("f32", 128), ("f32", 256)])
 @pytest.mark.parametrize("blocks", [100, 600, 1100, 2100])
 @pytest.mark.parametrize("crowd", [False, True])

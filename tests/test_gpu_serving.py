@@ -238,6 +238,35 @@ def test_on_another_stream(fmt):
             assert torch.equal(t.view(torch.uint8), x.view(torch.uint8))
 
 
+def test_another_current_device_is_refused(monkeypatch):
+    """Kernels go to the current device: with another one than the pool's nothing is launched."""
+    run, state, _ = sequence("bf16", 2, 1)
+    before = [t.clone() for t in state]
+    torch.cuda.synchronize()
+    pool = R.filled_pool("bf16", 4, 1, H, T, D, 3)
+    bounds, ws = ipv.BlockBounds(pool, BLOCK), ipv.alloc_page_workspace("cuda")
+    block_ws = ipv.alloc_blocks_workspace(bounds, 1, A, 1, TOP, T)
+    q = torch.zeros((1, A, 1, D), dtype=torch.bfloat16, device="cuda")
+    lists = torch.zeros((1, H, 1, TOP), dtype=torch.int32, device="cuda")
+    page = torch.zeros(1, dtype=torch.int32, device="cuda")
+    keep = torch.zeros((1, 1, H, 5), dtype=torch.int32, device="cuda")
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    for call in (run,
+                 lambda: ipv.ipv_qkv_write(pool, None, 0, 0, q, q[:, :H], q[:, :H], q, ws),
+                 lambda: ipv.ipv_block_bounds(pool, None, [0], [5], bounds, ws),
+                 lambda: ipv.ipv_block_select(pool, None, bounds, 5, 0, 0, q, lists, block_ws),
+                 lambda: ipv.ipv_attend_blocks(pool, None, 5, 0, 0, q, lists, q, block_ws, bounds=bounds),
+                 lambda: ipv.ipv_page_compact(pool, None, page[None], 5, keep, ws),
+                 lambda: ipv.ipv_page_copy(pool, page, page + 1, ws)):
+        with pytest.raises(ipv.IpvError) as e:
+            call()
+        assert e.value.status == ipv.ERR_ARG and "current device is 1" in str(e.value)
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    for t, x in zip(state, before):
+        assert torch.equal(t, x)
+
+
 def test_the_stream_argument():
     pool = R.filled_pool("bf16", 4, 1, H, T, D, 3)
     side, ws = torch.cuda.Stream(), ipv.alloc_page_workspace("cuda")
