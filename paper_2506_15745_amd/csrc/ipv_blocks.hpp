@@ -261,14 +261,14 @@ __device__ __forceinline__ void group_queries(const SelectArgs& a, int64_t at, d
 
 // The list of one query of a head. blockIdx.x: query; .y: head; .z: stream. Eight lanes have a block's bounds, eight blocks
 // a wave at a time, and add up their products in the vector unit: the matrix unit would take 16 queries' time for one.
-// Scores stay in LDS, and no workgroup waits for another. For few queries over up to 64 NR blocks; one token of 16 streams
-// of four heads over 512 blocks of 128 15 us, over 98 8: the way to the rows and back, and the products (64 bits a channel).
-constexpr int kOneThreads = 512;
-template <int FB, int D, int NR>
-__global__ __launch_bounds__(kOneThreads) void k_block_select_one(SelectArgs a) {
+// Scores stay in LDS, and no workgroup waits for another. For few queries over up to 64 NR blocks. 512 threads where each has
+// a CU of its own, else 256, of which a CU holds more: one token of 16 streams of four heads over 512 blocks of 128 15 us
+// (and 19), of 196 tokens over 98 16 (and 22): the way to the rows and back, and the products (64 bits a channel).
+template <int FB, int D, int NR, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_block_select_one(SelectArgs a) {
   constexpr int E = FB == kFmtF32 ? 4 : 2, PER = 16 / E, PIECES = 2 * D / 8 / PER;  // bytes of an element; elements of 16 bytes; of these, a lane's
   constexpr bool HELD = D <= 128;  // the lane's part of the queries in registers
-  constexpr int WAVES = kOneThreads / kWave, AHEAD = PIECES <= 4 ? 4 : PIECES <= 8 ? 2 : 1;  // eights of blocks on their way
+  constexpr int WAVES = THREADS / kWave, AHEAD = PIECES <= 4 ? 4 : PIECES <= 8 ? 2 : 1;  // eights of blocks on their way
   __shared__ __attribute__((aligned(16))) double lds_q[2 * D];
   __shared__ double lds_scores[NR * kWave];
   __shared__ __attribute__((aligned(16))) uint32_t hist[256];

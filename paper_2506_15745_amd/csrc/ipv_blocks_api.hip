@@ -18,13 +18,13 @@ constexpr int32_t kMaxTop = 4096;
 // times that the two ways take, as they were measured, say so. A workgroup: what it takes for all blocks, or what all
 // workgroups take on the card, by the bounds' bytes. Tiles of 16 queries: what they take at least, and the matrix
 // unit's time, by the tiles. E. g. us alone and in tiles, 8 KV heads of 128 in bf16: 16 tokens over 64 blocks 7.0
-// and 15, over 512 14 and 18; 64 over 256 16 and 20, over 512 23 and 23; 128 over 64 15 and 15, over 256 27 and 22; 512
-// over 64 50 and 14, over 512 142 and 36; one token of 64 streams over 256 22 and 32, of one over 512 13 and 9. Heads
-// of 256: 64 over 64 13 and 19, 512 over 256 151 and 36; of 32: 256 over 256 18 and 21, 512 over 64 19 and 12.
+// and 15, over 512 14 and 18; 64 over 256 15 and 20, over 512 21 and 22; 128 over 64 12 and 15, over 256 27 (512 threads) and
+// 21; 512 over 64 50 and 14, over 512 142 and 36; one token of 64 streams over 256 18 and 32, of one over 512 13 and 9.
+// Heads of 256: 64 over 64 10 and 19, 512 over 256 151 and 36; of 32: 256 over 256 18 and 21, 512 over 64 15 and 11.
 bool select_alone(int64_t queries, int32_t of_stream, int32_t units, int32_t padded, int32_t D, int32_t block_bytes) {
   if (padded > 32 * kWave) return false;
   const double bytes = block_bytes, blocks = padded, all = (double)queries * bytes;
-  const double alone = std::max(6000.0 + blocks * bytes / 32, 3000.0 + all * (155 + blocks) * 1e-4);  // ns
+  const double alone = std::max(6000.0 + blocks * bytes / 32, 3000.0 + (double)queries + all * (155 + blocks) * 0.65e-4);  // ns
   const double tiles = 10000.0 + (units < 256 ? 300 * std::min(of_stream, kScoreTile) : 1000) + (double)units * blocks * D / 850;
   return alone < tiles;
 }
@@ -92,8 +92,11 @@ void launch_select(const ipv_page_shape* s, dim3 grid, const SelectArgs& a, hipS
 
 template <int FB, int D>
 void launch_one_d(dim3 grid, const SelectArgs& a, hipStream_t st) {
-  if (a.padded <= 8 * kWave) k_block_select_one<FB, D, 8><<<grid, dim3(kOneThreads), 0, st>>>(a);
-  else k_block_select_one<FB, D, 32><<<grid, dim3(kOneThreads), 0, st>>>(a);
+  const bool few = (int64_t)grid.x * grid.y * grid.z <= 256;
+  if (a.padded <= 8 * kWave && few) k_block_select_one<FB, D, 8, 512><<<grid, dim3(512), 0, st>>>(a);
+  else if (a.padded <= 8 * kWave) k_block_select_one<FB, D, 8, 256><<<grid, dim3(256), 0, st>>>(a);
+  else if (few) k_block_select_one<FB, D, 32, 512><<<grid, dim3(512), 0, st>>>(a);
+  else k_block_select_one<FB, D, 32, 256><<<grid, dim3(256), 0, st>>>(a);
 }
 void launch_one(const ipv_page_shape* s, dim3 grid, const SelectArgs& a, hipStream_t st) {
   const bool f32 = s->format == IPV_PAGES_F32;
