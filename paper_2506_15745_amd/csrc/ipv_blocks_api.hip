@@ -14,6 +14,9 @@ using namespace ipv;
 namespace {
 
 constexpr int32_t kMaxTop = 4096;
+// Tiles of queries from which on a workgroup takes all blocks of its own: 128 of them over 64 blocks 12.8 us so and 18.6
+// shared out among four, over 512 33.5 and 33.7; 64 over 512 33.0 and 26.4.
+constexpr int32_t kOwnBlocks = 128;
 // Whether each query of a launch has a workgroup of its own: for up to 2048 blocks (its scores are in LDS), where the
 // times that the two ways take, as they were measured, say so. A workgroup: what it takes for all blocks, or what all
 // workgroups take on the card, by the bounds' bytes. Tiles of 16 queries: what they take at least, and the matrix
@@ -25,7 +28,7 @@ bool select_alone(int64_t queries, int32_t of_stream, int32_t units, int32_t pad
   if (padded > 32 * kWave) return false;
   const double bytes = block_bytes, blocks = padded, all = (double)queries * bytes;
   const double alone = std::max(6000.0 + blocks * bytes / 32, 3000.0 + (double)queries + all * (155 + blocks) * 0.65e-4);  // ns
-  const double tiles = 10000.0 + (units < 256 ? 300 * std::min(of_stream, kScoreTile) : 1000) + (double)units * blocks * D / 850;
+  const double tiles = 10000.0 + (units < kOwnBlocks ? 300 * std::min(of_stream, kScoreTile) : 1000) + (double)units * blocks * D / 850;
   return alone < tiles;
 }
 constexpr int64_t kScoreBytes = 128ll << 20;  // of scores at a time, where 16 queries of each stream need no more
@@ -133,7 +136,7 @@ ipv_status select_blocks(Select* s, const Counts& c, hipStream_t st) {
       const int32_t y = a.H * ((a.mq + kScoreTile - 1) / kScoreTile);
       // several workgroups share the blocks where tiles of queries alone leave the card empty: two a CU, if LDS takes them
       const int32_t D = s->pool->head_dim, most_wg = D <= 128 ? 512 : 256;
-      const int32_t units = y * nb, x = units >= 256 ? 1 : std::max(1, std::min(a.padded / kScoreTile, most_wg / units));
+      const int32_t units = y * nb, x = units >= kOwnBlocks ? 1 : std::max(1, std::min(a.padded / kScoreTile, most_wg / units));
       if (select_alone((int64_t)nb * a.H * a.mq, a.mq, units, a.padded, D, 2 * D * (s->pool->format == IPV_PAGES_F32 ? 4 : 2))) {
         launch_one(s->pool, dim3((uint32_t)a.mq, (uint32_t)a.H, (uint32_t)nb), a, st);
         IPV_TRY(launched(hipGetLastError()));
@@ -141,7 +144,7 @@ ipv_status select_blocks(Select* s, const Counts& c, hipStream_t st) {
       }
       a.spread = std::max(kMaxParts / units, 1);
       const dim3 grid((uint32_t)x, (uint32_t)y, (uint32_t)nb);
-      if (units >= 256) launch_select<false>(s->pool, grid, a, st);
+      if (units >= kOwnBlocks) launch_select<false>(s->pool, grid, a, st);
       else launch_select<true>(s->pool, grid, a, st);
       IPV_TRY(launched(hipGetLastError()));
     }
