@@ -527,7 +527,8 @@ ipv_status ipv_blocks_workspace_bytes(const ipv_page_shape* pool, int32_t block_
  * pick among the blocks that hold a row j < n_tokens[b], j <= p: the first c of the stream. For KV
  * head h, with the queries q_a of its q_heads / kv_heads heads and a block's bounds lo, hi,
  *   score = sum over a and d of max(q_a[d] lo[d], q_a[d] hi[d]),
- * which is no less than the sum over a of q_a . K_j for any row j of the block. Picked are the
+ * a product of 0 and an infinity counting as 0, NaN where a query's element or a bound is; it is no
+ * less than the sum over a of q_a . K_j for any row j of the block. Picked are the
  * first first_blocks and the last last_blocks of the c blocks and, of the others, those with
  * the highest scores (NaN above all others), ties to the lower block, min(top, c) in all:
  * blocks (int32 [streams, kv_heads, max_rows, top], device, 4-byte aligned) receives them in
