@@ -46,13 +46,18 @@ hipError_t by_shape(const ipv_page_shape* s, const CALL& what) {
   }
 }
 
-// Counts of positions from first[b] on, as ipv_page_write checks them.
+// Whether a grid holds that many workgroups side by side.
+bool in_grid(int64_t blocks) { return blocks * kPageThreads <= kGridThreads; }
+
+// Counts of positions from first[b] on, as ipv_page_write checks them; blocks(b): workgroups that a stream's take.
+template <class BLOCKS>
 ipv_status check_positions(const ipv_page_shape* s, int32_t cols, int32_t streams, const int32_t* first, const int32_t* rows,
-                           const float* rotary, int32_t rotary_rows) {
+                           const float* rotary, int32_t rotary_rows, const BLOCKS& blocks) {
   for (int32_t b = 0; b < streams; ++b) {
     if (rows[b] < 0 || first[b] < 0) return IPV_ERR_SHAPE;
     const int64_t end = (int64_t)first[b] + rows[b];
     if (rows[b] > 0 && end > table_rows(s, cols)) return IPV_ERR_SHAPE;
+    if (!in_grid(blocks(b))) return IPV_ERR_SHAPE;
     if (rows[b] > 0 && rotary && end > rotary_rows) return IPV_ERR_ARG;
   }
   return IPV_OK;
@@ -82,7 +87,11 @@ ipv_status ipv_qkv_write(const ipv_page_shape* pool, void* K_pages, void* V_page
   IPV_TRY(check_strides(out_strides, 3));
   if (layer < 0 || layer >= pool->layers || q_heads < 1 || q_heads % pool->kv_heads != 0) return IPV_ERR_SHAPE;
   if ((q_norm || k_norm) && (!(eps > 0) || !std::isnormal((float)eps))) return IPV_ERR_ARG;
-  IPV_TRY(check_positions(pool, table_cols, streams, first_row, rows, rotary, rotary_rows));
+  const auto blocks_of = [&](int32_t b) {
+    const int64_t blocks = row_blocks(pool->head_dim, rows[b]);
+    return bounds ? std::max(blocks, touched(first_row[b], rows[b], block_rows)) : blocks;
+  };
+  IPV_TRY(check_positions(pool, table_cols, streams, first_row, rows, rotary, rotary_rows, blocks_of));
   const int32_t kv_groups = (pool->kv_heads + kTokenHeads - 1) / kTokenHeads;
   const int64_t q_groups = ((int64_t)q_heads + kTokenHeads - 1) / kTokenHeads;
   const int64_t groups = q_groups + kv_groups + (bounds ? pool->kv_heads : kv_groups);
@@ -105,8 +114,7 @@ ipv_status ipv_qkv_write(const ipv_page_shape* pool, void* K_pages, void* V_page
     int64_t blocks = 0;
     for (int32_t i = 0; i < nb; ++i) {
       c.first[i] = first_row[b0 + i], c.rows[i] = rows[b0 + i];
-      blocks = std::max(blocks, row_blocks(pool->head_dim, c.rows[i]));
-      if (bounds) blocks = std::max(blocks, touched(c.first[i], c.rows[i], block_rows));
+      blocks = std::max(blocks, blocks_of(b0 + i));
     }
     if (blocks == 0) continue;
     c.b0 = b0;
@@ -131,7 +139,8 @@ ipv_status ipv_block_bounds(const ipv_page_shape* pool, const void* K_pages, con
   if (first_layer < 0 || layers < 1 || layers > pool->layers - first_layer) return IPV_ERR_SHAPE;
   const int64_t slices = (int64_t)layers * pool->kv_heads;
   if (slices > 65535) return IPV_ERR_SHAPE;  // a grid's second dimension
-  IPV_TRY(check_positions(pool, table_cols, streams, first_row, rows, nullptr, 0));
+  const auto blocks_of = [&](int32_t b) { return touched(first_row[b], rows[b], block_rows); };
+  IPV_TRY(check_positions(pool, table_cols, streams, first_row, rows, nullptr, 0, blocks_of));
   IPV_TRY(check_word(ws, ws_bytes, kWsHeader));
   c.bounds = static_cast<char*>(bounds);
   c.err = static_cast<uint32_t*>(ws);
@@ -142,7 +151,7 @@ ipv_status ipv_block_bounds(const ipv_page_shape* pool, const void* K_pages, con
     int64_t blocks = 0;
     for (int32_t i = 0; i < nb; ++i) {
       c.first[i] = first_row[b0 + i], c.rows[i] = rows[b0 + i];
-      blocks = std::max(blocks, touched(c.first[i], c.rows[i], block_rows));
+      blocks = std::max(blocks, blocks_of(b0 + i));
     }
     if (blocks == 0) continue;
     c.b0 = b0;
@@ -166,9 +175,18 @@ ipv_status ipv_page_compact(const ipv_page_shape* pool, void* K_pages, void* V_p
   if (!aligned(new_table, 4) || !aligned(keep_idx, 4) || (rotary && !aligned(rotary, 16))) return IPV_ERR_ALIGN;
   if (new_cols < 1 || C < 1) return IPV_ERR_SHAPE;
   if (2 * c.map.slices > 65535) return IPV_ERR_SHAPE;  // a grid's second dimension
+  const auto blocks_of = [&](int32_t b) {
+    int64_t blocks = 0;
+    for (bool with : {false, bounds != nullptr}) {
+      const int64_t per = compact_run(with, c.map.R.d);
+      blocks = std::max(blocks, (rows[b] + per - 1) / per);
+    }
+    return blocks;
+  };
   for (int32_t b = 0; b < streams; ++b) {
     if (n_tokens[b] < 0 || n_tokens[b] > table_rows(pool, table_cols)) return IPV_ERR_SHAPE;
     if (rows[b] < 0 || rows[b] > C || rows[b] > table_rows(pool, new_cols)) return IPV_ERR_SHAPE;
+    if (!in_grid(blocks_of(b))) return IPV_ERR_SHAPE;
     if (rows[b] > 0 && rotary && (n_tokens[b] > rotary_rows || rows[b] > rotary_rows)) return IPV_ERR_ARG;
   }
   IPV_TRY(check_word(ws, ws_bytes, kWsHeader));
@@ -185,10 +203,7 @@ ipv_status ipv_page_compact(const ipv_page_shape* pool, void* K_pages, void* V_p
     int64_t blocks = 0;
     for (int32_t i = 0; i < nb; ++i) {
       c.n[i] = n_tokens[b0 + i], c.rows[i] = rows[b0 + i];
-      for (bool with : {false, bounds != nullptr}) {
-        const int64_t per = compact_run(with, c.map.R.d);
-        blocks = std::max(blocks, (c.rows[i] + per - 1) / per);
-      }
+      blocks = std::max(blocks, blocks_of(b0 + i));
     }
     if (blocks == 0) continue;
     c.b0 = b0;
