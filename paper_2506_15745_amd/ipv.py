@@ -1124,15 +1124,20 @@ class PageTables:
 
     def compact(self, streams, n_tokens, keep_idx, ws, rows=None, rotary=None, bounds=None):
         """ipv_page_compact of these streams, keep_idx [len(streams), L, H, C], into pages of their own; those that they had go
-        back. It takes free pages for all new rows first; without enough nothing changes and the call raises."""
+        back. It takes free pages for all new rows first; without enough, or with more rows (n_tokens) than a stream has pages
+        for, nothing changes and the call raises."""
         self._stream_of(*streams)
         if len(set(streams)) != len(streams):
             raise IpvError(ERR_ARG, "a stream is named twice")
         if not streams:
             return
+        held = _host_counts(n_tokens, len(streams), "n_tokens")
         counts_ = _host_counts(keep_idx.shape[-1] if rows is None else rows, len(streams), "rows")
-        if min(counts_) < 0:
+        if min(counts_) < 0 or min(held) < 0:
             raise IpvError(ERR_SHAPE, "negative rows")
+        for b, n in zip(streams, held):
+            if n > len(self.pages[b]) * self.pool.shape.page_rows:
+                raise IpvError(ERR_SHAPE, "stream %d has no %d rows" % (b, n))
         cols = [self._columns_of(r) for r in counts_]
         self._have(sum(cols))
         had = [self.pages[b] for b in streams]
