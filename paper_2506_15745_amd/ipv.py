@@ -979,7 +979,7 @@ def ipv_page_compact(pool, page_table, new_table, n_tokens, keep_idx, ws, rows=N
     """Row j < rows[b] (all C if None) of every slice of stream b, in the pages of new_table[b], becomes row keep_idx[b, l, h, j]
     (int32 [B, L, H, C], as ipv_select writes it) of the n_tokens[b] rows in the pages of page_table[b], which may not be
     among the new ones. With rotary keys are turned from the position that they had to the one that they get; bounds
-    (BlockBounds, or None) of the new blocks are made."""
+    (BlockBounds, or None) of the new blocks are made. Without rows (C = 0 as well) the call does nothing."""
     s, shape, table, cols = pool.shape, keep_idx.shape, None, 1
     if keep_idx.dtype is not torch.int32 or len(shape) != 4 or tuple(shape[1:3]) != (s.layers, s.kv_heads):
         raise IpvError(ERR_SHAPE, "keep_idx must be int32 [B, %d, %d, C]" % (s.layers, s.kv_heads))
@@ -991,11 +991,13 @@ def ipv_page_compact(pool, page_table, new_table, n_tokens, keep_idx, ws, rows=N
     new, new_cols = _table(pool, new_table, B)
     _same_gpu(pool, ws, keep_idx=keep_idx)
     n, counts_ = _host_counts(n_tokens, B, "n_tokens"), _host_counts(C if rows is None else rows, B, "rows")
-    at = _ptr(ws)
+    if C == 0 and any(counts_):
+        raise IpvError(ERR_SHAPE, "more rows than keep_idx's 0")
+    at = _ptr(ws)  # also stands for a tensor without elements, whose own address is null
     angles, positions = _angle_args(pool, rotary, at)
     bound, block_rows = _bounds_args(pool, bounds)
     rc = _paged().ipv_page_compact(*pool._args, bound, block_rows, table, cols, new, new_cols, B, n.buffer_info()[0], _ptr(keep_idx) or at,
-                                   C, counts_.buffer_info()[0], angles, positions, at, ws.nbytes, _pool_stream(pool, stream))
+                                   C or 1, counts_.buffer_info()[0], angles, positions, at, ws.nbytes, _pool_stream(pool, stream))
     if rc != OK:
         _check(rc, "ipv_page_compact")
 
