@@ -580,6 +580,15 @@ def _host_counts(values, streams, what):
         raise IpvError(ERR_SHAPE, "%s holds a count of more than 32 bits" % what) from None
 
 
+def _query_counts(q_rows, streams, most):
+    """A host array of each stream's queries (None: all). The library sees one at the least as the most that there are: tensors
+    of none are checked here."""
+    rows = _host_counts(most if q_rows is None else q_rows, streams, "q_rows")
+    if most == 0 and any(rows):
+        raise IpvError(ERR_SHAPE, "more queries than the tensor's 0")
+    return rows
+
+
 _I32 = 2**31
 
 
@@ -720,7 +729,7 @@ def ipv_attend(pool, page_table, n_tokens, q_first, layer, q, out, ws, q_rows=No
     if ws is None or ws.get_device() != dev or q.get_device() != dev or out.get_device() != dev:
         _same_gpu(pool, ws, q=q, out=out)
     n, first = _host_counts(n_tokens, B, "n_tokens"), _host_counts(q_first, B, "q_first")
-    rows = _host_counts(M if q_rows is None else q_rows, B, "q_rows")
+    rows = _query_counts(q_rows, B, M)
     q_strides, out_strides = q.stride(), out.stride()
     q_at = _stride_array(q_strides, shape)
     if 0 in out_strides:
@@ -920,7 +929,7 @@ def ipv_block_select(pool, page_table, bounds, n_tokens, q_first, layer, q, bloc
     listed, top = _lists(pool, blocks, B, M)
     _same_gpu(pool, ws, q=q)
     n, first = _host_counts(n_tokens, B, "n_tokens"), _host_counts(q_first, B, "q_first")
-    rows = _host_counts(M if q_rows is None else q_rows, B, "q_rows")
+    rows = _query_counts(q_rows, B, M)
     _whole32("layer, first_blocks, last_blocks", layer, first_blocks, last_blocks)
     at = _ptr(ws)
     _check(_paged().ipv_block_select(pool._args[0], bound, block_rows, table, cols, B, n.buffer_info()[0], first.buffer_info()[0],
@@ -958,7 +967,7 @@ def ipv_attend_blocks(pool, page_table, n_tokens, q_first, layer, q, blocks, out
     if ws is None or ws.get_device() != dev or q.get_device() != dev or out.get_device() != dev:
         _same_gpu(pool, ws, q=q, out=out)
     n, first = _host_counts(n_tokens, B, "n_tokens"), _host_counts(q_first, B, "q_first")
-    rows = _host_counts(M if q_rows is None else q_rows, B, "q_rows")
+    rows = _query_counts(q_rows, B, M)
     q_strides, out_strides = q.stride(), out.stride()
     q_at = _stride_array(q_strides, shape)
     if 0 in out_strides:

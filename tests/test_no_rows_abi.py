@@ -33,3 +33,30 @@ def test_compaction(host, rows, status):
     except ipv.IpvError as e:
         got = e.status
     assert got == status
+
+
+def attend(pool, ws, q, blocks, lse, **kw):
+    ipv.ipv_attend(pool, torch.zeros((1, 3), dtype=torch.int32), [40], [5], 0, q, q, ws, lse=lse, **kw)
+
+
+def attend_blocks(pool, ws, q, blocks, lse, **kw):
+    ipv.ipv_attend_blocks(pool, torch.zeros((1, 3), dtype=torch.int32), [40], [5], 0, q, blocks, q, ws, block_rows=16, lse=lse, **kw)
+
+
+def select(pool, ws, q, blocks, lse, **kw):
+    bounds = object.__new__(ipv.BlockBounds)
+    bounds.pool, bounds.block_rows, bounds._at = pool, 16, ws.data_ptr()
+    ipv.ipv_block_select(pool, torch.zeros((1, 3), dtype=torch.int32), bounds, [40], [5], 0, q, blocks, ws, **kw)
+
+
+@pytest.mark.parametrize("call", [attend, attend_blocks, select])
+@pytest.mark.parametrize("rows,status", [(None, ipv.OK), (0, ipv.OK), ([0], ipv.OK), ([1], ipv.ERR_SHAPE), (1, ipv.ERR_SHAPE), ([-1], ipv.ERR_SHAPE)])
+def test_queries(host, call, rows, status):
+    """A query of tensors that hold none would be read from the workspace, and its result written there."""
+    pool, ws = host
+    got = ipv.OK
+    try:
+        call(pool, ws, torch.zeros((1, 4, 0, 64), dtype=torch.bfloat16), torch.zeros((1, 2, 0, 5), dtype=torch.int32), torch.zeros((1, 4, 0)), q_rows=rows)
+    except ipv.IpvError as e:
+        got = e.status
+    assert got == status
