@@ -3,8 +3,10 @@
 // A block's score for a query's group of heads is the sum over the heads a and the channels d of
 // max(q_a[d] lo[d], q_a[d] hi[d]), lo and hi the bounds of its keys: with
 // Q+[d] = sum_a max(q_a[d], 0) and Q-[d] = sum_a min(q_a[d], 0) that is Q+ . hi + Q- . lo, one product of
-// 2 D terms whatever the number of heads. It is taken in 64 bits by the matrix unit: equal bounds give
-// equal scores, and no rounding decides between blocks that differ.
+// 2 D terms whatever the number of heads. It is taken in 64 bits, by the vector or the matrix unit: within a call bounds of the
+// same bits give scores of the same bits, and scores that differ by more than the rounding of a 64-bit sum of 2 D terms
+// are ordered as they are. Closer ones may be ordered either way, and otherwise in a call of other sizes, whose sums run in
+// another order.
 #pragma once
 
 #include "ipv_attend.hpp"
@@ -35,7 +37,8 @@ struct SelectArgs {
   int32_t* blocks;
   uint32_t* err;
   uint32_t* arrived;  // workgroups of a tile of queries that have left their scores: zero before and after a call
-  int32_t spread;     // counters from one to the next: apart, since one line takes them one after the other
+  int32_t spread;     // counters from one to the next: apart, since one line takes them one after the other (up to 32 tiles of
+                      // queries have a line each, 127 of them 32 bytes)
   int32_t n[kAttendStreams], first[kAttendStreams], rows[kAttendStreams];
 };
 
@@ -295,7 +298,8 @@ __device__ __forceinline__ double score_by_terms(const SelectArgs& a, int b, int
 // a wave at a time, and add up their products in the vector unit: the matrix unit would take 16 queries' time for one.
 // Scores stay in LDS, and no workgroup waits for another. For few queries over up to 64 NR blocks. 512 threads where each has
 // a CU of its own, else 256, of which a CU holds more: one token of 16 streams of four heads over 512 blocks of 128 15 us
-// (and 19), of 196 tokens over 98 16 (and 22): the way to the rows and back, and the products (64 bits a channel).
+// by trace (and 19; 12.3 in a captured run of calls), of 196 tokens over 98 16 (and 22): the way to the bounds, and the
+// products (64 bits a channel).
 template <int FB, int D, int NR, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_block_select_one(SelectArgs a) {
   constexpr int E = FB == kFmtF32 ? 4 : 2, PER = 16 / E, PIECES = 2 * D / 8 / PER;  // bytes of an element; elements of 16 bytes; of these, a lane's
@@ -412,7 +416,8 @@ __device__ __forceinline__ int select_place(int ch, int col) {
 // of blocks or, where there are few queries (SPLIT), a quarter of its steps, added up through LDS: then the way through
 // all of them is what a tile costs. The scores go to memory; the workgroup, the last one to come where several share the
 // blocks, picks from them. Bound by the 64-bit products where there are many queries (1024 tokens of 8 KV heads over 512
-// blocks 61 to 68 us, 33 of them the products at the rate of a large one), by the trips to memory for one (9 us).
+// blocks: 62 us in a captured run of such calls, 64 to 76 by trace, 33 of them the products at the rate of a large one; the matrix
+// unit is busy for 48% of the cycles); for one by the trips to table, bounds, scores, counter and scores again (9, and 10 to 13).
 template <int FB, int D, int NR, bool SPLIT>
 __global__ __launch_bounds__(select_threads(FB, D, SPLIT), select_waves(FB, D, SPLIT)) void k_block_select(SelectArgs a) {
   constexpr int THREADS = select_threads(FB, D, SPLIT), SELECT_WAVES = THREADS / kWave;

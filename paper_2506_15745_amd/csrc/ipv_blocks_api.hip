@@ -20,8 +20,8 @@ constexpr int32_t kOwnBlocks = 128;
 // Whether each query of a launch has a workgroup of its own: for up to 2048 blocks (its scores are in LDS), where the
 // times that the two ways take, as they were measured, say so. A workgroup: what it takes for all blocks, or what all
 // workgroups take on the card, by the bounds' bytes. Tiles of 16 queries: what they take at least, and the matrix
-// unit's time, by the tiles. E. g. us alone and in tiles, 8 KV heads of 128 in bf16: 16 tokens over 64 blocks 7.0
-// and 15, over 512 14 and 18; 64 over 256 15 and 20, over 512 21 and 22; 128 over 64 12 and 15, over 256 27 (512 threads) and
+// unit's time, by the tiles. E. g. us alone and in tiles (captured runs of calls), 8 KV heads of 128 in bf16: 16 tokens over
+// 64 blocks 7.0 and 15, over 512 14 and 18; 64 over 256 15 and 20, over 512 21 and 22; 128 over 64 12 and 15, over 256 27 (512 threads) and
 // 21; 512 over 64 50 and 14, over 512 142 and 36; one token of 64 streams over 256 18 and 32, of one over 512 13 and 9.
 // Heads of 256: 64 over 64 10 and 19, 512 over 256 151 and 36; of 32: 256 over 256 18 and 21, 512 over 64 15 and 11.
 bool select_alone(int64_t queries, int32_t of_stream, int32_t units, int32_t padded, int32_t D, int32_t block_bytes) {

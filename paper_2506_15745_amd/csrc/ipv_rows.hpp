@@ -279,8 +279,8 @@ __device__ __forceinline__ void load_norm(const float* norm, int d, int half, fl
 // blockIdx.z: stream; .y: heads, kTokenHeads of the queries, then of the values, then of the keys (with
 // bounds one head of those); .x: positions (with bounds, of the keys: a block that has new rows, whose
 // older rows are read for its bounds). Bound by the rows' bytes: 6272 tokens of 64 heads and 8 KV heads of 128
-// with bounds, 260 MB, in 54.8 us (4.7 TB/s); one token of 16 streams of 28 and 4 heads 5.1 us, the way to the older
-// rows and back.
+// with bounds, 260 MB, in 55 to 58 us (4.5 to 4.7 TB/s); one token of 16 streams of 28 and 4 heads 4.9 to 5.7 us, the way to
+// the older rows and back; 196 tokens of 4 streams in e4m3 7.4, of whose five waves a CU 60% of the cycles are waits for memory.
 template <int F, int SRC, int D>
 __global__ __launch_bounds__(kPageThreads) void k_qkv_write(TokenCall c) {
   using S = RowSplit<D>;
@@ -390,7 +390,8 @@ struct BoundsCall {
 };
 
 // blockIdx.x: a block that holds one of the positions; .y: slice; .z: stream. Bound by the keys' bytes: 6272 rows of 28
-// layers of 4 heads of 128 take 73 us in fp32 (371 MB, 5.1 TB/s), 28 in bf16; in e2m1 25, where unpacking counts.
+// layers of 4 heads of 128 take 73 us in fp32 (371 MB, 5.1 TB/s), 28 in bf16; in e2m1 25, for whose unpacking and comparing
+// the vector unit is busy throughout.
 template <int F, int D>
 __global__ __launch_bounds__(kPageThreads) void k_block_bounds(BoundsCall c) {
   using S = RowSplit<D>;

@@ -1111,7 +1111,9 @@ class PageTables:
             self._publish()
 
     def fork(self, stream, to, n_tokens):
-        """Stream `to` has the pages of the first n_tokens rows of `stream`, instead of those that it had."""
+        """Stream `to` has the pages of the first n_tokens rows of `stream`, instead of those that it had. Bounds of the last
+        block are still those of all the rows that are there, which selection for `to` sees (no score comes out too low) until
+        rows are written to that block (ipv_qkv_write makes them anew) or, in a page of its own (reserve), ipv_block_bounds does."""
         self._stream_of(stream, to)
         cols = self._columns_of(n_tokens)
         if n_tokens < 0 or cols > len(self.pages[stream]):
@@ -1124,7 +1126,8 @@ class PageTables:
         self._publish()
 
     def free(self, stream, n_tokens=0):
-        """The pages behind the first n_tokens rows of a stream go back."""
+        """The pages behind the first n_tokens rows of a stream go back. Bounds of the last block that is left are those of all
+        the rows that are there, as after fork."""
         self._stream_of(stream)
         if n_tokens < 0:
             raise IpvError(ERR_SHAPE, "negative rows")
