@@ -262,36 +262,14 @@ __device__ __forceinline__ void group_queries(const SelectArgs& a, int64_t at, d
   }
 }
 
-// A score term by term, in the whole wave: q hi or q lo by the sign of q, where 0 times an infinity counts as 0. The product
-// form makes NaN of that (a side to which no query adds is 0 times that side's bound), and nothing but NaN: other scores are
-// right as they are, and only those that came out as NaN are made here, after the loops over the blocks. A NaN bound or query
-// stays one. Bounds that are finite pay the comparison (1024 tokens over 512 blocks 61.4 and 61.8 us); with an infinite channel in
-// every block, a score in 256 made so, those take 340.
-template <int FB, int D>
-__device__ __forceinline__ double score_by_terms(const SelectArgs& a, int b, int h, int i, int32_t j) {
-  constexpr int E = FB == kFmtF32 ? 4 : 2;
-  const auto element = [](const char* base, int64_t at) __attribute__((always_inline)) {
-    if constexpr (FB == kFmtF32) return *reinterpret_cast<const float*>(base + at * 4);
-    else return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(base + at * 2) << 16);
-  };
-  const int lane = threadIdx.x % kWave;
-  const uint32_t p = (uint32_t)j * a.map.R.d;
-  int32_t page = a.table ? a.table[(int64_t)(a.b0 + b) * a.cols + fast_div(p, a.T)] : a.b0 + b;
-  if ((uint32_t)page >= (uint32_t)a.pages) page = 0;  // (reported where it is met first)
-  const char* bounds = a.bounds + a.map.block(page, (uint32_t)(a.layer * a.H + h), p, a.T) * (2 * D * E);
-  const int64_t q0 = (int64_t)(a.b0 + b) * a.q_b + (int64_t)h * a.G * a.q_h + (int64_t)i * a.q_m;
-  double s = 0;
-  for (int d = lane; d < D; d += kWave) {
-    const float lo = element(bounds, d), hi = element(bounds, D + d);
-    if (lo != lo || hi != hi) s = __builtin_nan("");
-    for (int g = 0; g < a.G; ++g) {
-      const float q = element(a.q, q0 + (int64_t)g * a.q_h + d), k = q > 0.f ? hi : lo;
-      s += q == 0.f || (k == 0.f && q == q) ? 0.0 : (double)q * (double)k;
-    }
-  }
-  s = group_sum64<16>(s);
-  s += __builtin_bit_cast(double, shfl64(__builtin_bit_cast(int64_t, s), lane ^ 16));
-  return s + __builtin_bit_cast(double, shfl64(__builtin_bit_cast(int64_t, s), lane ^ 32));
+// A term of a score where the product form came out as NaN: 0 times an infinity counts as 0, as on a side to which no query adds
+// against that side's infinite bound (a group's sum is 0 only if each of its parts is). Such scores, and no others, are made
+// again so after the loops over the blocks; a NaN bound or query stays one. Bounds that are finite pay the comparison (1024 tokens
+// over 512 blocks 61.4 and 61.8 us, 256 over 256 of heads of 32 16.9 and 18.1); with a NaN in every block or query those 1024 take
+// 0.4 ms (made again a score at a time by a whole wave: 4.2).
+__device__ __forceinline__ double score_term(double q, float bound) {
+  const double p = q * (double)bound;
+  return p != p && q == q && bound == bound ? 0.0 : p;
 }
 
 // The list of one query of a head. blockIdx.x: query; .y: head; .z: stream. Eight lanes have a block's bounds, eight blocks
@@ -322,10 +300,13 @@ __global__ __launch_bounds__(THREADS) void k_block_select_one(SelectArgs a) {
     const uint32_t p = (uint32_t)min(j0 + own, count - 1) * a.map.R.d;
     return a.table ? a.table[(int64_t)(a.b0 + b) * a.cols + fast_div(p, a.T)] : a.b0 + b;
   };
-  const auto load_block = [&](int j0, int32_t page) __attribute__((always_inline)) {
+  const auto bounds_of = [&](int j0, int32_t page) __attribute__((always_inline)) {
     const uint32_t p = (uint32_t)min(j0 + own, count - 1) * a.map.R.d;
     if ((uint32_t)page >= (uint32_t)a.pages) page = 0, bad = true;
-    const char* at = a.bounds + a.map.block(page, (uint32_t)(a.layer * a.H + h), p, a.T) * (2 * D * E) + part * 16;
+    return a.bounds + a.map.block(page, (uint32_t)(a.layer * a.H + h), p, a.T) * (2 * D * E) + part * 16;
+  };
+  const auto load_block = [&](int j0, int32_t page) __attribute__((always_inline)) {
+    const char* at = bounds_of(j0, page);
     Piece x;
 #pragma unroll
     for (int c = 0; c < PIECES; ++c) x.r[c] = load16(at + c * 128);
@@ -386,14 +367,20 @@ __global__ __launch_bounds__(THREADS) void k_block_select_one(SelectArgs a) {
     odd |= s != s;
     if (part == 0 && j0 + own < count) lds_scores[j0 + own] = s;
   }
-  if (__ballot(odd) != 0) {  // the wave's own once more
-    asm volatile("" ::: "memory");
-    for (int j1 = wave * 8; j1 < count; j1 += STEP)
-      for (int j = j1; j < min(j1 + 8, count); ++j) {
-        if (lds_scores[j] == lds_scores[j]) continue;  // (the same in all lanes)
-        const double v = score_by_terms<FB, D>(a, b, h, i, j);
-        if (lane == 0) lds_scores[j] = v;
+  if (__ballot(odd) != 0) {  // the wave's blocks once more
+    for (int j1 = wave * 8; j1 < count; j1 += STEP) {
+      const char* at = bounds_of(j1, page_of(j1));
+      double s = 0;
+#pragma unroll 1
+      for (int c = 0; c < PIECES; ++c) {
+        float f[PER];
+        Lane<std::conditional_t<FB == kFmtF32, float, uint16_t>>::decode(load16(at + c * 128), f);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) s += score_term(query(c, e), f[e]);
       }
+      s = group_sum64<8>(s);
+      if (part == 0 && j1 + own < count && lds_scores[j1 + own] != lds_scores[j1 + own]) lds_scores[j1 + own] = s;
+    }
   }
   if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, kDevBadPage);
   __syncthreads();
@@ -544,16 +531,24 @@ __global__ __launch_bounds__(select_threads(FB, D, SPLIT), select_waves(FB, D, S
     for (int tile = first; tile < tiles; tile += step)
       for (int e = 0; e < (SPLIT ? 1 : 4); ++e) {
         const int x = SPLIT ? (int)threadIdx.x : e * kWave + lane, col = x % kScoreTile, j = tile * kScoreTile + x / kScoreTile;
-        double* at = scores_of(a, b, h, min(i0 + col, i1 - 1)) + j;
-        const bool mine = i0 + col < i1 && j < most;
+        double* to = scores_of(a, b, h, min(i0 + col, i1 - 1)) + j;
         uint64_t v = 0;
-        if (mine) v = __hip_atomic_load(reinterpret_cast<uint64_t*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (i0 + col < i1 && j < most) v = __hip_atomic_load(reinterpret_cast<uint64_t*>(to), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         const double was = __builtin_bit_cast(double, v);
-        for (uint64_t m = __ballot(was != was); m != 0; m &= m - 1) {
-          const int from = __builtin_ctzll(m);
-          const double y = score_by_terms<FB, D>(a, b, h, i0 + __builtin_amdgcn_readlane(col, from), __builtin_amdgcn_readlane(j, from));
-          if (lane == from) put(at, y);
+        if (__ballot(was != was) == 0) continue;
+        const uint32_t p = (uint32_t)min(j, most - 1) * a.map.R.d;
+        int32_t there = a.table ? a.table[(int64_t)(a.b0 + b) * a.cols + fast_div(p, a.T)] : a.b0 + b;
+        if ((uint32_t)there >= (uint32_t)a.pages) there = 0;
+        const int64_t at = a.map.block(there, (uint32_t)(a.layer * a.H + h), p, a.T) * (2 * D);
+        double s = 0;
+#pragma unroll 1
+        for (int ch = 0; ch < 2 * D; ch += 8) {
+          float f[8];
+          load_row8<FB>(a.bounds, at + ch, f);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s += score_term(lds[select_place(ch + i, col)], f[i]);
         }
+        if (was != was) put(to, s);
       }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
