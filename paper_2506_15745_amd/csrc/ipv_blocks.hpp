@@ -403,7 +403,7 @@ __device__ __forceinline__ int select_place(int ch, int col) {
 // of blocks or, where there are few queries (SPLIT), a quarter of its steps, added up through LDS: then the way through
 // all of them is what a tile costs. The scores go to memory; the workgroup, the last one to come where several share the
 // blocks, picks from them. Bound by the 64-bit products where there are many queries (1024 tokens of 8 KV heads over 512
-// blocks: 62 us in a captured run of such calls, 64 to 76 by trace, 33 of them the products at the rate of a large one; the matrix
+// blocks: 62 us in a captured run of such calls, 63 to 76 by trace, 33 of them the products at the rate of a large one; the matrix
 // unit is busy for 48% of the cycles); for one by the trips to table, bounds, scores, counter and scores again (9, and 10 to 13).
 template <int FB, int D, int NR, bool SPLIT>
 __global__ __launch_bounds__(select_threads(FB, D, SPLIT), select_waves(FB, D, SPLIT)) void k_block_select(SelectArgs a) {
